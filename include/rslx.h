@@ -459,6 +459,93 @@ int32_t rslx_rnd(const rslx_mlp* target, const rslx_mlp* predictor, const float*
                  float weight, int32_t update_stats, float* r_int_out, float* rewards_inout_or_null,
                  void* ws, size_t ws_bytes, void* stream);
 
+/* ---- linear attention with a decay for each head (a memory over whole sequences) ------------- */
+
+/* Types of the activations of the operators from here on; parameters, states and statistics are fp32. */
+#define RSLX_F32 0
+#define RSLX_BF16 1
+#define RSLX_F16 2
+
+/* A matrix [T, N, H, width] (steps, sequences or environments, heads): element (t, n, h, i) lies at
+ * data + t*step + n*seq + h*head + i, strides in elements.  Inputs may have any strides, zero among
+ * them (a row shared by heads or sequences; its gradient then comes per head, for the caller to add
+ * up); rows of outputs must not overlap.  `data` is aligned to its type; where all of a call's matrices
+ * start at multiples of 16 bytes, with widths and strides of whole 16 bytes, they are moved 16 bytes
+ * at a time. */
+typedef struct rslx_seq_view {
+  void* data;
+  int64_t step, seq, head;
+} rslx_seq_view;
+
+/* With l_h = exp(log_decay[h]), per sequence n and head h, state S [Dk, Dv]:
+ *   S_t = l keep_{t-1} S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t,   S_{-1} = s0 (0 if NULL), keep_{-1} = 1
+ * keep_t = 0 where dones[t, n] is set: the state is zeroed after every step that ends an episode, as in
+ * rslx_ppo_update_recurrent.  s_last = keep_{T-1} S_{T-1} is what the next call starts from: a sequence
+ * in two calls gives what one call gives, up to rounding.  With lengths, sequence n has the first
+ * lengths[n] steps only (values outside 0..T count as 0 or T): behind them outputs and gradients are
+ * zero, inputs are not looked at, and s_last is the state behind the last step that exists (s0 if none does).
+ * log_decay is at most 0 in earnest (-inf: no memory); it is a constant of the layer and has no gradient.
+ * What is not finite stays where the recurrence above puts it: a step's values reach no earlier step
+ * and no other episode. */
+#define RSLX_ATTN_MAX_DIM 128
+typedef struct rslx_linear_attn {
+  int32_t dtype;                 /* RSLX_F32, RSLX_BF16, RSLX_F16: q, k, v, o and their gradients */
+  int32_t T, N, H;
+  int32_t Dk, Dv;                /* 1..RSLX_ATTN_MAX_DIM */
+  float scale;
+  const float* log_decay;        /* device [H] */
+  const uint8_t* dones;          /* device [T, N] or NULL */
+  const int32_t* lengths;        /* device [N] or NULL */
+} rslx_linear_attn;
+
+/* The whole sequence.  q, k: width Dk; v, o: width Dv; s0, s_last: device [N, H, Dk, Dv] or NULL (s_last may be
+ * the buffer of s0).  o must not overlap an input.  A few long sequences are walked in pieces side by side, which
+ * takes workspace; otherwise ws may be NULL. */
+size_t rslx_linear_attention_workspace_bytes(const rslx_linear_attn* a);
+int32_t rslx_linear_attention(const rslx_linear_attn* a, const rslx_seq_view* q, const rslx_seq_view* k,
+                              const rslx_seq_view* v, const float* s0_or_null, const rslx_seq_view* o,
+                              float* s_last_or_null, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients of a loss L through the call above, from those of its outputs, d_o and ds_last (NULL = 0):
+ *   dS_t = scale q_t d_o_t^T + keep_t (t + 1 < T ? l dS_{t+1} : ds_last)
+ *   dq_t = scale S_t d_o_t,   dk_t = dS_t v_t,   dv_t = dS_t^T k_t,   ds0 = l dS_0 (ds_last where there is no step)
+ * Nothing is kept from the forward call: states are walked again.  ds0 (or NULL) must not overlap s0 or ds_last;
+ * dq, dk, dv must not overlap an input. */
+size_t rslx_linear_attention_backward_workspace_bytes(const rslx_linear_attn* a);
+int32_t rslx_linear_attention_backward(const rslx_linear_attn* a, const rslx_seq_view* q, const rslx_seq_view* k,
+                                       const rslx_seq_view* v, const float* s0_or_null, const rslx_seq_view* d_o,
+                                       const float* ds_last_or_null, const rslx_seq_view* dq, const rslx_seq_view* dk,
+                                       const rslx_seq_view* dv, float* ds0_or_null, void* ws, size_t ws_bytes,
+                                       void* stream);
+
+/* One step of every environment, while acting (a->T = 1, dones and lengths NULL; the views' step is not used):
+ *   s_out = (reset[n] ? 0 : l s_in) + k v^T,   o = scale s_out^T q
+ * reset_or_null (device uint8 [N]) carries the previous step's episode-end flags, as in rslx_act_recurrent;
+ * s_in (NULL = 0) and s_out may be one buffer. */
+int32_t rslx_linear_attention_step(const rslx_linear_attn* a, const rslx_seq_view* q, const rslx_seq_view* k,
+                                   const rslx_seq_view* v, const uint8_t* reset_or_null, const float* s_in_or_null,
+                                   float* s_out, const rslx_seq_view* o, void* stream);
+
+/* ---- layer norm ------------------------------------------------------------------------ */
+
+/* Per row:  m = mean x,  r = 1 / sqrt(mean (x - m)^2 + eps),  y = (x - m) r weight + bias.
+ * x, y: [rows, cols] of `dtype`, rows ldx and ldy elements apart (y may be x); weight, bias: device fp32 [cols],
+ * NULL = 1 and 0.  mean, rstd: device fp32 [rows] or NULL; the backward pass reads them. */
+#define RSLX_NORM_MAX_COLS 16384
+int32_t rslx_layer_norm(int32_t dtype, const void* x, int64_t ldx, int64_t rows, int32_t cols,
+                        const float* weight_or_null, const float* bias_or_null, float eps, void* y, int64_t ldy,
+                        float* mean_or_null, float* rstd_or_null, void* stream);
+
+/* With g = dy weight and h = (x - mean) rstd:  dx = rstd (g - mean(g) - h mean(g h)) per row,
+ * dweight = sum over rows of dy h, dbias = sum over rows of dy (device fp32 [cols]; zero where there are no rows).
+ * Any of dx, dweight, dbias may be NULL; dx may be dy or x.  The sums are taken in a fixed order: the same inputs give
+ * the same bits.  Without dweight and dbias no workspace is needed. */
+size_t rslx_layer_norm_backward_workspace_bytes(int64_t rows, int32_t cols);
+int32_t rslx_layer_norm_backward(int32_t dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                                 int64_t rows, int32_t cols, const float* weight_or_null, const float* mean,
+                                 const float* rstd, void* dx_or_null, int64_t lddx, float* dweight_or_null,
+                                 float* dbias_or_null, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

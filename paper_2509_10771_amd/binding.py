@@ -16,6 +16,9 @@ __all__ = [
     "rslx_ppo_update_recurrent_workspace_bytes", "rslx_ppo_update_recurrent", "rslx_memory_step_workspace_bytes",
     "rslx_memory_step", "rslx_bc_update_recurrent_workspace_bytes", "rslx_bc_update_recurrent",
     "rslx_act_recurrent_dc", "rslx_ppo_update_recurrent_dc", "rslx_gae_noalloc", "GAE_NOALLOC_MAX_ENVS",
+    "LinearAttn", "ATTN_MAX_DIM", "NORM_MAX_COLS", "rslx_linear_attention_workspace_bytes", "rslx_linear_attention",
+    "rslx_linear_attention_backward_workspace_bytes", "rslx_linear_attention_backward", "rslx_linear_attention_step",
+    "rslx_layer_norm", "rslx_layer_norm_backward_workspace_bytes", "rslx_layer_norm_backward",
 ]
 
 MAX_LAYERS = 8
@@ -32,9 +35,13 @@ EXPORTS = [
     "rslx_act_recurrent_workspace_bytes", "rslx_act_recurrent", "rslx_ppo_update_recurrent_workspace_bytes",
     "rslx_ppo_update_recurrent", "rslx_memory_step_workspace_bytes", "rslx_memory_step",
     "rslx_bc_update_recurrent_workspace_bytes", "rslx_bc_update_recurrent", "rslx_act_recurrent_dc",
-    "rslx_ppo_update_recurrent_dc", "rslx_gae_noalloc",
+    "rslx_ppo_update_recurrent_dc", "rslx_gae_noalloc", "rslx_linear_attention_workspace_bytes", "rslx_linear_attention",
+    "rslx_linear_attention_backward_workspace_bytes", "rslx_linear_attention_backward", "rslx_linear_attention_step",
+    "rslx_layer_norm", "rslx_layer_norm_backward_workspace_bytes", "rslx_layer_norm_backward",
 ]
 GAE_NOALLOC_MAX_ENVS = 1 << 20
+ATTN_MAX_DIM = 128
+NORM_MAX_COLS = 16384
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "librslx.so")
 
@@ -95,6 +102,15 @@ class _CBcCfg(C.Structure):
 
 class _CTraceRecord(C.Structure):
     _fields_ = [("kernel", C.c_char * 48), ("flops", C.c_double), ("bytes", C.c_double), ("ms", C.c_float)]
+
+
+class _CSeqView(C.Structure):
+    _fields_ = [("data", _vp), ("step", C.c_int64), ("seq", C.c_int64), ("head", C.c_int64)]
+
+
+class _CLinearAttn(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("T", C.c_int32), ("N", C.c_int32), ("H", C.c_int32), ("Dk", C.c_int32), ("Dv", C.c_int32),
+                ("scale", C.c_float), ("log_decay", _vp), ("dones", _vp), ("lengths", _vp)]
 
 
 def _sig(name, restype, argtypes):
@@ -158,6 +174,18 @@ _sig("rslx_rnd", C.c_int32, [_P(_CMlp), _P(_CMlp), _vp, C.c_int32, C.c_int32, _v
                              _vp, _vp, _vp, C.c_size_t, _vp])
 
 
+_sig("rslx_linear_attention_workspace_bytes", C.c_size_t, [_P(_CLinearAttn)])
+_sig("rslx_linear_attention", C.c_int32, [_P(_CLinearAttn), _P(_CSeqView), _P(_CSeqView), _P(_CSeqView), _vp, _P(_CSeqView), _vp, _vp,
+                                          C.c_size_t, _vp])
+_sig("rslx_linear_attention_backward_workspace_bytes", C.c_size_t, [_P(_CLinearAttn)])
+_sig("rslx_linear_attention_backward", C.c_int32, [_P(_CLinearAttn), _P(_CSeqView), _P(_CSeqView), _P(_CSeqView), _vp, _P(_CSeqView), _vp,
+                                                   _P(_CSeqView), _P(_CSeqView), _P(_CSeqView), _vp, _vp, C.c_size_t, _vp])
+_sig("rslx_linear_attention_step", C.c_int32, [_P(_CLinearAttn), _P(_CSeqView), _P(_CSeqView), _P(_CSeqView), _vp, _vp, _vp, _P(_CSeqView),
+                                               _vp])
+_sig("rslx_layer_norm", C.c_int32, [C.c_int32, _vp, C.c_int64, C.c_int64, C.c_int32, _vp, _vp, C.c_float, _vp, C.c_int64, _vp, _vp, _vp])
+_sig("rslx_layer_norm_backward_workspace_bytes", C.c_size_t, [C.c_int64, C.c_int32])
+_sig("rslx_layer_norm_backward", C.c_int32, [C.c_int32, _vp, C.c_int64, _vp, C.c_int64, C.c_int64, C.c_int32, _vp, _vp, _vp, _vp, C.c_int64, _vp,
+                                             _vp, _vp, C.c_size_t, _vp])
 _sig("rslx_trace_begin", C.c_int32, [C.c_int32])
 _sig("rslx_trace_end", C.c_int32, [_P(_CTraceRecord), C.c_int32, _P(C.c_int32)])
 
@@ -533,6 +561,125 @@ def rslx_rnd(target, predictor, obs, N, D, subset_idx, n_subset, running, weight
     ct, cp = target.c, predictor.c
     _check(lib.rslx_rnd(_ref(ct), _ref(cp), _ptr(obs), N, D, _ptr(subset_idx), n_subset, _ptr(running), weight,
                         int(update_stats), _ptr(r_int_out), _ptr(rewards_inout), _ptr(ws), ws.numel(), _stream()), "rslx_rnd")
+
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+class LinearAttn:
+    """Sizes and constants of a linear-attention layer (struct rslx_linear_attn): T steps of N sequences, H heads, keys Dk and values
+    Dv wide, in `dtype`; log_decay [H] float32; dones uint8 [T, N] and lengths int32 [N] or None."""
+
+    def __init__(self, dtype, T, N, H, Dk, Dv, log_decay, scale=1.0, dones=None, lengths=None):
+        if dtype not in _DTYPES:
+            raise RslxError("LinearAttn: dtype %s is not one of float32, bfloat16, float16" % dtype)
+        for name, t, want, n in (("log_decay", log_decay, torch.float32, H), ("dones", dones, torch.uint8, T * N), ("lengths", lengths, torch.int32, N)):
+            if t is not None and (t.dtype != want or t.numel() != n):
+                raise RslxError("LinearAttn: %s has %d values of %s, %d of %s are needed" % (name, t.numel(), t.dtype, n, want))
+        self.dtype, self.T, self.N, self.H, self.Dk, self.Dv = dtype, int(T), int(N), int(H), int(Dk), int(Dv)
+        self.scale, self.log_decay, self.dones, self.lengths = float(scale), log_decay, dones, lengths
+        self.c = _CLinearAttn(_DTYPES[dtype], self.T, self.N, self.H, self.Dk, self.Dv, self.scale, _ptr(log_decay), _ptr(dones), _ptr(lengths))
+
+    def view(self, name, t, width):
+        """t [T, N, H, width] of any strides with its values side by side -> struct rslx_seq_view."""
+        if t.dtype != self.dtype or t.shape != (self.T, self.N, self.H, width):
+            raise RslxError("%s is %s %s, %s %s is needed" % (name, t.dtype, tuple(t.shape), self.dtype, (self.T, self.N, self.H, width)))
+        step, seq, head, one = t.stride()
+        if one != 1 and width > 1 and t.numel() > 0:
+            raise RslxError("%s: the values of a row must lie side by side" % name)
+        return _CSeqView(t.data_ptr(), step, seq, head)
+
+    def state(self, name, t):
+        """t [N, H, Dk, Dv] float32, contiguous, or None -> address."""
+        if t is None:
+            return None
+        if t.dtype != torch.float32 or t.numel() != self.N * self.H * self.Dk * self.Dv:
+            raise RslxError("%s has %d values of %s, %d of float32 are needed" % (name, t.numel(), t.dtype, self.N * self.H * self.Dk * self.Dv))
+        return _ptr(t)
+
+
+def rslx_linear_attention_workspace_bytes(la):
+    n = lib.rslx_linear_attention_workspace_bytes(C.byref(la.c))
+    if n == 0:
+        raise RslxError("rslx_linear_attention_workspace_bytes: %s" % lib.rslx_last_error().decode())
+    return n
+
+
+def rslx_linear_attention(la, q, k, v, s0, o, s_last, ws):
+    """q, k [T, N, H, Dk], v, o [T, N, H, Dv]; s0, s_last [N, H, Dk, Dv] float32 or None."""
+    _check(lib.rslx_linear_attention(la.c, la.view("q", q, la.Dk), la.view("k", k, la.Dk), la.view("v", v, la.Dv), la.state("s0", s0),
+                                     la.view("o", o, la.Dv), la.state("s_last", s_last), _ptr(ws), ws.numel() if ws is not None else 0,
+                                     _stream()), "rslx_linear_attention")
+
+
+def rslx_linear_attention_backward_workspace_bytes(la):
+    n = lib.rslx_linear_attention_backward_workspace_bytes(C.byref(la.c))
+    if n == 0:
+        raise RslxError("rslx_linear_attention_backward_workspace_bytes: %s" % lib.rslx_last_error().decode())
+    return n
+
+
+def rslx_linear_attention_backward(la, q, k, v, s0, do, ds_last, dq, dk, dv, ds0, ws):
+    """Gradients of rslx_linear_attention from do [T, N, H, Dv] and ds_last [N, H, Dk, Dv] (or None)."""
+    _check(lib.rslx_linear_attention_backward(la.c, la.view("q", q, la.Dk), la.view("k", k, la.Dk), la.view("v", v, la.Dv),
+                                              la.state("s0", s0), la.view("do", do, la.Dv), la.state("ds_last", ds_last),
+                                              la.view("dq", dq, la.Dk), la.view("dk", dk, la.Dk), la.view("dv", dv, la.Dv),
+                                              la.state("ds0", ds0), _ptr(ws), ws.numel() if ws is not None else 0, _stream()),
+           "rslx_linear_attention_backward")
+
+
+def rslx_linear_attention_step(la, q, k, v, reset, s_in, s_out, o):
+    """One step (la.T == 1): q, k [1, N, H, Dk], v, o [1, N, H, Dv]; reset uint8 of N values or None; s_in (or None), s_out [N, H, Dk, Dv]."""
+    if reset is not None and (reset.dtype != torch.uint8 or reset.numel() != la.N):
+        raise RslxError("reset has %d values of %s, %d of uint8 are needed" % (reset.numel(), reset.dtype, la.N))
+    _check(lib.rslx_linear_attention_step(la.c, la.view("q", q, la.Dk), la.view("k", k, la.Dk), la.view("v", v, la.Dv), _ptr(reset),
+                                          la.state("s_in", s_in), la.state("s_out", s_out), la.view("o", o, la.Dv), _stream()),
+           "rslx_linear_attention_step")
+
+
+def _rows(name, t, like=None):
+    """A matrix [rows, cols] whose rows may lie apart -> (address, distance)."""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or t.dtype not in _DTYPES or (like is not None and (t.shape != like.shape or t.dtype != like.dtype)):
+        raise RslxError("%s is %s %s, %s is needed" % (name, t.dtype, tuple(t.shape), "a matrix of float32, bfloat16 or float16" if like is None
+                                                       else "%s %s" % (like.dtype, tuple(like.shape))))
+    ld, one = t.stride()
+    if one != 1 and t.shape[1] > 1 and t.numel() > 0:
+        raise RslxError("%s: the values of a row must lie side by side" % name)
+    return t.data_ptr(), ld
+
+
+def _f32(name, t, n):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != n:
+        raise RslxError("%s has %d values of %s, %d of float32 are needed" % (name, t.numel(), t.dtype, n))
+    return _ptr(t)
+
+
+def rslx_layer_norm(x, weight, bias, eps, y, mean, rstd):
+    """x, y [rows, cols]; weight, bias [cols] and mean, rstd [rows] float32 or None."""
+    rows, cols = x.shape
+    (px, ldx), (py, ldy) = _rows("x", x), _rows("y", y, x)
+    _check(lib.rslx_layer_norm(_DTYPES[x.dtype], px, ldx, rows, cols, _f32("weight", weight, cols), _f32("bias", bias, cols), eps, py, ldy,
+                               _f32("mean", mean, rows), _f32("rstd", rstd, rows), _stream()), "rslx_layer_norm")
+
+
+def rslx_layer_norm_backward_workspace_bytes(rows, cols):
+    n = lib.rslx_layer_norm_backward_workspace_bytes(rows, cols)
+    if n == 0:
+        raise RslxError("rslx_layer_norm_backward_workspace_bytes: %s" % lib.rslx_last_error().decode())
+    return n
+
+
+def rslx_layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, ws):
+    """dy, x, dx [rows, cols]; mean, rstd [rows] as rslx_layer_norm leaves them; dx, dweight, dbias or None."""
+    rows, cols = x.shape
+    (px, ldx), (pd, lddy), (pg, lddx) = _rows("x", x), _rows("dy", dy, x), _rows("dx", dx, x)
+    _check(lib.rslx_layer_norm_backward(_DTYPES[x.dtype], pd, lddy, px, ldx, rows, cols, _f32("weight", weight, cols), _f32("mean", mean, rows),
+                                        _f32("rstd", rstd, rows), pg, lddx, _f32("dweight", dweight, cols), _f32("dbias", dbias, cols), _ptr(ws),
+                                        ws.numel() if ws is not None else 0, _stream()), "rslx_layer_norm_backward")
 
 
 def rslx_trace_begin(max_records):

@@ -1,0 +1,28 @@
+// Activations of the sequence operators (linear attention, layer norm) come in three types; arithmetic is fp32.
+#pragma once
+
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace rslx {
+
+struct bf16_t { uint16_t bits; };
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(bf16_t x) { return __uint_as_float((uint32_t)x.bits << 16); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+
+// Rounded to nearest, ties to even; a NaN stays one.
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ bf16_t from_float<bf16_t>(float x) {
+  const __bf16 b = (__bf16)x;
+  return {__builtin_bit_cast(uint16_t, b)};
+}
+template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half(x); }
+
+// N consecutive values, moved in accesses of up to 16 bytes.
+template <typename T, int N> struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Pack { T v[N]; };
+
+}  // namespace rslx
