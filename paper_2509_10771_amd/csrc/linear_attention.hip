@@ -17,6 +17,8 @@
 #include "sequence.h"
 #include "typed.h"
 
+#include <type_traits>
+
 namespace rslx {
 
 namespace {
@@ -38,60 +40,118 @@ template <typename T, int N> struct Frag {
   }
 };
 
-template <int N> struct alignas(N * 4) Words { uint32_t v[N]; };
+// Memory is read through buffer descriptors: what lies past a row's end, or in a row that does not exist, is asked for at an offset
+// beyond the descriptor's range and comes back as zero, without a branch and without a select; stores there are dropped.
+// PIECE: bytes of one access (16; 4 and 2 where widths, strides or addresses are no multiples of 16), 0: rows too far apart for
+// 32-bit offsets, value by value through 64-bit addresses.
+constexpr uint32_t NOWHERE = 0x80000000u;
+constexpr int64_t MAX_OFFSET = 0x7fff0000;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __amdgpu_buffer_rsrc_t Descriptor;
 
-// Values e0 .. e0 + N - 1 of a row of `width`; zero past the row's end and where the row does not exist (`row` then points at one that does).
-// whole: all of them exist.
-template <typename T, int N, bool VEC>
-__device__ __forceinline__ void load_frag(Frag<T, N>& f, const T* row, int e0, int width, bool exists, bool whole) {
-  constexpr int WORDS = Frag<T, N>::WORDS;
-  if constexpr (VEC) {
-    constexpr int PW = WORDS < 4 ? WORDS : 4, PE = PW * 4 / (int)sizeof(T);
+__device__ __forceinline__ Descriptor descriptor(const void* base, bool exists = true, int bytes = 0x7fffffff) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, exists ? bytes : 0, 0x00020000);
+}
+
+// The 16 rows of a chunk, slot by slot; positions go up or down in memory.
+struct Rows {
+  const char* low;               // of the row at the lowest address
+  int64_t step;                  // bytes from a position to the next one, either sign
+  __device__ __forceinline__ void move(int positions) { low += positions * step; }
+  __device__ __forceinline__ int order(int slot) const { return step < 0 ? CHUNK - 1 - slot : slot; }
+  __device__ __forceinline__ uint32_t at(int slot) const { return (uint32_t)order(slot) * (uint32_t)(step < 0 ? -step : step); }
+  __device__ __forceinline__ const char* address(int slot) const { return low + (int64_t)order(slot) * (step < 0 ? -step : step); }
+};
+template <typename T>
+__device__ __forceinline__ Rows rows_at(const T* first, int64_t step, int position) {
+  const int64_t bytes = step * (int64_t)sizeof(T);
+  return {reinterpret_cast<const char*>(first) + (position + (step < 0 ? CHUNK - 1 : 0)) * bytes, bytes};
+}
+
+// A value that the compiler does not know: what is made of it is neither kept from elsewhere nor made ahead of time (in registers that the
+// products need).
+__device__ __forceinline__ int opaque(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// N values of a row from offset `at` on (or NOWHERE).  `there`: how many of them the row has; WHOLE: all.
+template <typename T, int N, int PIECE, bool WHOLE>
+__device__ __forceinline__ void load_frag(Frag<T, N>& f, Descriptor d, uint32_t at, int there) {
+  constexpr int WORDS = Frag<T, N>::WORDS, PB = PIECE < WORDS * 4 ? PIECE : WORDS * 4, PE = PB / (int)sizeof(T);
 #pragma unroll
-    for (int k = 0; k < WORDS / PW; ++k) {
-      const int e = e0 + k * PE;
-      Words<PW> x;
-      if (whole) {
-        x = *reinterpret_cast<const Words<PW>*>(row + e);
-      } else {
-        const bool in = exists && e < width;
-        x = *reinterpret_cast<const Words<PW>*>(row + (in ? e : 0));
+  for (int k = 0; k < N / PE; ++k) {
+    const int o = (int)(WHOLE || k * PE < there ? at + (uint32_t)(k * PB) : NOWHERE);
+    if constexpr (PB == 16) {
+      const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(d, o, 0, 0);
 #pragma unroll
-        for (int i = 0; i < PW; ++i) x.v[i] = in ? x.v[i] : 0u;
-      }
-#pragma unroll
-      for (int i = 0; i < PW; ++i) f.w[k * PW + i] = x.v[i];
+      for (int i = 0; i < 4; ++i) f.w[4 * k + i] = x[i];
+    } else if constexpr (PB == 8) {
+      const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(d, o, 0, 0);
+      f.w[2 * k] = x[0];
+      f.w[2 * k + 1] = x[1];
+    } else if constexpr (PB == 4) {
+      f.w[k] = __builtin_amdgcn_raw_buffer_load_b32(d, o, 0, 0);
+    } else {
+      const uint32_t x = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(d, o, 0, 0);
+      f.w[k / 2] = k % 2 ? f.w[k / 2] | x << 16 : x;
     }
-  } else {
+  }
+}
+template <typename T, int N>
+__device__ __forceinline__ void load_far(Frag<T, N>& f, const char* row, bool exists, int e0, int width) {
 #pragma unroll
-    for (int k = 0; k < WORDS; ++k) {
-      if constexpr (sizeof(T) == 4) {
-        const bool in = exists && e0 + k < width;
-        const uint32_t x = reinterpret_cast<const uint32_t*>(row)[in ? e0 + k : 0];
-        f.w[k] = in ? x : 0u;
-      } else {
-        const uint16_t* r = reinterpret_cast<const uint16_t*>(row);
-        const int e = e0 + 2 * k;
-        const bool in0 = exists && e < width, in1 = exists && e + 1 < width;
-        const uint32_t x0 = r[in0 ? e : 0], x1 = r[in1 ? e + 1 : 0];
-        f.w[k] = (in0 ? x0 : 0u) | (in1 ? x1 << 16 : 0u);
-      }
+  for (int k = 0; k < Frag<T, N>::WORDS; ++k) {
+    f.w[k] = 0;
+#pragma unroll
+    for (int h = 0; h < 4 / (int)sizeof(T); ++h) {
+      const int e = e0 + k * (4 / (int)sizeof(T)) + h;
+      if (!exists || e >= width) continue;
+      if constexpr (sizeof(T) == 4) f.w[k] = reinterpret_cast<const uint32_t*>(row)[e];
+      else f.w[k] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[e] << (16 * h);
     }
   }
 }
 
-template <typename T, int N, bool VEC>
-__device__ __forceinline__ void store_row(T* row, int e0, int width, const float (&v)[N]) {
-  if constexpr (VEC) {
-    if (e0 >= width) return;
-    Pack<T, N> p;
+template <typename T, int N, int PIECE, bool WHOLE>
+__device__ __forceinline__ void store_frag(Descriptor d, uint32_t at, int there, const float (&v)[N]) {
+  constexpr int PB = PIECE < N * (int)sizeof(T) ? PIECE : N * (int)sizeof(T), PE = PB / (int)sizeof(T);
 #pragma unroll
-    for (int i = 0; i < N; ++i) p.v[i] = from_float<T>(v[i]);
-    *reinterpret_cast<Pack<T, N>*>(row + e0) = p;
-  } else {
+  for (int k = 0; k < N / PE; ++k) {
+    const int o = (int)(WHOLE || k * PE < there ? at + (uint32_t)(k * PB) : NOWHERE);
+    Pack<T, PE> p;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (e0 + i < width) row[e0 + i] = from_float<T>(v[i]);
+    for (int i = 0; i < PE; ++i) p.v[i] = from_float<T>(v[k * PE + i]);
+    if constexpr (PB == 16) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, p), d, o, 0, 0);
+    else if constexpr (PB == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, p), d, o, 0, 0);
+    else if constexpr (PB == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, p), d, o, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, p), d, o, 0, 0);
+  }
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_far(const char* row, bool exists, int e0, int width, const float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (exists && e0 + i < width) reinterpret_cast<T*>(const_cast<char*>(row))[e0 + i] = from_float<T>(v[i]);
+}
+
+// N values of a state, BYTES at a time.
+template <int N, int BYTES>
+__device__ __forceinline__ void load_state(float (&v)[N], Descriptor d, const uint32_t (&at)[N]) {
+#pragma unroll
+  for (int k = 0; k < N; k += BYTES / 4) {
+    if constexpr (BYTES == 16) {
+      const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(d, (int)at[k], 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[k + i] = __uint_as_float(x[i]);
+    } else if constexpr (BYTES == 8) {
+      const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(d, (int)at[k], 0, 0);
+      v[k] = __uint_as_float(x[0]);
+      v[k + 1] = __uint_as_float(x[1]);
+    } else {
+      v[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(d, (int)at[k], 0, 0));
+    }
   }
 }
 
@@ -114,13 +174,7 @@ __device__ __forceinline__ int sequence_length(const WalkArgs& w, int n) {
   return w.lengths ? min(max(w.lengths[n], 0), w.T) : w.T;
 }
 
-// Whether an episode ends between position p and the next one.
-__device__ __forceinline__ bool cut_behind(const WalkArgs& w, bool reversed, int n, int len, int p) {
-  const int t = reversed ? len - 2 - p : p;
-  return t >= 0 && p < len && w.dones[(int64_t)t * w.N + n] != 0;
-}
-
-template <typename T, int DKT, int DVT, bool VEC, bool STATES>
+template <typename T, int DKT, int DVT, int PIECE, bool WHOLE, bool STATES>
 __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_kernel(WalkArgs w, int tiles) {
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   int item = uniform((int)blockIdx.x * WALK_WAVES + (int)(threadIdx.x >> 6));
@@ -137,29 +191,63 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
   const int lead = rev ? 0 : 1;
   const int len = uniform(sequence_length(w, n));
   const int p0 = min(piece * w.seg_len, len), p1 = min(p0 + w.seg_len, len);
+  // The first chunk is the one that may be short: it fills the last slots, so that the weights towards the state behind a chunk are
+  // the same for every chunk.
+  const int chunks = (p1 - p0 + CHUNK - 1) / CHUNK;
+  int skip = chunks * CHUNK - (p1 - p0);
+  int at = p0 - skip;                     // position of the chunk's slot 0
   const int64_t first = rev ? len - 1 : 0, dir = rev ? -1 : 1;
-  auto base = [&](const WalkMatrix& m) { return static_cast<const T*>(m.p) + n * m.seq + h * m.head + first * m.step; };
-  const T* A = STATES ? nullptr : base(job.a);
-  const T* B = base(job.b);
-  const T* C = base(job.c);
-  T* O = STATES ? nullptr : const_cast<T*>(base(job.o));
-  const int64_t sa = dir * job.a.step, sb = dir * job.b.step, sc = dir * job.c.step, so = dir * job.o.step;
-  const bool whole_d = D == 16 * DKT, whole_e = e_tile + 16 * DVT <= E;
-
-  // weights that every whole chunk shares
-  const double l2 = log2_decay(w.log_decay[h]);
-  float wp[4], wq[4], wk[4];
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int i = 4 * g + r;
-    wp[r] = c >= i ? w.scale * decay_pow(l2, c - i) : 0.f;
-    wq[r] = (rev ? 1.f : w.scale) * decay_pow(l2, i + lead);
-    wk[r] = (rev ? w.scale : 1.f) * decay_pow(l2, CHUNK - lead - i);
+  auto rows = [&](const WalkMatrix& m) {
+    return rows_at(static_cast<const T*>(m.p) + n * m.seq + h * m.head + first * m.step, dir * m.step, at);
+  };
+  Rows A{}, O{}, B = rows(job.b), C = rows(job.c);
+  if constexpr (!STATES) {
+    A = rows(job.a);
+    O = rows(job.o);
   }
-  // The state is multiplied by the same number once a chunk: its rounding would add up over a long sequence (3e-8 a chunk), so it
-  // is kept in two parts.
-  const double chunk_decay = exp2(l2 * CHUNK);
-  const float f_hi = (float)chunk_decay, f_lo = f_hi < 1e30f ? (float)(chunk_decay - (double)f_hi) : 0.f;
+
+  // The operands of a chunk; each set is asked for again, for the next chunk, as soon as this one's products have read it: by the time it is
+  // needed the other half of a chunk's products has gone by.
+  Frag<T, 4 * DKT> fa, fb;
+  Frag<T, DKT> fk[4];
+  Frag<T, DVT> fv[4];
+  uint32_t end = 0;
+  constexpr int SIZE = (int)sizeof(T);
+  const uint32_t at_a = A.at(c) + 4 * DKT * g * SIZE, at_b = B.at(c) + 4 * DKT * g * SIZE, at_k = B.at(4 * g) + DKT * c * SIZE,
+                 at_v = C.at(4 * g) + e_lane * SIZE, at_o = O.at(4 * g) + e_lane * SIZE;
+  // (at the start: slots below skip do not exist; afterwards all do)
+  auto load_row = [&](auto start, auto& f, const Rows& m, uint32_t from, bool exists) {
+    constexpr int N = 4 * DKT;
+    const bool in = !start || c >= skip;
+    if constexpr (PIECE != 0) load_frag<T, N, PIECE, WHOLE>(f, descriptor(m.low, exists), in ? (uint32_t)opaque((int)from) : NOWHERE, opaque(D - 4 * DKT * g));
+    else load_far<T, N>(f, m.address(c), exists && in, 4 * DKT * g, D);
+  };
+  auto load_update = [&](auto start, bool exists) {
+    if (w.dones && exists) {
+      const int t = rev ? len - 2 - at - lane : at + lane;
+      end = w.dones[(int64_t)min(max(t, 0), len - 1) * w.N + n];
+    }
+    const uint32_t from_k = opaque((int)at_k), from_v = opaque((int)at_v);
+    const int there_k = opaque(D - DKT * c), there_v = opaque(E - e_lane);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const bool in = !start || 4 * g + s >= skip;
+      if constexpr (PIECE != 0) {
+        load_frag<T, DVT, PIECE, WHOLE>(fv[s], descriptor(C.low, exists), in ? from_v + (uint32_t)(s * (int)C.step) : NOWHERE, there_v);
+        load_frag<T, DKT, PIECE, WHOLE>(fk[s], descriptor(B.low, exists), in ? from_k + (uint32_t)(s * (int)B.step) : NOWHERE, there_k);
+      } else {
+        load_far<T, DVT>(fv[s], C.address(4 * g + s), exists && in, e_lane, E);
+        load_far<T, DKT>(fk[s], B.address(4 * g + s), exists && in, DKT * c, D);
+      }
+    }
+  };
+  constexpr auto START = std::true_type{};
+  constexpr auto NEXT = std::false_type{};
+  if constexpr (!STATES) {
+    load_row(START, fb, B, at_b, chunks > 0);
+    load_row(START, fa, A, at_a, chunks > 0);
+  }
+  load_update(START, chunks > 0);
 
   f32x4 S[DKT][DVT];
 #pragma unroll
@@ -169,80 +257,76 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
   bool live = false;                      // the state may be other than zero
   if (!STATES && job.s_in != nullptr && !(w.segments == 1 && rev && len > 0 && w.dones && w.dones[(int64_t)(len - 1) * w.N + n])) {
     live = true;
-    const float* s = job.s_in + (((int64_t)n * w.H + h) * w.segments + piece) * D * E;
+    const int g = opaque(lane >> 4), c = opaque(lane & 15), e_lane = e_tile + DVT * c;
+    const Descriptor d = descriptor(job.s_in + (((int64_t)n * w.H + h) * w.segments + piece) * D * E, true, D * E * 4);
+    if (job.in_col == 1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int d0 = DKT * (4 * g + i);
-      if (job.in_col == 1 && E % DVT == 0) {
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int a = 0; a < DKT; ++a)
-          if (d0 + a < D && e_lane < E) {
-            const Pack<float, DVT> x = *reinterpret_cast<const Pack<float, DVT>*>(s + (int64_t)(d0 + a) * job.in_row + e_lane);
+        for (int a = 0; a < DKT; ++a) {
+          float v[DVT];
+          uint32_t o[DVT];
 #pragma unroll
-            for (int t = 0; t < DVT; ++t) S[a][t][i] = x.v[t];
+          for (int t = 0; t < DVT; ++t) o[t] = e_lane + t < E ? (uint32_t)((DKT * (4 * g + i) + a) * E + e_lane + t) * 4 : NOWHERE;
+          if (E % DVT == 0) load_state<DVT, DVT * 4>(v, d, o);
+          else load_state<DVT, 4>(v, d, o);
+#pragma unroll
+          for (int t = 0; t < DVT; ++t) S[a][t][i] = v[t];
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int t = 0; t < DVT; ++t) {
+          float v[DKT];
+          uint32_t o[DKT];
+#pragma unroll
+          for (int a = 0; a < DKT; ++a) {
+            const int x = DKT * (4 * g + i) + a;
+            o[a] = x < D ? (uint32_t)((e_lane + t) * D + x) * 4 : NOWHERE;
           }
-      } else if (job.in_row == 1 && D % DKT == 0) {
+          if (D % DKT == 0) load_state<DKT, (DKT < 4 ? DKT : 4) * 4>(v, d, o);
+          else load_state<DKT, 4>(v, d, o);
 #pragma unroll
-        for (int t = 0; t < DVT; ++t)
-          if (d0 < D && e_lane + t < E) {
-            const Pack<float, DKT> x = *reinterpret_cast<const Pack<float, DKT>*>(s + (int64_t)(e_lane + t) * job.in_col + d0);
-#pragma unroll
-            for (int a = 0; a < DKT; ++a) S[a][t][i] = x.v[a];
-          }
-      } else {
-#pragma unroll
-        for (int a = 0; a < DKT; ++a)
-#pragma unroll
-          for (int t = 0; t < DVT; ++t)
-            if (d0 + a < D && e_lane + t < E) S[a][t][i] = s[(int64_t)(d0 + a) * job.in_row + (int64_t)(e_lane + t) * job.in_col];
-      }
+          for (int a = 0; a < DKT; ++a) S[a][t][i] = v[a];
+        }
     }
   }
 
+  // weights inside a chunk, of the state before it, and towards the state behind it
+  const double l2 = log2_decay(w.log_decay[h]);
+  const float b_scale = rev ? w.scale : 1.f, o_scale = rev ? 1.f : w.scale;
+  float wp[4], wq[4], wk[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int i = 4 * g + r;
+    wp[r] = c >= i ? w.scale * decay_pow(l2, c - i) : 0.f;
+    wq[r] = o_scale * decay_pow(l2, max(i - skip, 0) + lead);
+    wk[r] = b_scale * decay_pow(l2, CHUNK - lead - i);
+  }
+  // The state is multiplied by the same number once a chunk, and its rounding would add up over a long sequence (3e-8 a chunk): every
+  // eighth chunk takes off what eight of them left.
+  constexpr int CORRECT = 8;
+  const double chunk_decay = exp2(l2 * CHUNK);
+  float keep = decay_pow(l2, CHUNK - skip);
+  const float keep_whole = (float)chunk_decay;
+  const float off = keep_whole > 0.f && keep_whole < 1e30f ? (float)(CORRECT * (chunk_decay / (double)keep_whole - 1.0)) : 0.f;
+
   const bool wants_state = STATES || (job.s_out != nullptr && piece == w.segments - 1);
   bool any_cut = false;
-  int careful = p0;                       // positions before this one are taken one at a time
-  for (int p = p0; p < p1;) {
-    const int m = p < careful ? 1 : min(CHUNK, p1 - p);
-    const bool whole_m = m == CHUNK;
-    Frag<T, 4 * DKT> fa, fb;
-    Frag<T, DKT> fk[4];
-    Frag<T, DVT> fv[4];
-    const int row_c = min(c, m - 1);
+  int careful = p1;                       // positions from here on are taken one by one
+  for (int q = 0; q < chunks; ++q) {
+    const bool more = q + 1 < chunks, update = wants_state || more;
+    const int skip_now = skip;
+    skip = 0;                             // of the next chunk
+    f32x4 o[DVT];
+    f32x4 P = {0.f, 0.f, 0.f, 0.f};
     if constexpr (!STATES) {
-      load_frag<T, 4 * DKT, VEC>(fb, B + (p + row_c) * sb, 4 * DKT * g, D, c < m, whole_m && whole_d);
-      load_frag<T, 4 * DKT, VEC>(fa, A + (p + row_c) * sa, 4 * DKT * g, D, c < m, whole_m && whole_d);
-    }
-    const bool update = wants_state || p + m < p1;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int j = 4 * g + s, row = min(j, m - 1);
-      load_frag<T, DVT, VEC>(fv[s], C + (p + row) * sc, e_lane, E, j < m, whole_m && whole_e);
-      load_frag<T, DKT, VEC>(fk[s], B + (p + row) * sb, DKT * c, D, j < m, whole_m && whole_d);
-    }
-    // bit i: an episode ends between positions p + i and p + i + 1
-    uint32_t cut = 0;
-    if (w.dones) cut = (uint32_t)__ballot(lane < m && cut_behind(w, rev, n, len, p + lane)) & 0xffffu;
-
-    // A position's weight for an earlier or later one that it has nothing to do with is zero, but zero times infinity is not: where a
-    // chunk's C holds anything that is not finite its positions go one at a time, as the recurrence does.
-    if (m > 1) {
-      float bad = 0.f;
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-#pragma unroll
-        for (int t = 0; t < DVT; ++t) bad = fmaf(fv[s].get(t), 0.f, bad);
-      if (__any(bad != 0.f)) {
-        careful = p + m;
-        continue;
-      }
-    }
-
-    if constexpr (!STATES) {
-      f32x4 P = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int x = 0; x < 4 * DKT; ++x) P = __builtin_amdgcn_mfma_f32_16x16x4f32(fb.get(x), fa.get(x), P, 0, 0, 0);
-      f32x4 o[DVT];
+      __builtin_amdgcn_sched_barrier(0);      // the next chunk's operands take the registers of this one's
+      B.move(CHUNK);
+      load_row(NEXT, fb, B, at_b, more);
 #pragma unroll
       for (int t = 0; t < DVT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (live) {
@@ -253,91 +337,185 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
 #pragma unroll
             for (int t = 0; t < DVT; ++t) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa.get(DKT * s + a), S[a][t][s], o[t], 0, 0, 0);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const bool reached = (cut & ((1u << (4 * g + r)) - 1u)) == 0;
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int t = 0; t < DVT; ++t) o[t][r] = reached ? o[t][r] * wq[r] : 0.f;
+          for (int t = 0; t < DVT; ++t) o[t][r] *= wq[r];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      A.move(CHUNK);
+      load_row(NEXT, fa, A, at_a, more);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) P[r] = c >= 4 * g + r ? P[r] * wp[r] : 0.f;
+    } else {
+      B.move(CHUNK);
+    }
+    // bit i: an episode ends between slots i and i + 1
+    uint32_t cut = 0;
+    if (w.dones) cut = (uint32_t)__ballot(lane >= skip_now && end != 0 && !(rev && at + lane >= len - 1)) & 0xffffu;
+    if constexpr (!STATES) {
+      if (cut) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int i = 4 * g + r;
+          P[r] = ((cut >> i) & ((1u << ((c - i) & 31)) - 1u)) == 0 ? P[r] : 0.f;
+#pragma unroll
+          for (int t = 0; t < DVT; ++t) o[t][r] = (cut & ((1u << i) - 1u)) == 0 ? o[t][r] : 0.f;
         }
       }
+    }
+
+    // A position's weight for an earlier or later one that it has nothing to do with is zero, but zero times infinity is not: from a chunk
+    // on whose C holds anything that is not finite, positions are taken one by one, as the recurrence has them.
+    float bad = 0.f;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int j = 4 * g + r;
-        const bool same = c >= j && ((cut >> j) & ((1u << ((c - j) & 31)) - 1u)) == 0;
-        P[r] = same ? P[r] * wp[r] : 0.f;
-      }
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int t = 0; t < DVT; ++t) bad = fmaf(fv[s].get(t), 0.f, bad);
+    if (__any(bad != 0.f)) {
+      careful = at + skip_now;
+      break;
+    }
+
+    if constexpr (!STATES) {
 #pragma unroll
       for (int s = 0; s < 4; ++s)
 #pragma unroll
         for (int t = 0; t < DVT; ++t) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(P[s], fv[s].get(t), o[t], 0, 0, 0);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = 4 * g + r;
-        float v[DVT];
-#pragma unroll
-        for (int t = 0; t < DVT; ++t) v[t] = o[t][r];
-        if (i < m) store_row<T, DVT, VEC>(O + (p + i) * so, e_lane, E, v);
-      }
     }
-
     if (update) {
-      float hi = f_hi, lo = f_lo, wj[4];
-#pragma unroll
-      for (int s = 0; s < 4; ++s) wj[s] = wk[s];
-      if (!whole_m) {
-        hi = decay_pow(l2, m);
-        lo = 0.f;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) wj[s] = 4 * g + s < m ? (rev ? w.scale : 1.f) * decay_pow(l2, m - lead - 4 * g - s) : 0.f;
-      }
       if (live) {
+        const float f = cut ? 0.f : keep;
 #pragma unroll
         for (int a = 0; a < DKT; ++a)
 #pragma unroll
           for (int t = 0; t < DVT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[a][t][r] = cut ? 0.f : fmaf(S[a][t][r], lo, S[a][t][r] * hi);
+            for (int r = 0; r < 4; ++r) S[a][t][r] *= f;
+        if (cut) {                       // (a state that is not finite ends with its episode too)
+#pragma unroll
+          for (int a = 0; a < DKT; ++a)
+#pragma unroll
+            for (int t = 0; t < DVT; ++t) S[a][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        } else if (q % CORRECT == CORRECT - 1) {
+#pragma unroll
+          for (int a = 0; a < DKT; ++a)
+#pragma unroll
+            for (int t = 0; t < DVT; ++t)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) S[a][t][r] = fmaf(S[a][t][r], off, S[a][t][r]);
+        }
       }
+      live = true;
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const bool stays = (cut >> (4 * g + s)) == 0;
 #pragma unroll
         for (int a = 0; a < DKT; ++a) {
-          const float k = stays ? fk[s].get(a) * wj[s] : 0.f;
+          const float k = stays ? fk[s].get(a) * wk[s] : 0.f;
 #pragma unroll
           for (int t = 0; t < DVT; ++t) S[a][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k, fv[s].get(t), S[a][t], 0, 0, 0);
         }
       }
-      live = true;
     }
+    __builtin_amdgcn_sched_barrier(0);
+    at += CHUNK;
+    C.move(CHUNK);
+    load_update(NEXT, more);
+    if constexpr (!STATES) {
+      const uint32_t from_o = opaque((int)at_o);
+      const int there_o = opaque(E - e_lane);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float v[DVT];
+#pragma unroll
+        for (int t = 0; t < DVT; ++t) v[t] = o[t][r];
+        if constexpr (PIECE != 0) store_frag<T, DVT, PIECE, WHOLE>(descriptor(O.low), 4 * g + r >= skip_now ? from_o + (uint32_t)(r * (int)O.step) : NOWHERE, there_o, v);
+        else store_far<T, DVT>(O.address(4 * g + r), 4 * g + r >= skip_now, e_lane, E, v);
+      }
+    }
+    if constexpr (!STATES) O.move(CHUNK);
     if constexpr (STATES) any_cut |= cut != 0;
-    p += m;
+    if (q == 0) {
+      keep = keep_whole;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) wq[r] = o_scale * decay_pow(l2, 4 * g + r + lead);
+    }
+  }
+
+  if (careful < p1) {
+    const int g = opaque(lane >> 4), c = opaque(lane & 15), e_lane = e_tile + DVT * c;
+    const float l1 = decay_pow(l2, 1);
+    at = careful;
+    Rows a{}, b = rows(job.b), z = rows(job.c), out{};
+    if constexpr (!STATES) {
+      a = rows(job.a);
+      out = rows(job.o);
+    }
+    for (; at < p1; ++at) {
+      const int t = rev ? len - 2 - at : at;
+      const bool cut = w.dones && t >= 0 && w.dones[(int64_t)t * w.N + n] != 0;
+      Frag<T, 4 * DKT> xa, xb;
+      Frag<T, DVT> xc;
+      load_far<T, 4 * DKT>(xb, b.address(0), true, 4 * DKT * g, D);
+      load_far<T, DVT>(xc, z.address(0), true, e_lane, E);
+      if constexpr (!STATES) load_far<T, 4 * DKT>(xa, a.address(0), true, 4 * DKT * g, D);
+      float sum[DVT] = {};
+#pragma unroll
+      for (int x = 0; x < DKT; ++x)
+#pragma unroll
+        for (int t = 0; t < DVT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float v = fmaf(xb.get(DKT * r + x) * b_scale, xc.get(t), rev ? S[x][t][r] : S[x][t][r] * l1);
+            if constexpr (!STATES) sum[t] = fmaf(xa.get(DKT * r + x), v, sum[t]);
+            if (rev) v *= l1;
+            S[x][t][r] = cut ? 0.f : v;
+          }
+      if constexpr (!STATES) {
+#pragma unroll
+        for (int t = 0; t < DVT; ++t) {
+          sum[t] += __shfl_xor(sum[t], 16, 64);
+          sum[t] = (sum[t] + __shfl_xor(sum[t], 32, 64)) * o_scale;
+        }
+        store_far<T, DVT>(out.address(0), g == 0, e_lane, E, sum);
+        a.move(1);
+        out.move(1);
+      }
+      b.move(1);
+      z.move(1);
+      if constexpr (STATES) any_cut |= cut;
+    }
   }
 
   if (wants_state) {
-    float* s = job.s_out + (((int64_t)n * w.H + h) * (STATES ? w.segments : 1) + (STATES ? piece + 1 : 0)) * D * E;
+    const int g = opaque(lane >> 4), c = opaque(lane & 15), e_lane = e_tile + DVT * c;
+    const Descriptor d = descriptor(job.s_out + (((int64_t)n * w.H + h) * (STATES ? w.segments : 1) + (STATES ? piece + 1 : 0)) * D * E, true, D * E * 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int a = 0; a < DKT; ++a) {
-        const int d = DKT * (4 * g + i) + a;
         float v[DVT];
 #pragma unroll
         for (int t = 0; t < DVT; ++t) v[t] = S[a][t][i];
-        if (d >= D) continue;
-        if (E % DVT == 0)
-          store_row<float, DVT, true>(s + (int64_t)d * E, e_lane, E, v);
-        else
-          store_row<float, DVT, false>(s + (int64_t)d * E, e_lane, E, v);
+        const uint32_t o = (uint32_t)((DKT * (4 * g + i) + a) * E + e_lane) * 4;
+        if (E % DVT == 0) store_frag<float, DVT, 16, false>(d, o, E - e_lane, v);
+        else store_frag<float, DVT, 4, false>(d, o, E - e_lane, v);
       }
   }
   if constexpr (STATES) {
     if (w.cuts && h == 0 && tile == 0 && lane == 0) w.cuts[((int64_t)ji * w.N + n) * w.segments + piece] = any_cut ? 1 : 0;
   } else {
     // steps that do not exist: zero
-    T* Z = static_cast<T*>(const_cast<void*>(job.o.p)) + n * job.o.seq + h * job.o.head;
     const float zero[DVT] = {};
-    const int t1 = piece == w.segments - 1 ? w.T : min((piece + 1) * w.seg_len, w.T);
-    for (int t = max(len, piece * w.seg_len) + g; t < t1; t += 4) store_row<T, DVT, VEC>(Z + (int64_t)t * job.o.step, e_lane, E, zero);
+    const int t0 = max(len, piece * w.seg_len), t1 = piece == w.segments - 1 ? w.T : min((piece + 1) * w.seg_len, w.T);
+    Rows Z = rows_at(static_cast<const T*>(job.o.p) + n * job.o.seq + h * job.o.head, job.o.step, t0);
+    for (int t = t0; t < t1; t += CHUNK, Z.move(CHUNK))
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const bool exists = 4 * g + r < t1 - t;
+        if constexpr (PIECE != 0) store_frag<T, DVT, PIECE, WHOLE>(descriptor(Z.low), exists ? Z.at(4 * g + r) + e_lane * SIZE : NOWHERE, E - e_lane, zero);
+        else store_far<T, DVT>(Z.address(4 * g + r), exists, e_lane, E, zero);
+      }
   }
 }
 
@@ -451,45 +629,60 @@ __global__ __launch_bounds__(256) void attention_step_kernel(StepArgs a, int LR)
 struct WalkClass { int dkt, dvt; };
 WalkClass walk_class(int D, int E) { return {D <= 32 ? 2 : D <= 64 ? 4 : 8, E <= 32 ? 2 : 4}; }
 
-template <typename T, int DKT, int DVT>
-void run_walk(const WalkArgs& w, bool vec, int tiles, unsigned blocks, hipStream_t s) {
+template <typename T, int DKT, int DVT, int PIECE, bool WHOLE>
+void run_walk(const WalkArgs& w, int tiles, unsigned blocks, hipStream_t s) {
   const dim3 grid(blocks), threads(64 * WALK_WAVES);
-  if (w.states_only) {
-    if (vec)
-      hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, true, true>), grid, threads, 0, s, w, tiles);
-    else
-      hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, false, true>), grid, threads, 0, s, w, tiles);
-  } else {
-    if (vec)
-      hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, true, false>), grid, threads, 0, s, w, tiles);
-    else
-      hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, false, false>), grid, threads, 0, s, w, tiles);
+  if (w.states_only)
+    hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, PIECE, WHOLE, true>), grid, threads, 0, s, w, tiles);
+  else
+    hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, PIECE, WHOLE, false>), grid, threads, 0, s, w, tiles);
+}
+
+template <typename T, int PIECE, bool WHOLE>
+void dispatch_walk(const WalkArgs& w, WalkClass k, int tiles, unsigned blocks, hipStream_t s) {
+  switch (k.dkt * 8 + k.dvt) {
+    case 2 * 8 + 2: run_walk<T, 2, 2, PIECE, WHOLE>(w, tiles, blocks, s); break;
+    case 2 * 8 + 4: run_walk<T, 2, 4, PIECE, WHOLE>(w, tiles, blocks, s); break;
+    case 4 * 8 + 2: run_walk<T, 4, 2, PIECE, WHOLE>(w, tiles, blocks, s); break;
+    case 4 * 8 + 4: run_walk<T, 4, 4, PIECE, WHOLE>(w, tiles, blocks, s); break;
+    case 8 * 8 + 2: run_walk<T, 8, 2, PIECE, WHOLE>(w, tiles, blocks, s); break;
+    default: run_walk<T, 8, 4, PIECE, WHOLE>(w, tiles, blocks, s); break;
   }
+}
+
+// The largest access that every row of every matrix allows.
+int walk_piece(const WalkArgs& w, int size) {
+  uintptr_t bits = 0;
+  bool near = true;
+  auto add = [&](const WalkMatrix& m, int width) {
+    if (!m.p) return;
+    bits |= reinterpret_cast<uintptr_t>(m.p) | (uintptr_t)(m.step * size) | (uintptr_t)(m.seq * size) | (uintptr_t)(m.head * size) | (uintptr_t)(width * size);
+    const int64_t step = m.step < 0 ? -m.step : m.step;
+    near = near && step < MAX_OFFSET / (size * CHUNK);
+  };
+  for (int j = 0; j < w.jobs; ++j) {
+    add(w.job[j].a, w.job[j].D);
+    add(w.job[j].b, w.job[j].D);
+    add(w.job[j].c, w.job[j].E);
+    add(w.job[j].o, w.job[j].E);
+  }
+  return !near ? 0 : bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
+}
+
+// Whether every width fills its tiles: 32, 64 or 128, the everyday ones.
+bool walk_whole(const WalkArgs& w, WalkClass k) {
+  for (int j = 0; j < w.jobs; ++j)
+    if (w.job[j].D != 16 * k.dkt || w.job[j].E % (16 * k.dvt) != 0) return false;
+  return true;
 }
 
 template <typename T>
-void dispatch_walk(const WalkArgs& w, WalkClass k, bool vec, int tiles, unsigned blocks, hipStream_t s) {
-  switch (k.dkt * 8 + k.dvt) {
-    case 2 * 8 + 2: run_walk<T, 2, 2>(w, vec, tiles, blocks, s); break;
-    case 2 * 8 + 4: run_walk<T, 2, 4>(w, vec, tiles, blocks, s); break;
-    case 4 * 8 + 2: run_walk<T, 4, 2>(w, vec, tiles, blocks, s); break;
-    case 4 * 8 + 4: run_walk<T, 4, 4>(w, vec, tiles, blocks, s); break;
-    case 8 * 8 + 2: run_walk<T, 8, 2>(w, vec, tiles, blocks, s); break;
-    default: run_walk<T, 8, 4>(w, vec, tiles, blocks, s); break;
-  }
-}
-
-// Loads of up to 16 bytes: every row of every matrix starts at a multiple of them and is a whole number of them.
-bool walk_wide(const WalkArgs& w, int size) {
-  const int per = 16 / size;
-  auto fits = [&](const WalkMatrix& m, int width) {
-    return !m.p || ((reinterpret_cast<uintptr_t>(m.p) & 15) == 0 && width % per == 0 && m.step % per == 0 && m.seq % per == 0 && m.head % per == 0);
-  };
-  for (int j = 0; j < w.jobs; ++j) {
-    const WalkJob& k = w.job[j];
-    if (!(fits(k.a, k.D) && fits(k.b, k.D) && fits(k.c, k.E) && fits(k.o, k.E))) return false;
-  }
-  return true;
+void launch_pieces(const WalkArgs& w, WalkClass k, int piece, int tiles, unsigned blocks, hipStream_t s) {
+  if (piece == 16 && walk_whole(w, k)) dispatch_walk<T, 16, true>(w, k, tiles, blocks, s);
+  else if (piece == 16) dispatch_walk<T, 16, false>(w, k, tiles, blocks, s);
+  else if (piece == 4) dispatch_walk<T, 4, false>(w, k, tiles, blocks, s);
+  else if (piece == 0) run_walk<T, 8, 4, 0, false>(w, tiles, blocks, s);       // one class for all widths: rows gigabytes apart are no everyday case
+  else if constexpr (sizeof(T) == 2) dispatch_walk<T, 2, false>(w, k, tiles, blocks, s);
 }
 
 }  // namespace
@@ -537,17 +730,19 @@ hipError_t launch_walk(const WalkArgs& all, int dtype, hipStream_t stream) {
       flops += tokens * x.D * x.E * (all.states_only ? 2 : 4);
       bytes += tokens * size * (all.states_only ? x.D + x.E : 2 * x.D + 2 * x.E);
     }
+    const int piece = walk_piece(w, size);
+    if (piece == 0)
+      for (int i = 0; i < w.jobs; ++i) tiles = max(tiles, (w.job[i].E + 63) / 64);
     const int64_t waves = (int64_t)(w.states_only ? w.segments - 1 : w.segments) * w.N * w.H * tiles * w.jobs;
     const int64_t blocks = (waves + WALK_WAVES - 1) / WALK_WAVES;
     if (blocks > (1 << 23)) return hipErrorInvalidConfiguration;
-    const bool vec = walk_wide(w, size);
     TraceScope trace(stream, w.states_only ? "linear_attention_states" : "linear_attention_walk", flops, bytes);
     if (dtype == RSLX_F32)
-      dispatch_walk<float>(w, k, vec, tiles, (unsigned)blocks, stream);
+      launch_pieces<float>(w, k, piece, tiles, (unsigned)blocks, stream);
     else if (dtype == RSLX_BF16)
-      dispatch_walk<bf16_t>(w, k, vec, tiles, (unsigned)blocks, stream);
+      launch_pieces<bf16_t>(w, k, piece, tiles, (unsigned)blocks, stream);
     else
-      dispatch_walk<__half>(w, k, vec, tiles, (unsigned)blocks, stream);
+      launch_pieces<__half>(w, k, piece, tiles, (unsigned)blocks, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
