@@ -15,6 +15,7 @@
 //   - column tile t is put to e = DVT c + t: C is read, and O written, DVT consecutive values of a row at a time.
 // Every operand comes straight from memory in the layout in which it is used: no LDS, no barriers, no shuffles.
 #include "sequence.h"
+#include "split_bf16.h"
 #include "typed.h"
 
 #include <type_traits>
@@ -25,7 +26,9 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int CHUNK = 16;
+// Positions of a chunk: one block of 16, or two where the 16-bit matrix instructions contract over 32.
+template <typename T> constexpr int BLOCKS = sizeof(T) == 2 ? 2 : 1;
+constexpr int MOST_CHUNK = 32;
 constexpr int WALK_WAVES = 4;           // wavefronts per workgroup; they share nothing but the caches
 
 // N consecutive values as they lie in memory; converted where they are used.
@@ -54,8 +57,8 @@ __device__ __forceinline__ Descriptor descriptor(const void* base, bool exists =
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, exists ? bytes : 0, 0x00020000);
 }
 
-// The 16 rows of a chunk, slot by slot; positions go up or down in memory.
-struct Rows {
+// The rows of a chunk, slot by slot; positions go up or down in memory.
+template <int CHUNK> struct Rows {
   const char* low;               // of the row at the lowest address
   int64_t step;                  // bytes from a position to the next one, either sign
   __device__ __forceinline__ void move(int positions) { low += positions * step; }
@@ -63,8 +66,8 @@ struct Rows {
   __device__ __forceinline__ uint32_t at(int slot) const { return (uint32_t)order(slot) * (uint32_t)(step < 0 ? -step : step); }
   __device__ __forceinline__ const char* address(int slot) const { return low + (int64_t)order(slot) * (step < 0 ? -step : step); }
 };
-template <typename T>
-__device__ __forceinline__ Rows rows_at(const T* first, int64_t step, int position) {
+template <int CHUNK, typename T>
+__device__ __forceinline__ Rows<CHUNK> rows_at(const T* first, int64_t step, int position) {
   const int64_t bytes = step * (int64_t)sizeof(T);
   return {reinterpret_cast<const char*>(first) + (position + (step < 0 ? CHUNK - 1 : 0)) * bytes, bytes};
 }
@@ -174,8 +177,247 @@ __device__ __forceinline__ int sequence_length(const WalkArgs& w, int n) {
   return w.lengths ? min(max(w.lengths[n], 0), w.T) : w.T;
 }
 
+// ---- the four products of a chunk ---------------------------------------------------------------------------------
+// fp32 operands: fp32 matrix instructions, one block of 16 positions.
+//
+// 16-bit operands: v_mfma_f32_16x16x32, two blocks.  Its operands hold eight contraction indices a lane, and again any order will do: of
+// the widths, the lane's 4 DKT consecutive values as they lie in memory, eight by eight (value DKT r + a is row r of state tile a: pairs
+// of tiles fill a register); of the positions, 4 g + s of the first block, then of the second.  What is exact in 16 bits is multiplied as it
+// is; what is not (weighted scores, the state, the weighted C) is taken apart into bf16 values: two for results that are rounded to 16
+// bits (what is left out is 2^-17 of a term, far below that rounding), three for the state, which stays exact to fp32.  fp16 inputs reach
+// products with such parts as two bf16 values of their own, which hold them exactly.
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+template <typename T> constexpr int PARTS = __is_same(T, __half) ? 2 : 1;      // bf16 values that make an input
+
+__device__ __forceinline__ f32x4 mfma_bf16(const uint32_t* a, const uint32_t* b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, (u32x4){a[0], a[1], a[2], a[3]}),
+                                                 __builtin_bit_cast(bf16x8, (u32x4){b[0], b[1], b[2], b[3]}), c, 0, 0, 0);
+}
+__device__ __forceinline__ float low_half(uint32_t x) { return __uint_as_float(x << 16); }
+__device__ __forceinline__ float high_half(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
+
+// Two fp32 values as COUNT packed bf16 values each.
+template <int COUNT>
+__device__ __forceinline__ void parts_of(float x, float y, uint32_t (&p)[COUNT]) {
+#pragma unroll
+  for (int k = 0; k < COUNT; ++k) {
+    p[k] = pack_bf16(x, y);
+    if (k + 1 < COUNT) {
+      x -= low_half(p[k]);
+      y -= high_half(p[k]);
+    }
+  }
+}
+// A register of two inputs as bf16 parts.
+template <typename T>
+__device__ __forceinline__ void input_parts(uint32_t x, uint32_t (&p)[PARTS<T>]) {
+  if constexpr (PARTS<T> == 1) p[0] = x;
+  else parts_of<2>(__half2float(__ushort_as_half((unsigned short)x)), __half2float(__ushort_as_half((unsigned short)(x >> 16))), p);
+}
+// The low (HIGH = 0) or high halves of x and y side by side.
+template <int HIGH> __device__ __forceinline__ uint32_t halves(uint32_t x, uint32_t y) {
+  return __builtin_amdgcn_perm(y, x, HIGH ? 0x07060302u : 0x05040100u);
+}
+// Values i of four rows of each block, position by position, as an operand of eight.
+template <typename T, int N>
+__device__ __forceinline__ void column(const Frag<T, N> (&f)[2][4], int i, uint32_t (&x)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t u = f[k / 2][2 * (k % 2)].w[i / 2], v = f[k / 2][2 * (k % 2) + 1].w[i / 2];
+    x[k] = i % 2 ? halves<1>(u, v) : halves<0>(u, v);
+  }
+}
+
+// Transposed scores of a block: P[j][i] at register r of lane (i = c, g), j = 4 g + r.
+template <typename T, int DKT>
+__device__ __forceinline__ f32x4 scores(const Frag<T, 4 * DKT>& b, const Frag<T, 4 * DKT>& a) {
+  f32x4 p = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int x = 0; x < 4 * DKT; ++x) p = __builtin_amdgcn_mfma_f32_16x16x4f32(b.get(x), a.get(x), p, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int x = 0; x < 2 * DKT; x += 4) {
+      const u32x4 u = {b.w[x], b.w[x + 1], b.w[x + 2], b.w[x + 3]}, v = {a.w[x], a.w[x + 1], a.w[x + 2], a.w[x + 3]};
+      if constexpr (__is_same(T, bf16_t)) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u), __builtin_bit_cast(bf16x8, v), p, 0, 0, 0);
+      else p = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, u), __builtin_bit_cast(f16x8, v), p, 0, 0, 0);
+    }
+  }
+  return p;
+}
+
+// o += A S
+template <typename T, int DKT, int DVT>
+__device__ __forceinline__ void read_state(f32x4 (&o)[BLOCKS<T>][DVT], const Frag<T, 4 * DKT> (&fa)[BLOCKS<T>], const f32x4 (&S)[DKT][DVT]) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int a = 0; a < DKT; ++a)
+#pragma unroll
+        for (int t = 0; t < DVT; ++t) o[0][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[0].get(DKT * s + a), S[a][t][s], o[0][t], 0, 0, 0);
+  } else {
+    constexpr int WORDS = 2 * DKT;
+    uint32_t x[2][PARTS<T>][WORDS];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int k = 0; k < WORDS; ++k) {
+        uint32_t p[PARTS<T>];
+        input_parts<T>(fa[b].w[k], p);
+#pragma unroll
+        for (int i = 0; i < PARTS<T>; ++i) x[b][i][k] = p[i];
+      }
+#pragma unroll
+    for (int t = 0; t < DVT; ++t)
+#pragma unroll
+      for (int k = 0; k < WORDS; k += 4) {
+        uint32_t y[2][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 2 * (k + i) / DKT, a = 2 * (k + i) % DKT;
+          uint32_t p[2];
+          parts_of<2>(S[a][t][r], S[a + 1][t][r], p);
+          y[0][i] = p[0];
+          y[1][i] = p[1];
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < PARTS<T>; ++i)
+#pragma unroll
+            for (int j = 0; j < 2 - i; ++j) o[b][t] = mfma_bf16(&x[b][i][k], y[j], o[b][t]);
+      }
+  }
+}
+
+// o += P C
+template <typename T, int DVT>
+__device__ __forceinline__ void add_values(f32x4 (&o)[BLOCKS<T>][DVT], const f32x4 (&P)[BLOCKS<T>][BLOCKS<T>], const Frag<T, DVT> (&fv)[BLOCKS<T>][4]) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int t = 0; t < DVT; ++t) o[0][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(P[0][0][s], fv[0][s].get(t), o[0][t], 0, 0, 0);
+  } else {
+    uint32_t x[2][2][4];                   // [block of i][part]
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t p[2] = {0u, 0u};
+        if (k / 2 <= b) parts_of<2>(P[k / 2][b][2 * (k % 2)], P[k / 2][b][2 * (k % 2) + 1], p);
+        x[b][0][k] = p[0];
+        x[b][1][k] = p[1];
+      }
+#pragma unroll
+    for (int t = 0; t < DVT; ++t) {
+      uint32_t v[4], y[PARTS<T>][4];
+      column<T, DVT>(fv, t, v);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t p[PARTS<T>];
+        input_parts<T>(v[k], p);
+#pragma unroll
+        for (int j = 0; j < PARTS<T>; ++j) y[j][k] = p[j];
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < PARTS<T> && i + j < 2; ++j) o[b][t] = mfma_bf16(x[b][i], y[j], o[b][t]);
+    }
+  }
+}
+
+// S += (weighted B)^T C; a position whose episode ends inside the chunk leaves nothing.
+template <typename T, int DKT, int DVT>
+__device__ __forceinline__ void add_state(f32x4 (&S)[DKT][DVT], const Frag<T, DKT> (&fk)[BLOCKS<T>][4], const Frag<T, DVT> (&fv)[BLOCKS<T>][4],
+                                          const float (&wk)[BLOCKS<T>][4], uint32_t cut, int g) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const bool stays = (cut >> (4 * g + s)) == 0;
+#pragma unroll
+      for (int a = 0; a < DKT; ++a) {
+        const float k = stays ? fk[0][s].get(a) * wk[0][s] : 0.f;
+#pragma unroll
+        for (int t = 0; t < DVT; ++t) S[a][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k, fv[0][s].get(t), S[a][t], 0, 0, 0);
+      }
+    }
+  } else {
+    uint32_t x[DKT][PARTS<T>][4], mask[4];
+    if (cut) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = 16 * (k / 2) + 4 * g + 2 * (k % 2);
+        mask[k] = ((cut >> i) == 0 ? 0xffffu : 0u) | ((cut >> (i + 1)) == 0 ? 0xffff0000u : 0u);
+      }
+    }
+#pragma unroll
+    for (int a = 0; a < DKT; ++a) {
+      uint32_t v[4];
+      column<T, DKT>(fk, a, v);
+      if (cut)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] &= mask[k];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t p[PARTS<T>];
+        input_parts<T>(v[k], p);
+#pragma unroll
+        for (int i = 0; i < PARTS<T>; ++i) x[a][i][k] = p[i];
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < DVT; ++t) {
+      uint32_t y[3][4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int b = k / 2, s = 2 * (k % 2);
+        uint32_t p[3];
+        parts_of<3>(fv[b][s].get(t) * wk[b][s], fv[b][s + 1].get(t) * wk[b][s + 1], p);
+#pragma unroll
+        for (int j = 0; j < 3; ++j) y[j][k] = p[j];
+      }
+#pragma unroll
+      for (int a = 0; a < DKT; ++a)
+#pragma unroll
+        for (int i = 0; i < PARTS<T>; ++i)
+#pragma unroll
+          for (int j = 0; j < 3 - i; ++j) S[a][t] = mfma_bf16(x[a][i], y[j], S[a][t]);
+    }
+  }
+}
+
+template <typename T, int DVT>
+__device__ __forceinline__ bool not_finite(const Frag<T, DVT> (&fv)[BLOCKS<T>][4]) {
+  if constexpr (sizeof(T) == 4) {
+    float bad = 0.f;
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int t = 0; t < DVT; ++t) bad = fmaf(fv[0][s].get(t), 0.f, bad);
+    return bad != 0.f;
+  } else {
+    // an exponent of ones carries into the sign's place
+    constexpr uint32_t ONE = __is_same(T, __half) ? 0x04000400u : 0x00800080u;
+    uint32_t bad = 0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int k = 0; k < DVT / 2; ++k) bad |= (fv[b][s].w[k] & 0x7fff7fffu) + ONE;
+    return (bad & 0x80008000u) != 0;
+  }
+}
+
 template <typename T, int DKT, int DVT, int PIECE, bool WHOLE, bool STATES>
 __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_kernel(WalkArgs w, int tiles) {
+  constexpr int NB = BLOCKS<T>, CHUNK = 16 * NB;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   int item = uniform((int)blockIdx.x * WALK_WAVES + (int)(threadIdx.x >> 6));
   const int pieces = STATES ? w.segments - 1 : w.segments;
@@ -198,9 +440,9 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
   int at = p0 - skip;                     // position of the chunk's slot 0
   const int64_t first = rev ? len - 1 : 0, dir = rev ? -1 : 1;
   auto rows = [&](const WalkMatrix& m) {
-    return rows_at(static_cast<const T*>(m.p) + n * m.seq + h * m.head + first * m.step, dir * m.step, at);
+    return rows_at<CHUNK>(static_cast<const T*>(m.p) + n * m.seq + h * m.head + first * m.step, dir * m.step, at);
   };
-  Rows A{}, O{}, B = rows(job.b), C = rows(job.c);
+  Rows<CHUNK> A{}, O{}, B = rows(job.b), C = rows(job.c);
   if constexpr (!STATES) {
     A = rows(job.a);
     O = rows(job.o);
@@ -208,19 +450,24 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
 
   // The operands of a chunk; each set is asked for again, for the next chunk, as soon as this one's products have read it: by the time it is
   // needed the other half of a chunk's products has gone by.
-  Frag<T, 4 * DKT> fa, fb;
-  Frag<T, DKT> fk[4];
-  Frag<T, DVT> fv[4];
+  Frag<T, 4 * DKT> fa[NB], fb[NB];
+  Frag<T, DKT> fk[NB][4];
+  Frag<T, DVT> fv[NB][4];
   uint32_t end = 0;
   constexpr int SIZE = (int)sizeof(T);
   const uint32_t at_a = A.at(c) + 4 * DKT * g * SIZE, at_b = B.at(c) + 4 * DKT * g * SIZE, at_k = B.at(4 * g) + DKT * c * SIZE,
                  at_v = C.at(4 * g) + e_lane * SIZE, at_o = O.at(4 * g) + e_lane * SIZE;
   // (at the start: slots below skip do not exist; afterwards all do)
-  auto load_row = [&](auto start, auto& f, const Rows& m, uint32_t from, bool exists) {
+  auto load_row = [&](auto start, auto& f, const Rows<CHUNK>& m, uint32_t from, bool exists) {
     constexpr int N = 4 * DKT;
-    const bool in = !start || c >= skip;
-    if constexpr (PIECE != 0) load_frag<T, N, PIECE, WHOLE>(f, descriptor(m.low, exists), in ? (uint32_t)opaque((int)from) : NOWHERE, opaque(D - 4 * DKT * g));
-    else load_far<T, N>(f, m.address(c), exists && in, 4 * DKT * g, D);
+    const uint32_t from_now = opaque((int)from);
+    const int there = opaque(D - 4 * DKT * g);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const bool in = !start || 16 * b + c >= skip;
+      if constexpr (PIECE != 0) load_frag<T, N, PIECE, WHOLE>(f[b], descriptor(m.low, exists), in ? from_now + (uint32_t)(16 * b * (int)m.step) : NOWHERE, there);
+      else load_far<T, N>(f[b], m.address(16 * b + c), exists && in, 4 * DKT * g, D);
+    }
   };
   auto load_update = [&](auto start, bool exists) {
     if (w.dones && exists) {
@@ -230,16 +477,19 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
     const uint32_t from_k = opaque((int)at_k), from_v = opaque((int)at_v);
     const int there_k = opaque(D - DKT * c), there_v = opaque(E - e_lane);
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const bool in = !start || 4 * g + s >= skip;
-      if constexpr (PIECE != 0) {
-        load_frag<T, DVT, PIECE, WHOLE>(fv[s], descriptor(C.low, exists), in ? from_v + (uint32_t)(s * (int)C.step) : NOWHERE, there_v);
-        load_frag<T, DKT, PIECE, WHOLE>(fk[s], descriptor(B.low, exists), in ? from_k + (uint32_t)(s * (int)B.step) : NOWHERE, there_k);
-      } else {
-        load_far<T, DVT>(fv[s], C.address(4 * g + s), exists && in, e_lane, E);
-        load_far<T, DKT>(fk[s], B.address(4 * g + s), exists && in, DKT * c, D);
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const int slot = 16 * b + 4 * g + s;
+        const bool in = !start || slot >= skip;
+        if constexpr (PIECE != 0) {
+          load_frag<T, DVT, PIECE, WHOLE>(fv[b][s], descriptor(C.low, exists), in ? from_v + (uint32_t)((16 * b + s) * (int)C.step) : NOWHERE, there_v);
+          load_frag<T, DKT, PIECE, WHOLE>(fk[b][s], descriptor(B.low, exists), in ? from_k + (uint32_t)((16 * b + s) * (int)B.step) : NOWHERE, there_k);
+        } else {
+          load_far<T, DVT>(fv[b][s], C.address(slot), exists && in, e_lane, E);
+          load_far<T, DKT>(fk[b][s], B.address(slot), exists && in, DKT * c, D);
+        }
       }
-    }
   };
   constexpr auto START = std::true_type{};
   constexpr auto NEXT = std::false_type{};
@@ -293,17 +543,19 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
     }
   }
 
-  // weights inside a chunk, of the state before it, and towards the state behind it
+  // weights inside a chunk (in a block, and of the second block's positions for the first's), of the state before it, and towards the state behind it
   const double l2 = log2_decay(w.log_decay[h]);
   const float b_scale = rev ? w.scale : 1.f, o_scale = rev ? 1.f : w.scale;
-  float wp[4], wq[4], wk[4];
+  float wp[NB][4], wq[NB][4], wk[NB][4];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int i = 4 * g + r;
-    wp[r] = c >= i ? w.scale * decay_pow(l2, c - i) : 0.f;
-    wq[r] = o_scale * decay_pow(l2, max(i - skip, 0) + lead);
-    wk[r] = b_scale * decay_pow(l2, CHUNK - lead - i);
-  }
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int i = 16 * b + 4 * g + r, gap = 16 * b + c - 4 * g - r;
+      wp[b][r] = gap >= 0 ? w.scale * decay_pow(l2, gap) : 0.f;
+      wq[b][r] = o_scale * decay_pow(l2, max(i - skip, 0) + lead);
+      wk[b][r] = b_scale * decay_pow(l2, CHUNK - lead - i);
+    }
   // The state is multiplied by the same number once a chunk, and its rounding would add up over a long sequence (3e-8 a chunk): every
   // eighth chunk takes off what eight of them left.
   constexpr int CORRECT = 8;
@@ -319,84 +571,81 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
     const bool more = q + 1 < chunks, update = wants_state || more;
     const int skip_now = skip;
     skip = 0;                             // of the next chunk
-    f32x4 o[DVT];
-    f32x4 P = {0.f, 0.f, 0.f, 0.f};
+    f32x4 o[NB][DVT];
+    f32x4 P[NB][NB];                      // [block of j][block of i]
     if constexpr (!STATES) {
 #pragma unroll
-      for (int x = 0; x < 4 * DKT; ++x) P = __builtin_amdgcn_mfma_f32_16x16x4f32(fb.get(x), fa.get(x), P, 0, 0, 0);
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j <= i; ++j) P[j][i] = scores<T, DKT>(fb[j], fa[i]);
       __builtin_amdgcn_sched_barrier(0);      // the next chunk's operands take the registers of this one's
       B.move(CHUNK);
       load_row(NEXT, fb, B, at_b, more);
 #pragma unroll
-      for (int t = 0; t < DVT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int t = 0; t < DVT; ++t) o[b][t] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (live) {
+        read_state<T, DKT, DVT>(o, fa, S);
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int a = 0; a < DKT; ++a)
+          for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int t = 0; t < DVT; ++t) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa.get(DKT * s + a), S[a][t][s], o[t], 0, 0, 0);
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int t = 0; t < DVT; ++t) o[t][r] *= wq[r];
+            for (int t = 0; t < DVT; ++t) o[b][t][r] *= wq[b][r];
       }
       __builtin_amdgcn_sched_barrier(0);
       A.move(CHUNK);
       load_row(NEXT, fa, A, at_a, more);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) P[r] = c >= 4 * g + r ? P[r] * wp[r] : 0.f;
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j <= i; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) P[j][i][r] = j < i || c >= 4 * g + r ? P[j][i][r] * wp[i - j][r] : 0.f;
     } else {
       B.move(CHUNK);
     }
     // bit i: an episode ends between slots i and i + 1
     uint32_t cut = 0;
-    if (w.dones) cut = (uint32_t)__ballot(lane >= skip_now && end != 0 && !(rev && at + lane >= len - 1)) & 0xffffu;
+    if (w.dones) cut = (uint32_t)__ballot(lane < CHUNK && lane >= skip_now && end != 0 && !(rev && at + lane >= len - 1));
     if constexpr (!STATES) {
       if (cut) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int i = 4 * g + r;
-          P[r] = ((cut >> i) & ((1u << ((c - i) & 31)) - 1u)) == 0 ? P[r] : 0.f;
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int t = 0; t < DVT; ++t) o[t][r] = (cut & ((1u << i) - 1u)) == 0 ? o[t][r] : 0.f;
-        }
+          for (int r = 0; r < 4; ++r) {
+            const int i = 16 * b + 4 * g + r;
+#pragma unroll
+            for (int t = 0; t < DVT; ++t) o[b][t][r] = (cut & ((1u << i) - 1u)) == 0 ? o[b][t][r] : 0.f;
+            // here i is the earlier position
+#pragma unroll
+            for (int x = b; x < NB; ++x) P[b][x][r] = ((cut >> i) & ((1u << ((16 * x + c - i) & 31)) - 1u)) == 0 ? P[b][x][r] : 0.f;
+          }
       }
     }
 
     // A position's weight for an earlier or later one that it has nothing to do with is zero, but zero times infinity is not: from a chunk
     // on whose C holds anything that is not finite, positions are taken one by one, as the recurrence has them.
-    float bad = 0.f;
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int t = 0; t < DVT; ++t) bad = fmaf(fv[s].get(t), 0.f, bad);
-    if (__any(bad != 0.f)) {
+    if (__any(not_finite<T, DVT>(fv))) {
       careful = at + skip_now;
       break;
     }
 
-    if constexpr (!STATES) {
+    if (update && live) {
+      if (cut) {                           // (a state that is not finite ends with its episode too)
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+        for (int a = 0; a < DKT; ++a)
 #pragma unroll
-        for (int t = 0; t < DVT; ++t) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(P[s], fv[s].get(t), o[t], 0, 0, 0);
-    }
-    if (update) {
-      if (live) {
-        const float f = cut ? 0.f : keep;
+          for (int t = 0; t < DVT; ++t) S[a][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      } else {
 #pragma unroll
         for (int a = 0; a < DKT; ++a)
 #pragma unroll
           for (int t = 0; t < DVT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[a][t][r] *= f;
-        if (cut) {                       // (a state that is not finite ends with its episode too)
-#pragma unroll
-          for (int a = 0; a < DKT; ++a)
-#pragma unroll
-            for (int t = 0; t < DVT; ++t) S[a][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        } else if (q % CORRECT == CORRECT - 1) {
+            for (int r = 0; r < 4; ++r) S[a][t][r] *= keep;
+        if (q % CORRECT == CORRECT - 1) {
 #pragma unroll
           for (int a = 0; a < DKT; ++a)
 #pragma unroll
@@ -405,17 +654,11 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
               for (int r = 0; r < 4; ++r) S[a][t][r] = fmaf(S[a][t][r], off, S[a][t][r]);
         }
       }
+    }
+    if constexpr (!STATES) add_values<T, DVT>(o, P, fv);
+    if (update) {
+      add_state<T, DKT, DVT>(S, fk, fv, wk, cut, g);
       live = true;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const bool stays = (cut >> (4 * g + s)) == 0;
-#pragma unroll
-        for (int a = 0; a < DKT; ++a) {
-          const float k = stays ? fk[s].get(a) * wk[s] : 0.f;
-#pragma unroll
-          for (int t = 0; t < DVT; ++t) S[a][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k, fv[s].get(t), S[a][t], 0, 0, 0);
-        }
-      }
     }
     __builtin_amdgcn_sched_barrier(0);
     at += CHUNK;
@@ -425,20 +668,25 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
       const uint32_t from_o = opaque((int)at_o);
       const int there_o = opaque(E - e_lane);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float v[DVT];
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int t = 0; t < DVT; ++t) v[t] = o[t][r];
-        if constexpr (PIECE != 0) store_frag<T, DVT, PIECE, WHOLE>(descriptor(O.low), 4 * g + r >= skip_now ? from_o + (uint32_t)(r * (int)O.step) : NOWHERE, there_o, v);
-        else store_far<T, DVT>(O.address(4 * g + r), 4 * g + r >= skip_now, e_lane, E, v);
-      }
+        for (int r = 0; r < 4; ++r) {
+          const int slot = 16 * b + 4 * g + r;
+          float v[DVT];
+#pragma unroll
+          for (int t = 0; t < DVT; ++t) v[t] = o[b][t][r];
+          if constexpr (PIECE != 0) store_frag<T, DVT, PIECE, WHOLE>(descriptor(O.low), slot >= skip_now ? from_o + (uint32_t)((16 * b + r) * (int)O.step) : NOWHERE, there_o, v);
+          else store_far<T, DVT>(O.address(slot), slot >= skip_now, e_lane, E, v);
+        }
+      O.move(CHUNK);
     }
-    if constexpr (!STATES) O.move(CHUNK);
     if constexpr (STATES) any_cut |= cut != 0;
     if (q == 0) {
       keep = keep_whole;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) wq[r] = o_scale * decay_pow(l2, 4 * g + r + lead);
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) wq[b][r] = o_scale * decay_pow(l2, 16 * b + 4 * g + r + lead);
     }
   }
 
@@ -446,7 +694,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
     const int g = opaque(lane >> 4), c = opaque(lane & 15), e_lane = e_tile + DVT * c;
     const float l1 = decay_pow(l2, 1);
     at = careful;
-    Rows a{}, b = rows(job.b), z = rows(job.c), out{};
+    Rows<CHUNK> a{}, b = rows(job.b), z = rows(job.c), out{};
     if constexpr (!STATES) {
       a = rows(job.a);
       out = rows(job.o);
@@ -508,8 +756,8 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
     // steps that do not exist: zero
     const float zero[DVT] = {};
     const int t0 = max(len, piece * w.seg_len), t1 = piece == w.segments - 1 ? w.T : min((piece + 1) * w.seg_len, w.T);
-    Rows Z = rows_at(static_cast<const T*>(job.o.p) + n * job.o.seq + h * job.o.head, job.o.step, t0);
-    for (int t = t0; t < t1; t += CHUNK, Z.move(CHUNK))
+    Rows<CHUNK> Z = rows_at<CHUNK>(static_cast<const T*>(job.o.p) + n * job.o.seq + h * job.o.head, job.o.step, t0);
+    for (int t = t0; t < t1; t += 16, Z.move(16))
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const bool exists = 4 * g + r < t1 - t;
@@ -658,7 +906,7 @@ int walk_piece(const WalkArgs& w, int size) {
     if (!m.p) return;
     bits |= reinterpret_cast<uintptr_t>(m.p) | (uintptr_t)(m.step * size) | (uintptr_t)(m.seq * size) | (uintptr_t)(m.head * size) | (uintptr_t)(width * size);
     const int64_t step = m.step < 0 ? -m.step : m.step;
-    near = near && step < MAX_OFFSET / (size * CHUNK);
+    near = near && step < MAX_OFFSET / (size * MOST_CHUNK);
   };
   for (int j = 0; j < w.jobs; ++j) {
     add(w.job[j].a, w.job[j].D);
@@ -700,10 +948,10 @@ int walk_segments(int64_t waves, int32_t T, int32_t* seg_len) {
   m = m < T / LEAST ? m : T / LEAST;
   m = m < JOIN_MAX ? m : JOIN_MAX;
   if (m <= 1) {
-    *seg_len = T < 1 ? CHUNK : (T + CHUNK - 1) / CHUNK * CHUNK;
+    *seg_len = T < 1 ? MOST_CHUNK : (T + MOST_CHUNK - 1) / MOST_CHUNK * MOST_CHUNK;
     return 1;
   }
-  const int64_t len = ((T + m - 1) / m + CHUNK - 1) / CHUNK * CHUNK;
+  const int64_t len = ((T + m - 1) / m + MOST_CHUNK - 1) / MOST_CHUNK * MOST_CHUNK;
   *seg_len = (int32_t)len;
   return (int)((T + len - 1) / len);
 }
