@@ -92,7 +92,8 @@ void plan_attn(Carver& c, const rslx_linear_attn& a, bool backward, AttnPlan& p)
   memset(&p, 0, sizeof p);
   p.sets = backward ? 2 : 1;
   const int64_t heads = (int64_t)a.N * a.H;
-  const int64_t waves = heads * (walk_waves_per_head(a.Dk, a.Dv) + (backward ? 2 * walk_waves_per_head(a.Dv, a.Dk) : 0));
+  const int size = type_size(a.dtype);
+  const int64_t waves = heads * (walk_waves_per_head(a.Dk, a.Dv, size) + (backward ? 2 * walk_waves_per_head(a.Dv, a.Dk, size) : 0));
   p.segments = walk_segments(waves, a.T, &p.seg_len);
   if (p.segments > 1) {
     for (int s = 0; s < p.sets; ++s) p.states[s] = c.take<float>((size_t)heads * p.segments * a.Dk * a.Dv);

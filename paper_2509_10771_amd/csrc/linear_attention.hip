@@ -9,9 +9,9 @@
 // moved between lanes.  With lane = 16 g + c, the instruction v_mfma_f32_16x16x4_f32 leaves in register r row 4 g + r of column c, and
 // reads from an operand row (column) c at index g.  So
 //   - the transposed scores B A^T leave P[c][4 g + r]: the left operand of P C if step s takes the contraction index 4 g + s;
-//   - row r of state tile a is put to index d = DKT (4 g + r) + a: then the state's registers are the right operand of A S as they
-//     are, if lane (c, g) holds A[c][4 DKT g ...], 4 DKT consecutive values; and the left operand of the state's update, tile a, is
-//     B[4 g + s][DKT c + a]: DKT consecutive values of a row;
+//   - rows of state tiles are put to indices so that the state's registers are the right operand of A S as they are when lane (c, g) holds
+//     4 DKT values of row c of A, loaded 16 bytes at a time (place() below); and the left operand of the state's update is then, for all
+//     tiles, DKT consecutive values of a row of B (two times four for fp32 keys of 128);
 //   - column tile t is put to e = DVT c + t: C is read, and O written, DVT consecutive values of a row at a time.
 // Every operand comes straight from memory in the layout in which it is used: no LDS, no barriers, no shuffles.
 #include "sequence.h"
@@ -72,6 +72,11 @@ __device__ __forceinline__ Rows<CHUNK> rows_at(const T* first, int64_t step, int
   return {reinterpret_cast<const char*>(first) + (position + (step < 0 ? CHUNK - 1 : 0)) * bytes, bytes};
 }
 
+// Where a lane's N values of a row of keys lie: 16 bytes, then 16 more behind those of the other three groups of lanes, so that an access
+// of a wavefront covers 64 bytes of 16 rows.  Value y of group g is at place(y) + PE g.
+template <typename T> constexpr int PE16 = 16 / (int)sizeof(T);
+template <typename T> __device__ __forceinline__ constexpr int place(int y) { return 4 * PE16<T> * (y / PE16<T>) + y % PE16<T>; }
+
 // A value that the compiler does not know: what is made of it is neither kept from elsewhere nor made ahead of time (in registers that the
 // products need).
 __device__ __forceinline__ int opaque(int x) {
@@ -79,13 +84,15 @@ __device__ __forceinline__ int opaque(int x) {
   return x;
 }
 
-// N values of a row from offset `at` on (or NOWHERE).  `there`: how many of them the row has; WHOLE: all.
-template <typename T, int N, int PIECE, bool WHOLE>
+// N values of a row from offset `at` on (or NOWHERE).  `there`: how many values the row has from there on; WHOLE: enough.  APART: in the order of
+// place().
+template <typename T, int N, int PIECE, bool WHOLE, bool APART = false>
 __device__ __forceinline__ void load_frag(Frag<T, N>& f, Descriptor d, uint32_t at, int there) {
   constexpr int WORDS = Frag<T, N>::WORDS, PB = PIECE < WORDS * 4 ? PIECE : WORDS * 4, PE = PB / (int)sizeof(T);
 #pragma unroll
   for (int k = 0; k < N / PE; ++k) {
-    const int o = (int)(WHOLE || k * PE < there ? at + (uint32_t)(k * PB) : NOWHERE);
+    const int e = APART ? place<T>(k * PE) : k * PE;
+    const int o = (int)(WHOLE || e < there ? at + (uint32_t)(e * (int)sizeof(T)) : NOWHERE);
     if constexpr (PB == 16) {
       const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(d, o, 0, 0);
 #pragma unroll
@@ -102,14 +109,14 @@ __device__ __forceinline__ void load_frag(Frag<T, N>& f, Descriptor d, uint32_t 
     }
   }
 }
-template <typename T, int N>
+template <typename T, int N, bool APART = false>
 __device__ __forceinline__ void load_far(Frag<T, N>& f, const char* row, bool exists, int e0, int width) {
 #pragma unroll
   for (int k = 0; k < Frag<T, N>::WORDS; ++k) {
     f.w[k] = 0;
 #pragma unroll
     for (int h = 0; h < 4 / (int)sizeof(T); ++h) {
-      const int e = e0 + k * (4 / (int)sizeof(T)) + h;
+      const int y = k * (4 / (int)sizeof(T)) + h, e = e0 + (APART ? place<T>(y) : y);
       if (!exists || e >= width) continue;
       if constexpr (sizeof(T) == 4) f.w[k] = reinterpret_cast<const uint32_t*>(row)[e];
       else f.w[k] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[e] << (16 * h);
@@ -455,18 +462,20 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
   Frag<T, DVT> fv[NB][4];
   uint32_t end = 0;
   constexpr int SIZE = (int)sizeof(T);
-  const uint32_t at_a = A.at(c) + 4 * DKT * g * SIZE, at_b = B.at(c) + 4 * DKT * g * SIZE, at_k = B.at(4 * g) + DKT * c * SIZE,
+  // row c = 4 (c / 4) + c % 4 of state tile a is index place(DKT (c % 4) + a) + PE (c / 4): the first of this lane's DKT values for the state
+  const int d_col = place<T>(DKT * (c & 3)) + PE16<T> * (c >> 2);
+  const uint32_t at_a = A.at(c) + PE16<T> * g * SIZE, at_b = B.at(c) + PE16<T> * g * SIZE, at_k = B.at(4 * g) + d_col * SIZE,
                  at_v = C.at(4 * g) + e_lane * SIZE, at_o = O.at(4 * g) + e_lane * SIZE;
   // (at the start: slots below skip do not exist; afterwards all do)
   auto load_row = [&](auto start, auto& f, const Rows<CHUNK>& m, uint32_t from, bool exists) {
     constexpr int N = 4 * DKT;
     const uint32_t from_now = opaque((int)from);
-    const int there = opaque(D - 4 * DKT * g);
+    const int there = opaque(D - PE16<T> * g);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const bool in = !start || 16 * b + c >= skip;
-      if constexpr (PIECE != 0) load_frag<T, N, PIECE, WHOLE>(f[b], descriptor(m.low, exists), in ? from_now + (uint32_t)(16 * b * (int)m.step) : NOWHERE, there);
-      else load_far<T, N>(f[b], m.address(16 * b + c), exists && in, 4 * DKT * g, D);
+      if constexpr (PIECE != 0) load_frag<T, N, PIECE, WHOLE, true>(f[b], descriptor(m.low, exists), in ? from_now + (uint32_t)(16 * b * (int)m.step) : NOWHERE, there);
+      else load_far<T, N, true>(f[b], m.address(16 * b + c), exists && in, PE16<T> * g, D);
     }
   };
   auto load_update = [&](auto start, bool exists) {
@@ -475,7 +484,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
       end = w.dones[(int64_t)min(max(t, 0), len - 1) * w.N + n];
     }
     const uint32_t from_k = opaque((int)at_k), from_v = opaque((int)at_v);
-    const int there_k = opaque(D - DKT * c), there_v = opaque(E - e_lane);
+    const int there_k = opaque(D - d_col), there_v = opaque(E - e_lane);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -484,10 +493,10 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
         const bool in = !start || slot >= skip;
         if constexpr (PIECE != 0) {
           load_frag<T, DVT, PIECE, WHOLE>(fv[b][s], descriptor(C.low, exists), in ? from_v + (uint32_t)((16 * b + s) * (int)C.step) : NOWHERE, there_v);
-          load_frag<T, DKT, PIECE, WHOLE>(fk[b][s], descriptor(B.low, exists), in ? from_k + (uint32_t)((16 * b + s) * (int)B.step) : NOWHERE, there_k);
+          load_frag<T, DKT, PIECE, WHOLE, true>(fk[b][s], descriptor(B.low, exists), in ? from_k + (uint32_t)((16 * b + s) * (int)B.step) : NOWHERE, there_k);
         } else {
           load_far<T, DVT>(fv[b][s], C.address(slot), exists && in, e_lane, E);
-          load_far<T, DKT>(fk[b][s], B.address(slot), exists && in, DKT * c, D);
+          load_far<T, DKT, true>(fk[b][s], B.address(slot), exists && in, d_col, D);
         }
       }
   };
@@ -517,7 +526,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
           float v[DVT];
           uint32_t o[DVT];
 #pragma unroll
-          for (int t = 0; t < DVT; ++t) o[t] = e_lane + t < E ? (uint32_t)((DKT * (4 * g + i) + a) * E + e_lane + t) * 4 : NOWHERE;
+          for (int t = 0; t < DVT; ++t) o[t] = e_lane + t < E ? (uint32_t)((place<T>(DKT * i + a) + PE16<T> * g) * E + e_lane + t) * 4 : NOWHERE;
           if (E % DVT == 0) load_state<DVT, DVT * 4>(v, d, o);
           else load_state<DVT, 4>(v, d, o);
 #pragma unroll
@@ -532,10 +541,10 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
           uint32_t o[DKT];
 #pragma unroll
           for (int a = 0; a < DKT; ++a) {
-            const int x = DKT * (4 * g + i) + a;
+            const int x = place<T>(DKT * i + a) + PE16<T> * g;
             o[a] = x < D ? (uint32_t)((e_lane + t) * D + x) * 4 : NOWHERE;
           }
-          if (D % DKT == 0) load_state<DKT, (DKT < 4 ? DKT : 4) * 4>(v, d, o);
+          if (D % (DKT < 4 ? DKT : 4) == 0) load_state<DKT, (DKT < 4 ? DKT : 4) * 4>(v, d, o);
           else load_state<DKT, 4>(v, d, o);
 #pragma unroll
           for (int a = 0; a < DKT; ++a) S[a][t][i] = v[a];
@@ -568,7 +577,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
   bool any_cut = false;
   int careful = p1;                       // positions from here on are taken one by one
   for (int q = 0; q < chunks; ++q) {
-    const bool more = q + 1 < chunks, update = wants_state || more;
+    const bool more = q + 1 < chunks;
     const int skip_now = skip;
     skip = 0;                             // of the next chunk
     f32x4 o[NB][DVT];
@@ -578,9 +587,11 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
       for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int j = 0; j <= i; ++j) P[j][i] = scores<T, DKT>(fb[j], fa[i]);
-      __builtin_amdgcn_sched_barrier(0);      // the next chunk's operands take the registers of this one's
       B.move(CHUNK);
-      load_row(NEXT, fb, B, at_b, more);
+      if constexpr (NB == 1) {
+        __builtin_amdgcn_sched_barrier(0);    // the next chunk's operands take the registers of this one's
+        load_row(NEXT, fb, B, at_b, more);
+      }
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -595,6 +606,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
             for (int t = 0; t < DVT; ++t) o[b][t][r] *= wq[b][r];
       }
       __builtin_amdgcn_sched_barrier(0);
+      if constexpr (NB == 2) load_row(NEXT, fb, B, at_b, more);      // (not earlier: reading the state needs the registers)
       A.move(CHUNK);
       load_row(NEXT, fa, A, at_a, more);
 #pragma unroll
@@ -632,7 +644,25 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
       break;
     }
 
-    if (update && live) {
+    if constexpr (!STATES) {
+      add_values<T, DVT>(o, P, fv);
+      const uint32_t from_o = opaque((int)at_o);
+      const int there_o = opaque(E - e_lane);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int slot = 16 * b + 4 * g + r;
+          float v[DVT];
+#pragma unroll
+          for (int t = 0; t < DVT; ++t) v[t] = o[b][t][r];
+          if constexpr (PIECE != 0) store_frag<T, DVT, PIECE, WHOLE>(descriptor(O.low), slot >= skip_now ? from_o + (uint32_t)((16 * b + r) * (int)O.step) : NOWHERE, there_o, v);
+          else store_far<T, DVT>(O.address(slot), slot >= skip_now, e_lane, E, v);
+        }
+      O.move(CHUNK);
+    }
+    if (!more && !wants_state) break;       // nobody reads the state behind the last chunk
+    if (live) {
       if (cut) {                           // (a state that is not finite ends with its episode too)
 #pragma unroll
         for (int a = 0; a < DKT; ++a)
@@ -655,31 +685,12 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
         }
       }
     }
-    if constexpr (!STATES) add_values<T, DVT>(o, P, fv);
-    if (update) {
-      add_state<T, DKT, DVT>(S, fk, fv, wk, cut, g);
-      live = true;
-    }
+    add_state<T, DKT, DVT>(S, fk, fv, wk, cut, g);
+    live = true;
     __builtin_amdgcn_sched_barrier(0);
     at += CHUNK;
     C.move(CHUNK);
     load_update(NEXT, more);
-    if constexpr (!STATES) {
-      const uint32_t from_o = opaque((int)at_o);
-      const int there_o = opaque(E - e_lane);
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int slot = 16 * b + 4 * g + r;
-          float v[DVT];
-#pragma unroll
-          for (int t = 0; t < DVT; ++t) v[t] = o[b][t][r];
-          if constexpr (PIECE != 0) store_frag<T, DVT, PIECE, WHOLE>(descriptor(O.low), slot >= skip_now ? from_o + (uint32_t)((16 * b + r) * (int)O.step) : NOWHERE, there_o, v);
-          else store_far<T, DVT>(O.address(slot), slot >= skip_now, e_lane, E, v);
-        }
-      O.move(CHUNK);
-    }
     if constexpr (STATES) any_cut |= cut != 0;
     if (q == 0) {
       keep = keep_whole;
@@ -704,9 +715,9 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
       const bool cut = w.dones && t >= 0 && w.dones[(int64_t)t * w.N + n] != 0;
       Frag<T, 4 * DKT> xa, xb;
       Frag<T, DVT> xc;
-      load_far<T, 4 * DKT>(xb, b.address(0), true, 4 * DKT * g, D);
+      load_far<T, 4 * DKT, true>(xb, b.address(0), true, PE16<T> * g, D);
       load_far<T, DVT>(xc, z.address(0), true, e_lane, E);
-      if constexpr (!STATES) load_far<T, 4 * DKT>(xa, a.address(0), true, 4 * DKT * g, D);
+      if constexpr (!STATES) load_far<T, 4 * DKT, true>(xa, a.address(0), true, PE16<T> * g, D);
       float sum[DVT] = {};
 #pragma unroll
       for (int x = 0; x < DKT; ++x)
@@ -745,7 +756,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
         float v[DVT];
 #pragma unroll
         for (int t = 0; t < DVT; ++t) v[t] = S[a][t][i];
-        const uint32_t o = (uint32_t)((DKT * (4 * g + i) + a) * E + e_lane) * 4;
+        const uint32_t o = (uint32_t)((place<T>(DKT * i + a) + PE16<T> * g) * E + e_lane) * 4;
         if (E % DVT == 0) store_frag<float, DVT, 16, false>(d, o, E - e_lane, v);
         else store_frag<float, DVT, 4, false>(d, o, E - e_lane, v);
       }
@@ -875,7 +886,7 @@ __global__ __launch_bounds__(256) void attention_step_kernel(StepArgs a, int LR)
 }
 
 struct WalkClass { int dkt, dvt; };
-WalkClass walk_class(int D, int E) { return {D <= 32 ? 2 : D <= 64 ? 4 : 8, E <= 32 ? 2 : 4}; }
+WalkClass walk_class(int D, int E, int size) { return {D <= 32 ? 2 : D <= 64 ? 4 : 8, E <= 32 || (D > 64 && size == 2) ? 2 : 4}; }
 
 template <typename T, int DKT, int DVT, int PIECE, bool WHOLE>
 void run_walk(const WalkArgs& w, int tiles, unsigned blocks, hipStream_t s) {
@@ -935,8 +946,8 @@ void launch_pieces(const WalkArgs& w, WalkClass k, int piece, int tiles, unsigne
 
 }  // namespace
 
-int walk_waves_per_head(int D, int E) {
-  const WalkClass k = walk_class(D, E);
+int walk_waves_per_head(int D, int E, int size) {
+  const WalkClass k = walk_class(D, E, size);
   return (E + 16 * k.dvt - 1) / (16 * k.dvt);
 }
 
@@ -962,18 +973,18 @@ hipError_t launch_walk(const WalkArgs& all, int dtype, hipStream_t stream) {
   for (int j = 0; j < all.jobs; ++j) {
     if (done[j]) continue;
     // jobs of the same tile class share a launch: they read the same matrices
-    const WalkClass k = walk_class(all.job[j].D, all.job[j].E);
+    const WalkClass k = walk_class(all.job[j].D, all.job[j].E, size);
     WalkArgs w = all;
     w.jobs = 0;
     int tiles = 0;
     double flops = 0, bytes = 0;
     for (int i = j; i < all.jobs; ++i) {
-      const WalkClass q = walk_class(all.job[i].D, all.job[i].E);
+      const WalkClass q = walk_class(all.job[i].D, all.job[i].E, size);
       if (done[i] || q.dkt != k.dkt || q.dvt != k.dvt) continue;
       done[i] = true;
       w.job[w.jobs++] = all.job[i];
       const WalkJob& x = all.job[i];
-      tiles = max(tiles, walk_waves_per_head(x.D, x.E));
+      tiles = max(tiles, walk_waves_per_head(x.D, x.E, size));
       const double tokens = (double)all.T * all.N * all.H;
       flops += tokens * x.D * x.E * (all.states_only ? 2 : 4);
       bytes += tokens * size * (all.states_only ? x.D + x.E : 2 * x.D + 2 * x.E);

@@ -59,7 +59,7 @@ struct WalkArgs {
   int32_t* cuts;                // [job][N][segments]: whether an episode ends behind one of its positions
 };
 int walk_segments(int64_t waves, int32_t T, int32_t* seg_len);
-int walk_waves_per_head(int D, int E);
+int walk_waves_per_head(int D, int E, int size);      // size: bytes of a value
 hipError_t launch_walk(const WalkArgs& w, int dtype, hipStream_t stream);
 // slot[0] = start (0 where the sequence's last step ends an episode and the walk is reversed), slot[m + 1] = decay^len_m slot[m] + slot[m + 1]
 hipError_t launch_walk_join(const WalkArgs& w, const float* const* starts, hipStream_t stream);
