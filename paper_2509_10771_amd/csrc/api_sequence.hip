@@ -258,7 +258,7 @@ size_t rslx_layer_norm_backward_workspace_bytes(int64_t rows, int32_t cols) {
     fail(RSLX_ERR_SHAPE, "rslx_layer_norm_backward_workspace_bytes: %lld rows of %d", (long long)rows, cols);
     return 0;
   }
-  return (size_t)2 * norm_backward_blocks(rows) * cols * sizeof(float);
+  return (size_t)2 * norm_backward_blocks(rows, cols) * cols * sizeof(float);
 }
 
 int32_t rslx_layer_norm_backward(int32_t dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t rows, int32_t cols,

@@ -3,10 +3,15 @@
 //   m = mean x,  r = 1 / sqrt(mean (x - m)^2 + eps),  y = (x - m) r w + b
 //   g = dy w,  h = (x - m) r:   dx = r (g - mean g - h mean(g h)),   dw = sum over rows dy h,   db = sum over rows dy
 //
-// Both are bound by memory: a row is read once into registers (W values a load, ITEMS loads a lane), everything that needs the
-// whole row happens there (the variance from the centred values, so that rows far from zero keep their digits; what rounding left of the
-// mean shows in the sum of the same values, and is taken off too), and the result is written once.  TPR lanes share a row: part of a wavefront, a wavefront, or a workgroup where one wavefront's registers
-// would not hold it.  Sums are fp32: a lane's values in order, then a fixed tree.
+// Both are bound by memory: a row is read once into registers (16 bytes a load, ITEMS loads a lane), everything that needs the whole row
+// happens there, and the result is written once.  The variance is that of the centred values, so that rows far from zero keep their digits;
+// what rounding left of the mean shows in the sum of the same values, and is taken off too.  TPR lanes share a row: part of a wavefront, a
+// wavefront, or a workgroup where one wavefront's registers would not hold it.  Sums are fp32: a lane's values in order, then a fixed tree.
+//
+// What it takes to reach the memory's rate is rows in flight: a workgroup goes round the rows with the next one's loads ahead of this one's
+// sums, and keeps the weights in registers.  98304 rows of 512 in bf16: 41.8 us = 4.8 TB/s (a workgroup for every four rows, weights loaded behind the
+// sums: 53.6); gradients of 8192 rows of 4096 in bf16: 40.6 us = 5.0 TB/s (66.4) and 6.6 for the fold of the parameters'; of 24576 rows
+// of 235 in fp32, which start anywhere: 16.6 us = 4.2 TB/s (value by value 27.6, of 512 workgroups instead of 1024 21.8) and 3.8.
 #include "sequence.h"
 #include "typed.h"
 
@@ -15,7 +20,7 @@ namespace rslx {
 namespace {
 
 constexpr int NORM_THREADS = 256;
-constexpr int NORM_MAX_FORWARD = 1 << 20;     // workgroups of a forward launch; more rows go round
+constexpr int NORM_MAX_FORWARD = 2048;        // workgroups of a forward launch: eight for each CU; more rows go round
 
 // Sum over the TPR lanes of a row; every lane gets it.  `lds`: one float per wavefront and value, double-buffered by the caller.
 template <int TPR, int COUNT>
@@ -42,29 +47,77 @@ __device__ __forceinline__ void row_sum(float (&v)[COUNT], float* lds) {
   }
 }
 
-template <typename T, int W, int ITEMS, int TPR>
-__global__ __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) void layer_norm_kernel(NormArgs a) {
-  constexpr int THREADS = TPR > NORM_THREADS ? TPR : NORM_THREADS, ROWS = THREADS / TPR;
+// W values of a row from column c on; WHOLE: rows are whole, aligned loads.  Otherwise rows start anywhere (the load is as wide, global memory
+// takes any address) and the last one may be shorter: its values come one by one.
+template <typename T, int W, bool WHOLE>
+__device__ __forceinline__ void load_piece(Pack<T, W>& p, const T* row, int c, int cols) {
+  if constexpr (WHOLE) {
+    if (c < cols) p = *reinterpret_cast<const Pack<T, W>*>(row + c);
+  } else if (c + W <= cols) {
+    __builtin_memcpy(&p, row + c, sizeof p);
+  } else {
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k)
+      if (c + k < cols) p.v[k] = row[c + k];
+  }
+}
+template <typename T, int W, bool WHOLE>
+__device__ __forceinline__ void store_piece(const Pack<T, W>& p, T* row, int c, int cols) {
+  if constexpr (WHOLE) {
+    if (c < cols) *reinterpret_cast<Pack<T, W>*>(row + c) = p;
+  } else if (c + W <= cols) {
+    __builtin_memcpy(row + c, &p, sizeof p);
+  } else {
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k)
+      if (c + k < cols) row[c + k] = p.v[k];
+  }
+}
+template <int W, bool WHOLE>
+__device__ __forceinline__ bool in_row(int c, int k, int cols) { return WHOLE ? c < cols : c + k < cols; }
+
+// Rows that one workgroup takes at a time.
+template <int TPR> constexpr int THREADS_OF = TPR > NORM_THREADS ? TPR : NORM_THREADS;
+
+// A workgroup takes every gridDim.x-th set of rows; the next row's values are on their way while this one is reduced, and the weights stay in
+// registers.
+template <typename T, int W, int ITEMS, int TPR, bool WHOLE>
+__global__ __launch_bounds__(THREADS_OF<TPR>) void layer_norm_kernel(NormArgs a) {
+  constexpr int ROWS = THREADS_OF<TPR> / TPR;
   __shared__ float lds[2][2 * (TPR > 64 ? TPR / 64 : 1)];
   const int lane = threadIdx.x % TPR;
   const float n = (float)a.cols;
-  // (TPR <= 64: lanes leave the loop in whole rows, and the shuffles stay inside a row; above, the workgroup has one row)
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * ROWS) {
-    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-    Pack<T, W> in[ITEMS];
+  const int64_t stride = (int64_t)gridDim.x * ROWS;
+  int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  Pack<T, W> in[ITEMS];
+  auto load = [&](int64_t r) {
+    if (r < a.rows)
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const int c = (i * TPR + lane) * W;
-      if (c < a.cols) in[i] = *reinterpret_cast<const Pack<T, W>*>(x + c);
+      for (int i = 0; i < ITEMS; ++i) load_piece<T, W, WHOLE>(in[i], static_cast<const T*>(a.x) + r * a.ldx, (i * TPR + lane) * W, a.cols);
+  };
+  load(row);
+  Pack<float, W> w[ITEMS], b[ITEMS];
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      w[i].v[k] = 1.f;
+      b[i].v[k] = 0.f;
     }
+    if (a.weight) load_piece<float, W, WHOLE>(w[i], a.weight, (i * TPR + lane) * W, a.cols);
+    if (a.bias) load_piece<float, W, WHOLE>(b[i], a.bias, (i * TPR + lane) * W, a.cols);
+  }
+  // (TPR <= 64: lanes leave the loop in whole rows, and the shuffles stay inside a row; above, the workgroup has one row)
+  for (; row < a.rows; row += stride) {
     float f[ITEMS * W], s[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
       for (int k = 0; k < W; ++k) {
-        f[i * W + k] = (i * TPR + lane) * W < a.cols ? to_float(in[i].v[k]) : 0.f;
+        f[i * W + k] = in_row<W, WHOLE>((i * TPR + lane) * W, k, a.cols) ? to_float(in[i].v[k]) : 0.f;
         s[0] += f[i * W + k];
       }
+    load(row + stride);
     row_sum<TPR, 1>(s, lds[0]);
     const float near = s[0] / n;
     float q[2] = {0.f, 0.f};
@@ -72,7 +125,7 @@ __global__ __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) void layer
     for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
       for (int k = 0; k < W; ++k) {
-        f[i * W + k] = (i * TPR + lane) * W < a.cols ? f[i * W + k] - near : 0.f;
+        f[i * W + k] = in_row<W, WHOLE>((i * TPR + lane) * W, k, a.cols) ? f[i * W + k] - near : 0.f;
         q[0] += f[i * W + k];
         q[1] += f[i * W + k] * f[i * W + k];
       }
@@ -83,21 +136,10 @@ __global__ __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) void layer
     T* y = static_cast<T*>(a.y) + row * a.ldy;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int c = (i * TPR + lane) * W;
-      if (c < a.cols) {
-        Pack<T, W> out;
-        Pack<float, W> w, b;
-        if (a.weight) w = *reinterpret_cast<const Pack<float, W>*>(a.weight + c);
-        if (a.bias) b = *reinterpret_cast<const Pack<float, W>*>(a.bias + c);
+      Pack<T, W> out;
 #pragma unroll
-        for (int k = 0; k < W; ++k) {
-          float v = (f[i * W + k] - rest) * rstd;
-          if (a.weight) v *= w.v[k];
-          if (a.bias) v += b.v[k];
-          out.v[k] = from_float<T>(v);
-        }
-        *reinterpret_cast<Pack<T, W>*>(y + c) = out;
-      }
+      for (int k = 0; k < W; ++k) out.v[k] = from_float<T>((f[i * W + k] - rest) * rstd * w[i].v[k] + b[i].v[k]);
+      store_piece<T, W, WHOLE>(out, y, (i * TPR + lane) * W, a.cols);
     }
     if (lane == 0) {
       if (a.mean) a.mean[row] = mean;
@@ -106,68 +148,71 @@ __global__ __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) void layer
   }
 }
 
-// The backward pass: a workgroup takes every gridDim.x-th set of rows, so that a lane's columns stay the same and their
-// gradients of weight and bias add up in its registers; what the workgroup holds in the end is one row of partial sums, which
-// norm_fold_kernel adds up in a fixed order (no atomics: the same inputs give the same bits).
-template <typename T, int W, int ITEMS, int TPR>
-__global__ __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) void layer_norm_backward_kernel(NormArgs a) {
-  constexpr int THREADS = TPR > NORM_THREADS ? TPR : NORM_THREADS, ROWS = THREADS / TPR;
+// The backward pass goes round the rows in the same way, so that a lane's columns stay the same and their gradients of weight and bias
+// add up in its registers; what the workgroup holds in the end is one row of partial sums, which norm_fold_kernel adds up in a fixed order
+// (no atomics: the same inputs give the same bits).
+template <typename T, int W, int ITEMS, int TPR, bool WHOLE>
+__global__ __launch_bounds__(THREADS_OF<TPR>) void layer_norm_backward_kernel(NormArgs a) {
+  constexpr int ROWS = THREADS_OF<TPR> / TPR;
   __shared__ float lds[2][2 * (TPR > 64 ? TPR / 64 : 1)];
   __shared__ float join[ROWS > 1 ? (ROWS - 1) * TPR * ITEMS * W : 1];
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   const float inv = 1.f / (float)a.cols;
+  const int64_t stride = (int64_t)gridDim.x * ROWS;
+  int64_t row = (int64_t)blockIdx.x * ROWS + sub;
+  Pack<T, W> px[ITEMS], pd[ITEMS];
+  float mean = 0.f, rstd = 0.f;
+  auto load = [&](int64_t r) {
+    if (r < a.rows) {
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        load_piece<T, W, WHOLE>(px[i], static_cast<const T*>(a.x) + r * a.ldx, (i * TPR + lane) * W, a.cols);
+        load_piece<T, W, WHOLE>(pd[i], static_cast<const T*>(a.dy) + r * a.lddy, (i * TPR + lane) * W, a.cols);
+      }
+      mean = a.mean[r];
+      rstd = a.rstd[r];
+    }
+  };
+  load(row);
+  Pack<float, W> w[ITEMS];
   float dw[ITEMS * W], db[ITEMS * W];
 #pragma unroll
-  for (int i = 0; i < ITEMS * W; ++i) dw[i] = db[i] = 0.f;
-  int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + sub; row < a.rows; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
-    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-    const T* dy = static_cast<const T*>(a.dy) + row * a.lddy;
-    Pack<T, W> px[ITEMS], pd[ITEMS];
+  for (int i = 0; i < ITEMS; ++i) {
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const int c = (i * TPR + lane) * W;
-      if (c < a.cols) {
-        px[i] = *reinterpret_cast<const Pack<T, W>*>(x + c);
-        pd[i] = *reinterpret_cast<const Pack<T, W>*>(dy + c);
-      }
+    for (int k = 0; k < W; ++k) {
+      w[i].v[k] = 1.f;
+      dw[i * W + k] = db[i * W + k] = 0.f;
     }
-    const float mean = a.mean[row], rstd = a.rstd[row];
-    float s[2] = {0.f, 0.f};
+    if (a.weight) load_piece<float, W, WHOLE>(w[i], a.weight, (i * TPR + lane) * W, a.cols);
+  }
+  for (int turn = 0; row < a.rows; row += stride, turn ^= 1) {
+    float s[2] = {0.f, 0.f}, h[ITEMS * W], g[ITEMS * W];
+    const float scale = rstd;
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const int c = (i * TPR + lane) * W;
-      if (c < a.cols) {
-        Pack<float, W> w;
-        if (a.weight) w = *reinterpret_cast<const Pack<float, W>*>(a.weight + c);
+    for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-        for (int k = 0; k < W; ++k) {
-          const float d = to_float(pd[i].v[k]), h = (to_float(px[i].v[k]) - mean) * rstd, g = a.weight ? d * w.v[k] : d;
-          dw[i * W + k] += d * h;
-          db[i * W + k] += d;
-          s[0] += g;
-          s[1] += g * h;
-        }
+      for (int k = 0; k < W; ++k) {
+        const int x = i * W + k;
+        const bool here = in_row<W, WHOLE>((i * TPR + lane) * W, k, a.cols);
+        const float d = here ? to_float(pd[i].v[k]) : 0.f;
+        h[x] = here ? (to_float(px[i].v[k]) - mean) * rstd : 0.f;
+        g[x] = here ? d * w[i].v[k] : 0.f;
+        dw[x] += d * h[x];
+        db[x] += d;
+        s[0] += g[x];
+        s[1] += g[x] * h[x];
       }
-    }
+    load(row + stride);
     if (a.dx) {
       row_sum<TPR, 2>(s, lds[turn]);
       const float mg = s[0] * inv, mgh = s[1] * inv;
       T* dx = static_cast<T*>(a.dx) + row * a.lddx;
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
-        const int c = (i * TPR + lane) * W;
-        if (c < a.cols) {
-          Pack<T, W> out;
-          Pack<float, W> w;
-          if (a.weight) w = *reinterpret_cast<const Pack<float, W>*>(a.weight + c);
+        Pack<T, W> out;
 #pragma unroll
-          for (int k = 0; k < W; ++k) {
-            const float d = to_float(pd[i].v[k]), h = (to_float(px[i].v[k]) - mean) * rstd, g = a.weight ? d * w.v[k] : d;
-            out.v[k] = from_float<T>(rstd * (g - mg - h * mgh));
-          }
-          *reinterpret_cast<Pack<T, W>*>(dx + c) = out;
-        }
+        for (int k = 0; k < W; ++k) out.v[k] = from_float<T>(scale * (g[i * W + k] - mg - h[i * W + k] * mgh));
+        store_piece<T, W, WHOLE>(out, dx, (i * TPR + lane) * W, a.cols);
       }
     }
   }
@@ -191,83 +236,91 @@ __global__ __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) void layer
       float* to = a.partials + ((int64_t)pass * gridDim.x + blockIdx.x) * a.cols;
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
-        const int c = (i * TPR + lane) * W;
-        if (c < a.cols)
+        Pack<float, W> out;
 #pragma unroll
-          for (int k = 0; k < W; ++k) to[c + k] = v[i * W + k];
+        for (int k = 0; k < W; ++k) out.v[k] = v[i * W + k];
+        store_piece<float, W, WHOLE>(out, to, (i * TPR + lane) * W, a.cols);
       }
     }
   }
 }
 
-// dw[c] = sum over the workgroups' partial sums (blockIdx.y = 0), db[c] likewise (1): 16 columns, 16 lanes a column.
-__global__ __launch_bounds__(256) void norm_fold_kernel(const float* partials, int blocks, int cols, float* dweight, float* dbias) {
-  __shared__ float lds[16][17];
+// dw[c] = sum over the workgroups' partial sums (blockIdx.y = 0), db[c] likewise (1): 16 columns, 64 lanes a column.
+constexpr int FOLD_LANES = 64;
+__global__ __launch_bounds__(16 * FOLD_LANES) void norm_fold_kernel(const float* partials, int blocks, int cols, float* dweight, float* dbias) {
+  __shared__ float lds[FOLD_LANES][17], lds8[8][17];
   float* out = blockIdx.y == 0 ? dweight : dbias;
+  if (!out) return;
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
   const float* p = partials + (int64_t)blockIdx.y * blocks * cols;
-  float s = 0.f;
-  if (col < cols)
-    for (int b = r; b < blocks; b += 16) s += p[(int64_t)b * cols + col];
+  float v[NORM_MAX_BLOCKS / FOLD_LANES], s = 0.f;
+#pragma unroll
+  for (int i = 0; i < NORM_MAX_BLOCKS / FOLD_LANES; ++i) v[i] = col < cols && r + i * FOLD_LANES < blocks ? p[(int64_t)(r + i * FOLD_LANES) * cols + col] : 0.f;
+#pragma unroll
+  for (int i = 0; i < NORM_MAX_BLOCKS / FOLD_LANES; ++i) s += v[i];
   lds[r][c] = s;
   __syncthreads();
-  if (out && r == 0 && col < cols) {
-    for (int k = 1; k < 16; ++k) s += lds[k][c];
+  if (r < 8) {
+    s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s += lds[r * 8 + k][c];
+    lds8[r][c] = s;
+  }
+  __syncthreads();
+  if (r == 0 && col < cols) {
+    s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s += lds8[k][c];
     out[col] = s;
   }
 }
 
-// How many lanes share a row and how many loads each makes.
+// How many lanes share a row and how many loads of 16 bytes each makes.
 struct NormShape { int tpr, items; };
 NormShape norm_shape(int cols, int w) {
   const int n = (cols + w - 1) / w;
-  auto items = [&](int tpr) { int i = 1; while (i * tpr < n) i *= 2; return i; };
   if (n <= 16) return {16, 1};
   if (n <= 32) return {32, 1};
-  if (n <= 256) return {64, items(64)};
-  if (n <= 256 * (w == 1 ? 8 : 4)) return {256, items(256)};
-  return {1024, items(1024)};
+  if (n <= 64) return {64, 1};
+  if (n <= 128) return {64, 2};
+  if (n <= 256) return {256, 1};
+  if (n <= 512) return {256, 2};
+  if (n <= 1024) return {512, 2};
+  if (n <= 2048) return {1024, 2};
+  return {1024, 4};
 }
 
 int norm_rows_per_block(int tpr) { return tpr > NORM_THREADS ? 1 : NORM_THREADS / tpr; }
 
-template <typename T, int W, int ITEMS, int TPR>
+template <typename T, int W, int ITEMS, int TPR, bool WHOLE>
 void run_norm(const NormArgs& a, bool backward, int blocks, hipStream_t s) {
-  constexpr int THREADS = TPR > NORM_THREADS ? TPR : NORM_THREADS;
   if (backward)
-    hipLaunchKernelGGL((layer_norm_backward_kernel<T, W, ITEMS, TPR>), dim3(blocks), dim3(THREADS), 0, s, a);
+    hipLaunchKernelGGL((layer_norm_backward_kernel<T, W, ITEMS, TPR, WHOLE>), dim3(blocks), dim3(THREADS_OF<TPR>), 0, s, a);
   else
-    hipLaunchKernelGGL((layer_norm_kernel<T, W, ITEMS, TPR>), dim3(blocks), dim3(THREADS), 0, s, a);
+    hipLaunchKernelGGL((layer_norm_kernel<T, W, ITEMS, TPR, WHOLE>), dim3(blocks), dim3(THREADS_OF<TPR>), 0, s, a);
 }
 
-template <typename T, int W>
-bool dispatch_norm(const NormArgs& a, bool backward, int blocks, hipStream_t s) {
+template <typename T, bool WHOLE>
+void dispatch_norm(const NormArgs& a, bool backward, int blocks, hipStream_t s) {
+  constexpr int W = 16 / (int)sizeof(T);
   const NormShape f = norm_shape(a.cols, W);
   switch (f.tpr * 32 + f.items) {
-    case 16 * 32 + 1: run_norm<T, W, 1, 16>(a, backward, blocks, s); return true;
-    case 32 * 32 + 1: run_norm<T, W, 1, 32>(a, backward, blocks, s); return true;
-    case 64 * 32 + 1: run_norm<T, W, 1, 64>(a, backward, blocks, s); return true;
-    case 64 * 32 + 2: run_norm<T, W, 2, 64>(a, backward, blocks, s); return true;
-    case 64 * 32 + 4: run_norm<T, W, 4, 64>(a, backward, blocks, s); return true;
-    case 256 * 32 + 2: run_norm<T, W, 2, 256>(a, backward, blocks, s); return true;
-    case 256 * 32 + 4: run_norm<T, W, 4, 256>(a, backward, blocks, s); return true;
-    case 1024 * 32 + 2: run_norm<T, W, 2, 1024>(a, backward, blocks, s); return true;
-    case 1024 * 32 + 4: run_norm<T, W, 4, 1024>(a, backward, blocks, s); return true;
-    default: break;
+    case 16 * 32 + 1: run_norm<T, W, 1, 16, WHOLE>(a, backward, blocks, s); break;
+    case 32 * 32 + 1: run_norm<T, W, 1, 32, WHOLE>(a, backward, blocks, s); break;
+    case 64 * 32 + 1: run_norm<T, W, 1, 64, WHOLE>(a, backward, blocks, s); break;
+    case 64 * 32 + 2: run_norm<T, W, 2, 64, WHOLE>(a, backward, blocks, s); break;
+    case 256 * 32 + 1: run_norm<T, W, 1, 256, WHOLE>(a, backward, blocks, s); break;
+    case 256 * 32 + 2: run_norm<T, W, 2, 256, WHOLE>(a, backward, blocks, s); break;
+    case 512 * 32 + 2: run_norm<T, W, 2, 512, WHOLE>(a, backward, blocks, s); break;
+    case 1024 * 32 + 2: run_norm<T, W, 2, 1024, WHOLE>(a, backward, blocks, s); break;
+    default:
+      if constexpr (W == 4) run_norm<T, W, 4, 1024, WHOLE>(a, backward, blocks, s);      // (16384 values are 2048 loads of eight)
+      break;
   }
-  if constexpr (W == 1) {
-    switch (f.tpr * 32 + f.items) {
-      case 256 * 32 + 8: run_norm<T, W, 8, 256>(a, backward, blocks, s); return true;
-      case 1024 * 32 + 8: run_norm<T, W, 8, 1024>(a, backward, blocks, s); return true;
-      case 1024 * 32 + 16: run_norm<T, W, 16, 1024>(a, backward, blocks, s); return true;
-      default: break;
-    }
-  }
-  return false;
 }
 
-// Loads of 16 bytes where every row of every matrix starts at a multiple of them and the columns are whole loads.
-bool norm_wide(const NormArgs& a, int size) {
+// Whether every row of every matrix is a number of whole, aligned loads.
+bool norm_whole(const NormArgs& a, int size) {
   const int w = 16 / size;
   auto fits = [&](const void* p, int64_t ld) { return !p || ((reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % w == 0); };
   return a.cols % w == 0 && fits(a.x, a.ldx) && fits(a.y, a.ldy) && fits(a.dy, a.lddy) && fits(a.dx, a.lddx);
@@ -275,36 +328,36 @@ bool norm_wide(const NormArgs& a, int size) {
 
 }  // namespace
 
-int norm_backward_blocks(int64_t rows) {
-  const int64_t all = (rows + 15) / 16;
-  return (int)(all < 1 ? 1 : all > NORM_MAX_BLOCKS ? NORM_MAX_BLOCKS : all);
+// Workgroups of a backward launch.  Each leaves 2 cols sums behind, which are written and read once more: half as many where rows are long
+// (and a few fill the memory's queues anyway).
+int norm_backward_blocks(int64_t rows, int cols) {
+  const int64_t all = (rows + 15) / 16, most = cols <= 512 ? NORM_MAX_BLOCKS : NORM_MAX_BLOCKS / 2;
+  return (int)(all < 1 ? 1 : all > most ? most : all);
 }
 
 hipError_t launch_layer_norm(const NormArgs& a, int dtype, bool backward, hipStream_t stream) {
   const int size = dtype == RSLX_F32 ? 4 : 2;
-  const bool wide = norm_wide(a, size);
-  const NormShape f = norm_shape(a.cols, wide ? 16 / size : 1);
+  const bool whole = norm_whole(a, size);
+  const NormShape f = norm_shape(a.cols, 16 / size);
   const int per = norm_rows_per_block(f.tpr);
   const double n = (double)a.rows * a.cols;
   if (a.rows > 0 || backward) {
     TraceScope trace(stream, backward ? "layer_norm_backward" : "layer_norm", (backward ? 12 : 8) * n, (backward ? 3 : 2) * n * size);
     const int64_t sets = (a.rows + per - 1) / per;
-    const int blocks = backward ? norm_backward_blocks(a.rows) : (int)(sets < NORM_MAX_FORWARD ? sets : NORM_MAX_FORWARD);
-    bool ok;
+    const int blocks = backward ? norm_backward_blocks(a.rows, a.cols) : (int)(sets < NORM_MAX_FORWARD ? sets : NORM_MAX_FORWARD);
     if (dtype == RSLX_F32)
-      ok = wide ? dispatch_norm<float, 4>(a, backward, blocks, stream) : dispatch_norm<float, 1>(a, backward, blocks, stream);
+      whole ? dispatch_norm<float, true>(a, backward, blocks, stream) : dispatch_norm<float, false>(a, backward, blocks, stream);
     else if (dtype == RSLX_BF16)
-      ok = wide ? dispatch_norm<bf16_t, 8>(a, backward, blocks, stream) : dispatch_norm<bf16_t, 1>(a, backward, blocks, stream);
+      whole ? dispatch_norm<bf16_t, true>(a, backward, blocks, stream) : dispatch_norm<bf16_t, false>(a, backward, blocks, stream);
     else
-      ok = wide ? dispatch_norm<__half, 8>(a, backward, blocks, stream) : dispatch_norm<__half, 1>(a, backward, blocks, stream);
-    if (!ok) return hipErrorInvalidValue;
+      whole ? dispatch_norm<__half, true>(a, backward, blocks, stream) : dispatch_norm<__half, false>(a, backward, blocks, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (backward && a.partials) {
-    const int blocks = norm_backward_blocks(a.rows);
+    const int blocks = norm_backward_blocks(a.rows, a.cols);
     TraceScope trace(stream, "layer_norm_fold", 2.0 * blocks * a.cols, 8.0 * blocks * a.cols);
-    hipLaunchKernelGGL(norm_fold_kernel, dim3((a.cols + 15) / 16, 2), dim3(256), 0, stream, a.partials, blocks, a.cols, a.dweight, a.dbias);
+    hipLaunchKernelGGL(norm_fold_kernel, dim3((a.cols + 15) / 16, 2), dim3(16 * FOLD_LANES), 0, stream, a.partials, blocks, a.cols, a.dweight, a.dbias);
     return hipGetLastError();
   }
   return hipSuccess;

@@ -8,7 +8,7 @@
 namespace rslx {
 
 // ---- layer norm ---------------------------------------------------------------------------------------------------
-constexpr int NORM_MAX_BLOCKS = 512;      // workgroups of a backward launch: each leaves a row of partial sums
+constexpr int NORM_MAX_BLOCKS = 1024;     // workgroups of a backward launch: each leaves a row of partial sums
 
 struct NormArgs {
   const void* x; int64_t ldx;
@@ -27,7 +27,7 @@ struct NormArgs {
   float* dbias;
 };
 
-int norm_backward_blocks(int64_t rows);
+int norm_backward_blocks(int64_t rows, int cols);
 hipError_t launch_layer_norm(const NormArgs& a, int dtype, bool backward, hipStream_t stream);
 
 // ---- linear attention ---------------------------------------------------------------------------------------------
