@@ -18,8 +18,6 @@
 #include "split_bf16.h"
 #include "typed.h"
 
-#include <type_traits>
-
 namespace rslx {
 
 namespace {
@@ -83,24 +81,22 @@ __device__ __forceinline__ int opaque(int x) {
   asm volatile("" : "+v"(x));
   return x;
 }
+__device__ __forceinline__ float opaque(float x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
 
-// N values of a row from offset `at` on (or NOWHERE).  `there`: how many values the row has from there on; WHOLE: enough.  APART: in the order of
-// place().
-template <typename T, int N, int PIECE, bool WHOLE, bool APART = false>
+// N values of a row from offset `at` on (or NOWHERE).  `there`: how many values the row has from there on; WHOLE: enough.
+template <typename T, int N, int PIECE, bool WHOLE>
 __device__ __forceinline__ void load_frag(Frag<T, N>& f, Descriptor d, uint32_t at, int there) {
   constexpr int WORDS = Frag<T, N>::WORDS, PB = PIECE < WORDS * 4 ? PIECE : WORDS * 4, PE = PB / (int)sizeof(T);
 #pragma unroll
   for (int k = 0; k < N / PE; ++k) {
-    const int e = APART ? place<T>(k * PE) : k * PE;
-    const int o = (int)(WHOLE || e < there ? at + (uint32_t)(e * (int)sizeof(T)) : NOWHERE);
+    const int o = (int)(WHOLE || k * PE < there ? at + (uint32_t)(k * PB) : NOWHERE);
     if constexpr (PB == 16) {
       const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(d, o, 0, 0);
 #pragma unroll
       for (int i = 0; i < 4; ++i) f.w[4 * k + i] = x[i];
-    } else if constexpr (PB == 8) {
-      const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(d, o, 0, 0);
-      f.w[2 * k] = x[0];
-      f.w[2 * k + 1] = x[1];
     } else if constexpr (PB == 4) {
       f.w[k] = __builtin_amdgcn_raw_buffer_load_b32(d, o, 0, 0);
     } else {
@@ -109,6 +105,7 @@ __device__ __forceinline__ void load_frag(Frag<T, N>& f, Descriptor d, uint32_t 
     }
   }
 }
+// N values of a row from value e0 on, one by one.  APART: in the order of place().
 template <typename T, int N, bool APART = false>
 __device__ __forceinline__ void load_far(Frag<T, N>& f, const char* row, bool exists, int e0, int width) {
 #pragma unroll
@@ -122,6 +119,72 @@ __device__ __forceinline__ void load_far(Frag<T, N>& f, const char* row, bool ex
       else f.w[k] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[e] << (16 * h);
     }
   }
+}
+
+// A chunk's rows on their way through LDS.  From memory a wavefront takes them as they lie there, LPR lanes of 16 bytes a row; from LDS,
+// where rows are 16 bytes further apart (16 rows then start in 16 different groups of banks), every lane takes what the products want of it.
+template <typename T, int LPR> struct Staged {
+  static constexpr int CHUNK = 16 * BLOCKS<T>, STEP = 64 / LPR, COUNT = CHUNK / STEP, STRIDE = 16 * LPR + 16, BYTES = CHUNK * STRIDE;
+  Frag<T, PE16<T>> f[COUNT];
+  // `from`: offset of this lane's 16 bytes in slot lane / LPR; slots below skip do not exist
+  template <int PIECE, bool WHOLE>
+  __device__ __forceinline__ void load(const Rows<CHUNK>& m, uint32_t from, int lane, int skip, bool exists, int e0, int width) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+      const int slot = lane / LPR + i * STEP;
+      if constexpr (PIECE != 0)
+        load_frag<T, PE16<T>, PIECE, WHOLE>(f[i], descriptor(m.low, exists), slot >= skip ? from + (uint32_t)(i * STEP * (int)m.step) : NOWHERE, width - e0);
+      else load_far<T, PE16<T>>(f[i], m.address(slot), exists && slot >= skip, e0, width);
+    }
+  }
+  __device__ __forceinline__ void store(char* lds, int lane) const {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i)
+      *reinterpret_cast<u32x4*>(lds + (lane / LPR + i * STEP) * STRIDE + lane % LPR * 16) = u32x4{f[i].w[0], f[i].w[1], f[i].w[2], f[i].w[3]};
+  }
+  // Whether any value is infinite or NaN.
+  __device__ __forceinline__ bool not_finite() const {
+    if constexpr (sizeof(T) == 4) {
+      float bad = 0.f;
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) bad = fmaf(f[i].get(k), 0.f, bad);
+      return bad != 0.f;
+    } else {
+      // an exponent of ones carries into the sign's place
+      constexpr uint32_t ONE = __is_same(T, __half) ? 0x04000400u : 0x00800080u;
+      uint32_t bad = 0;
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) bad |= (f[i].w[k] & 0x7fff7fffu) + ONE;
+      return (bad & 0x80008000u) != 0;
+    }
+  }
+};
+// N values from LDS, in the order of place() where APART.
+template <typename T, int N, bool APART>
+__device__ __forceinline__ void take(Frag<T, N>& f, const char* p) {
+  constexpr int WORDS = Frag<T, N>::WORDS;
+  if constexpr (WORDS == 1) f.w[0] = *reinterpret_cast<const uint32_t*>(p);
+  else if constexpr (WORDS == 2) {
+    const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+    f.w[0] = x[0];
+    f.w[1] = x[1];
+  } else {
+#pragma unroll
+    for (int k = 0; k < WORDS / 4; ++k) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(p + k * (APART ? 64 : 16));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f.w[4 * k + i] = x[i];
+    }
+  }
+}
+// What a wavefront's lanes wrote to its own LDS is there for all of them (its LDS accesses are carried out in order; the compiler keeps theirs).
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
 template <typename T, int N, int PIECE, bool WHOLE>
@@ -265,21 +328,20 @@ __device__ __forceinline__ void read_state(f32x4 (&o)[BLOCKS<T>][DVT], const Fra
 #pragma unroll
         for (int t = 0; t < DVT; ++t) o[0][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[0].get(DKT * s + a), S[a][t][s], o[0][t], 0, 0, 0);
   } else {
-    constexpr int WORDS = 2 * DKT;
-    uint32_t x[2][PARTS<T>][WORDS];
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int k = 0; k < 2 * DKT; k += 4) {
+      uint32_t x[2][PARTS<T>][4];
 #pragma unroll
-      for (int k = 0; k < WORDS; ++k) {
-        uint32_t p[PARTS<T>];
-        input_parts<T>(fa[b].w[k], p);
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < PARTS<T>; ++i) x[b][i][k] = p[i];
-      }
+        for (int i = 0; i < 4; ++i) {
+          uint32_t p[PARTS<T>];
+          input_parts<T>(fa[b].w[k + i], p);
 #pragma unroll
-    for (int t = 0; t < DVT; ++t)
+          for (int j = 0; j < PARTS<T>; ++j) x[b][j][i] = p[j];
+        }
 #pragma unroll
-      for (int k = 0; k < WORDS; k += 4) {
+      for (int t = 0; t < DVT; ++t) {
         uint32_t y[2][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -294,8 +356,9 @@ __device__ __forceinline__ void read_state(f32x4 (&o)[BLOCKS<T>][DVT], const Fra
 #pragma unroll
           for (int i = 0; i < PARTS<T>; ++i)
 #pragma unroll
-            for (int j = 0; j < 2 - i; ++j) o[b][t] = mfma_bf16(&x[b][i][k], y[j], o[b][t]);
+            for (int j = 0; j < 2 - i; ++j) o[b][t] = mfma_bf16(x[b][i], y[j], o[b][t]);
       }
+    }
   }
 }
 
@@ -355,7 +418,17 @@ __device__ __forceinline__ void add_state(f32x4 (&S)[DKT][DVT], const Frag<T, DK
       }
     }
   } else {
-    uint32_t x[DKT][PARTS<T>][4], mask[4];
+    uint32_t y[DVT][3][4], mask[4];
+#pragma unroll
+    for (int t = 0; t < DVT; ++t)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int b = k / 2, s = 2 * (k % 2);
+        uint32_t p[3];
+        parts_of<3>(fv[b][s].get(t) * wk[b][s], fv[b][s + 1].get(t) * wk[b][s + 1], p);
+#pragma unroll
+        for (int j = 0; j < 3; ++j) y[t][j][k] = p[j];
+      }
     if (cut) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -365,60 +438,22 @@ __device__ __forceinline__ void add_state(f32x4 (&S)[DKT][DVT], const Frag<T, DK
     }
 #pragma unroll
     for (int a = 0; a < DKT; ++a) {
-      uint32_t v[4];
+      uint32_t v[4], x[PARTS<T>][4];
       column<T, DKT>(fk, a, v);
-      if (cut)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] &= mask[k];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         uint32_t p[PARTS<T>];
-        input_parts<T>(v[k], p);
+        input_parts<T>(cut ? v[k] & mask[k] : v[k], p);
 #pragma unroll
-        for (int i = 0; i < PARTS<T>; ++i) x[a][i][k] = p[i];
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < DVT; ++t) {
-      uint32_t y[3][4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int b = k / 2, s = 2 * (k % 2);
-        uint32_t p[3];
-        parts_of<3>(fv[b][s].get(t) * wk[b][s], fv[b][s + 1].get(t) * wk[b][s + 1], p);
-#pragma unroll
-        for (int j = 0; j < 3; ++j) y[j][k] = p[j];
+        for (int i = 0; i < PARTS<T>; ++i) x[i][k] = p[i];
       }
 #pragma unroll
-      for (int a = 0; a < DKT; ++a)
+      for (int t = 0; t < DVT; ++t)
 #pragma unroll
         for (int i = 0; i < PARTS<T>; ++i)
 #pragma unroll
-          for (int j = 0; j < 3 - i; ++j) S[a][t] = mfma_bf16(x[a][i], y[j], S[a][t]);
+          for (int j = 0; j < 3 - i; ++j) S[a][t] = mfma_bf16(x[i], y[t][j], S[a][t]);
     }
-  }
-}
-
-template <typename T, int DVT>
-__device__ __forceinline__ bool not_finite(const Frag<T, DVT> (&fv)[BLOCKS<T>][4]) {
-  if constexpr (sizeof(T) == 4) {
-    float bad = 0.f;
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int t = 0; t < DVT; ++t) bad = fmaf(fv[0][s].get(t), 0.f, bad);
-    return bad != 0.f;
-  } else {
-    // an exponent of ones carries into the sign's place
-    constexpr uint32_t ONE = __is_same(T, __half) ? 0x04000400u : 0x00800080u;
-    uint32_t bad = 0;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-#pragma unroll
-        for (int k = 0; k < DVT / 2; ++k) bad |= (fv[b][s].w[k] & 0x7fff7fffu) + ONE;
-    return (bad & 0x80008000u) != 0;
   }
 }
 
@@ -455,58 +490,31 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
     O = rows(job.o);
   }
 
-  // The operands of a chunk; each set is asked for again, for the next chunk, as soon as this one's products have read it: by the time it is
-  // needed the other half of a chunk's products has gone by.
-  Frag<T, 4 * DKT> fa[NB], fb[NB];
-  Frag<T, DKT> fk[NB][4];
-  Frag<T, DVT> fv[NB][4];
+  // The rows of a chunk are asked for while the one before it is worked on.
+  using Keys = Staged<T, DKT * (int)sizeof(T)>;
+  using Values = Staged<T, DVT * (int)sizeof(T)>;
+  constexpr int SIZE = (int)sizeof(T), K_LANES = DKT * SIZE, V_LANES = DVT * SIZE, WAVE_BYTES = (STATES ? 1 : 2) * Keys::BYTES + Values::BYTES;
+  __shared__ __attribute__((aligned(16))) char lds[WALK_WAVES * WAVE_BYTES];
+  char* const lds_b = lds + (threadIdx.x >> 6) * WAVE_BYTES;
+  char* const lds_c = lds_b + Keys::BYTES;
+  char* const lds_a = lds_c + Values::BYTES;
+  Keys sa, sb;
+  Values sc;
   uint32_t end = 0;
-  constexpr int SIZE = (int)sizeof(T);
   // row c = 4 (c / 4) + c % 4 of state tile a is index place(DKT (c % 4) + a) + PE (c / 4): the first of this lane's DKT values for the state
   const int d_col = place<T>(DKT * (c & 3)) + PE16<T> * (c >> 2);
-  const uint32_t at_a = A.at(c) + PE16<T> * g * SIZE, at_b = B.at(c) + PE16<T> * g * SIZE, at_k = B.at(4 * g) + d_col * SIZE,
-                 at_v = C.at(4 * g) + e_lane * SIZE, at_o = O.at(4 * g) + e_lane * SIZE;
-  // (at the start: slots below skip do not exist; afterwards all do)
-  auto load_row = [&](auto start, auto& f, const Rows<CHUNK>& m, uint32_t from, bool exists) {
-    constexpr int N = 4 * DKT;
-    const uint32_t from_now = opaque((int)from);
-    const int there = opaque(D - PE16<T> * g);
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const bool in = !start || 16 * b + c >= skip;
-      if constexpr (PIECE != 0) load_frag<T, N, PIECE, WHOLE, true>(f[b], descriptor(m.low, exists), in ? from_now + (uint32_t)(16 * b * (int)m.step) : NOWHERE, there);
-      else load_far<T, N, true>(f[b], m.address(16 * b + c), exists && in, PE16<T> * g, D);
-    }
-  };
-  auto load_update = [&](auto start, bool exists) {
+  const uint32_t at_o = O.at(4 * g) + e_lane * SIZE;
+  auto load = [&](int first_slot, int at, bool exists) {
+    const int k0 = opaque(lane % K_LANES * PE16<T>), v0 = opaque(e_tile + lane % V_LANES * PE16<T>);
     if (w.dones && exists) {
       const int t = rev ? len - 2 - at - lane : at + lane;
       end = w.dones[(int64_t)min(max(t, 0), len - 1) * w.N + n];
     }
-    const uint32_t from_k = opaque((int)at_k), from_v = opaque((int)at_v);
-    const int there_k = opaque(D - d_col), there_v = opaque(E - e_lane);
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const int slot = 16 * b + 4 * g + s;
-        const bool in = !start || slot >= skip;
-        if constexpr (PIECE != 0) {
-          load_frag<T, DVT, PIECE, WHOLE>(fv[b][s], descriptor(C.low, exists), in ? from_v + (uint32_t)((16 * b + s) * (int)C.step) : NOWHERE, there_v);
-          load_frag<T, DKT, PIECE, WHOLE, true>(fk[b][s], descriptor(B.low, exists), in ? from_k + (uint32_t)((16 * b + s) * (int)B.step) : NOWHERE, there_k);
-        } else {
-          load_far<T, DVT>(fv[b][s], C.address(slot), exists && in, e_lane, E);
-          load_far<T, DKT, true>(fk[b][s], B.address(slot), exists && in, d_col, D);
-        }
-      }
+    sb.template load<PIECE, WHOLE>(B, B.at(lane / K_LANES) + k0 * SIZE, lane, first_slot, exists, k0, D);
+    sc.template load<PIECE, WHOLE>(C, C.at(lane / V_LANES) + v0 * SIZE, lane, first_slot, exists, v0, E);
+    if constexpr (!STATES) sa.template load<PIECE, WHOLE>(A, A.at(lane / K_LANES) + k0 * SIZE, lane, first_slot, exists, k0, D);
   };
-  constexpr auto START = std::true_type{};
-  constexpr auto NEXT = std::false_type{};
-  if constexpr (!STATES) {
-    load_row(START, fb, B, at_b, chunks > 0);
-    load_row(START, fa, A, at_a, chunks > 0);
-  }
-  load_update(START, chunks > 0);
+  load(skip, at, chunks > 0);
 
   f32x4 S[DKT][DVT];
 #pragma unroll
@@ -552,19 +560,22 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
     }
   }
 
-  // weights inside a chunk (in a block, and of the second block's positions for the first's), of the state before it, and towards the state behind it
+  // Weights inside a chunk (in a block, and of the second block's positions for the first's), of the state before it, and towards the state
+  // behind it.  A lane's four positions of a block are one apart: where no weight ends on the way, one is kept and the others are made of it.
   const double l2 = log2_decay(w.log_decay[h]);
   const float b_scale = rev ? w.scale : 1.f, o_scale = rev ? 1.f : w.scale;
-  float wp[NB][4], wq[NB][4], wk[NB][4];
+  float step[4], wp[4], wp_next, wq[NB], wk[NB];
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
+  for (int r = 0; r < 4; ++r) {
+    step[r] = __uint_as_float(uniform(__float_as_uint(decay_pow(l2, r))));
+    wp[r] = c >= 4 * g + r ? w.scale * decay_pow(l2, c - 4 * g - r) : 0.f;
+  }
+  wp_next = w.scale * decay_pow(l2, 16 + c - 4 * g - 3);             // (times step[3 - r])
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int i = 16 * b + 4 * g + r, gap = 16 * b + c - 4 * g - r;
-      wp[b][r] = gap >= 0 ? w.scale * decay_pow(l2, gap) : 0.f;
-      wq[b][r] = o_scale * decay_pow(l2, max(i - skip, 0) + lead);
-      wk[b][r] = b_scale * decay_pow(l2, CHUNK - lead - i);
-    }
+  for (int b = 0; b < NB; ++b) {
+    wq[b] = o_scale * decay_pow(l2, 16 * b + 4 * g + lead);          // (times step[r])
+    wk[b] = b_scale * decay_pow(l2, CHUNK - lead - 16 * b - 4 * g - 3);    // (times step[3 - r])
+  }
   // The state is multiplied by the same number once a chunk, and its rounding would add up over a long sequence (3e-8 a chunk): every
   // eighth chunk takes off what eight of them left.
   constexpr int CORRECT = 8;
@@ -580,18 +591,37 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
     const bool more = q + 1 < chunks;
     const int skip_now = skip;
     skip = 0;                             // of the next chunk
+    // A position's weight for an earlier or later one that it has nothing to do with is zero, but zero times infinity is not: from a chunk
+    // on whose C holds anything that is not finite, positions are taken one by one, as the recurrence has them.
+    if (__any(sc.not_finite())) {
+      careful = at + skip_now;
+      break;
+    }
+    // bit i: an episode ends between slots i and i + 1
+    uint32_t cut = 0;
+    if (w.dones) cut = (uint32_t)__ballot(lane < CHUNK && lane >= skip_now && end != 0 && !(rev && at + lane >= len - 1));
+    sb.store(lds_b, lane);
+    sc.store(lds_c, lane);
+    if constexpr (!STATES) sa.store(lds_a, lane);
+    wave_fence();
+    B.move(CHUNK);
+    C.move(CHUNK);
+    if constexpr (!STATES) A.move(CHUNK);
+    load(0, at + CHUNK, more);
     f32x4 o[NB][DVT];
     f32x4 P[NB][NB];                      // [block of j][block of i]
     if constexpr (!STATES) {
+      Frag<T, 4 * DKT> fa[NB];
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
+      for (int b = 0; b < NB; ++b) take<T, 4 * DKT, true>(fa[b], lds_a + (16 * b + c) * Keys::STRIDE + 16 * g);
 #pragma unroll
-        for (int j = 0; j <= i; ++j) P[j][i] = scores<T, DKT>(fb[j], fa[i]);
-      B.move(CHUNK);
-      if constexpr (NB == 1) {
-        __builtin_amdgcn_sched_barrier(0);    // the next chunk's operands take the registers of this one's
-        load_row(NEXT, fb, B, at_b, more);
+      for (int j = 0; j < NB; ++j) {
+        Frag<T, 4 * DKT> fb;
+        take<T, 4 * DKT, true>(fb, lds_b + (16 * j + c) * Keys::STRIDE + 16 * g);
+#pragma unroll
+        for (int i = j; i < NB; ++i) P[j][i] = scores<T, DKT>(fb, fa[i]);
       }
+      __builtin_amdgcn_sched_barrier(0);    // (operands are taken from LDS when they are needed: registers are what is short)
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -601,26 +631,20 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
+          for (int r = 0; r < 4; ++r) {
+            const float x = q == 0 ? o_scale * decay_pow(l2, max(16 * b + 4 * g + r - skip_now, 0) + lead) : opaque(wq[b]) * step[r];
 #pragma unroll
-            for (int t = 0; t < DVT; ++t) o[b][t][r] *= wq[b][r];
+            for (int t = 0; t < DVT; ++t) o[b][t][r] *= x;
+          }
       }
       __builtin_amdgcn_sched_barrier(0);
-      if constexpr (NB == 2) load_row(NEXT, fb, B, at_b, more);      // (not earlier: reading the state needs the registers)
-      A.move(CHUNK);
-      load_row(NEXT, fa, A, at_a, more);
 #pragma unroll
       for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int j = 0; j <= i; ++j)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) P[j][i][r] = j < i || c >= 4 * g + r ? P[j][i][r] * wp[i - j][r] : 0.f;
-    } else {
-      B.move(CHUNK);
+          for (int r = 0; r < 4; ++r) P[j][i][r] = j < i ? P[j][i][r] * (opaque(wp_next) * step[3 - r]) : c >= 4 * g + r ? P[j][i][r] * wp[r] : 0.f;
     }
-    // bit i: an episode ends between slots i and i + 1
-    uint32_t cut = 0;
-    if (w.dones) cut = (uint32_t)__ballot(lane < CHUNK && lane >= skip_now && end != 0 && !(rev && at + lane >= len - 1));
     if constexpr (!STATES) {
       if (cut) {
 #pragma unroll
@@ -637,13 +661,11 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
       }
     }
 
-    // A position's weight for an earlier or later one that it has nothing to do with is zero, but zero times infinity is not: from a chunk
-    // on whose C holds anything that is not finite, positions are taken one by one, as the recurrence has them.
-    if (__any(not_finite<T, DVT>(fv))) {
-      careful = at + skip_now;
-      break;
-    }
-
+    Frag<T, DVT> fv[NB][4];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) take<T, DVT, false>(fv[b][i], lds_c + (16 * b + 4 * g + i) * Values::STRIDE + DVT * c * SIZE);
     if constexpr (!STATES) {
       add_values<T, DVT>(o, P, fv);
       const uint32_t from_o = opaque((int)at_o);
@@ -685,20 +707,22 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
         }
       }
     }
-    add_state<T, DKT, DVT>(S, fk, fv, wk, cut, g);
+    Frag<T, DKT> fk[NB][4];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) take<T, DKT, true>(fk[b][i], lds_b + (16 * b + 4 * g + i) * Keys::STRIDE + d_col * SIZE);
+    float weight[NB][4];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) weight[b][r] = opaque(wk[b]) * step[3 - r];
+    add_state<T, DKT, DVT>(S, fk, fv, weight, cut, g);
     live = true;
-    __builtin_amdgcn_sched_barrier(0);
+    wave_fence();
     at += CHUNK;
-    C.move(CHUNK);
-    load_update(NEXT, more);
     if constexpr (STATES) any_cut |= cut != 0;
-    if (q == 0) {
-      keep = keep_whole;
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) wq[b][r] = o_scale * decay_pow(l2, 16 * b + 4 * g + r + lead);
-    }
+    keep = keep_whole;
   }
 
   if (careful < p1) {
