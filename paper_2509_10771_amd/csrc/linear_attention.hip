@@ -105,42 +105,49 @@ __device__ __forceinline__ void load_frag(Frag<T, N>& f, Descriptor d, uint32_t 
     }
   }
 }
-// N values of a row from value e0 on, one by one.  APART: in the order of place().
+// N values of a row from value e0 on, one by one; zero where not `wanted`.  The row exists.  APART: in the order of place().
 template <typename T, int N, bool APART = false>
-__device__ __forceinline__ void load_far(Frag<T, N>& f, const char* row, bool exists, int e0, int width) {
+__device__ __forceinline__ void load_far(Frag<T, N>& f, const char* row, bool wanted, int e0, int width) {
 #pragma unroll
   for (int k = 0; k < Frag<T, N>::WORDS; ++k) {
     f.w[k] = 0;
 #pragma unroll
     for (int h = 0; h < 4 / (int)sizeof(T); ++h) {
       const int y = k * (4 / (int)sizeof(T)) + h, e = e0 + (APART ? place<T>(y) : y);
-      if (!exists || e >= width) continue;
-      if constexpr (sizeof(T) == 4) f.w[k] = reinterpret_cast<const uint32_t*>(row)[e];
-      else f.w[k] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[e] << (16 * h);
+      const bool here = wanted & (e < width);
+      const int from = here ? e : 0;
+      uint32_t x;
+      if constexpr (sizeof(T) == 4) x = reinterpret_cast<const uint32_t*>(row)[from];
+      else x = (uint32_t)reinterpret_cast<const uint16_t*>(row)[from] << (16 * h);
+      f.w[k] |= here ? x : 0u;
     }
   }
 }
 
 // A chunk's rows on their way through LDS.  From memory a wavefront takes them as they lie there, LPR lanes of 16 bytes a row; from LDS,
 // where rows are 16 bytes further apart (16 rows then start in 16 different groups of banks), every lane takes what the products want of it.
-template <typename T, int LPR> struct Staged {
-  static constexpr int CHUNK = 16 * BLOCKS<T>, STEP = 64 / LPR, COUNT = CHUNK / STEP, STRIDE = 16 * LPR + 16, BYTES = CHUNK * STRIDE;
+// WAVES wavefronts take a part of them each.
+template <typename T, int LPR, int WAVES> struct Staged {
+  static constexpr int CHUNK = 16 * BLOCKS<T>, STEP = 64 / LPR, COUNT = CHUNK / STEP / WAVES, STRIDE = 16 * LPR + 16, BYTES = CHUNK * STRIDE;
   Frag<T, PE16<T>> f[COUNT];
-  // `from`: offset of this lane's 16 bytes in slot lane / LPR; slots below skip do not exist
+  static __device__ __forceinline__ int slot_of(int i, int lane, int wave) { return lane / LPR + (i * WAVES + wave) * STEP; }
+  // The lane's 16 bytes of a row begin at value e0; slots below skip do not exist.
   template <int PIECE, bool WHOLE>
-  __device__ __forceinline__ void load(const Rows<CHUNK>& m, uint32_t from, int lane, int skip, bool exists, int e0, int width) {
+  __device__ __forceinline__ void load(const Rows<CHUNK>& m, int lane, int wave, int skip, bool exists, int e0, int width) {
+    const uint32_t from = m.at(slot_of(0, lane, wave)) + e0 * (int)sizeof(T);
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) {
-      const int slot = lane / LPR + i * STEP;
+      const int slot = slot_of(i, lane, wave);
       if constexpr (PIECE != 0)
-        load_frag<T, PE16<T>, PIECE, WHOLE>(f[i], descriptor(m.low, exists), slot >= skip ? from + (uint32_t)(i * STEP * (int)m.step) : NOWHERE, width - e0);
-      else load_far<T, PE16<T>>(f[i], m.address(slot), exists && slot >= skip, e0, width);
+        load_frag<T, PE16<T>, PIECE, WHOLE>(f[i], descriptor(m.low, exists), slot >= skip ? from + (uint32_t)(i * WAVES * STEP * (int)m.step) : NOWHERE,
+                                            width - e0);
+      else if (exists) load_far<T, PE16<T>>(f[i], m.address(max(slot, skip)), slot >= skip, e0, width);
     }
   }
-  __device__ __forceinline__ void store(char* lds, int lane) const {
+  __device__ __forceinline__ void store(char* lds, int lane, int wave) const {
 #pragma unroll
     for (int i = 0; i < COUNT; ++i)
-      *reinterpret_cast<u32x4*>(lds + (lane / LPR + i * STEP) * STRIDE + lane % LPR * 16) = u32x4{f[i].w[0], f[i].w[1], f[i].w[2], f[i].w[3]};
+      *reinterpret_cast<u32x4*>(lds + slot_of(i, lane, wave) * STRIDE + lane % LPR * 16) = u32x4{f[i].w[0], f[i].w[1], f[i].w[2], f[i].w[3]};
   }
   // Whether any value is infinite or NaN.
   __device__ __forceinline__ bool not_finite() const {
@@ -457,20 +464,26 @@ __device__ __forceinline__ void add_state(f32x4 (&S)[DKT][DVT], const Frag<T, DK
   }
 }
 
-template <typename T, int DKT, int DVT, int PIECE, bool WHOLE, bool STATES>
+// SHARED: the wavefronts of a workgroup are the tiles of one head's columns and take the rows of A and B together: a fourth of the loads and of the
+// registers for them.  LDS then holds two chunks of A and B, so that one barrier a chunk is enough; a wavefront beyond the last column
+// helps with the loads.
+template <typename T, int DKT, int DVT, int PIECE, bool WHOLE, bool STATES, bool SHARED>
 __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_kernel(WalkArgs w, int tiles) {
   constexpr int NB = BLOCKS<T>, CHUNK = 16 * NB;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  int item = uniform((int)blockIdx.x * WALK_WAVES + (int)(threadIdx.x >> 6));
+  const int wave = uniform((int)(threadIdx.x >> 6));
+  int item = SHARED ? (int)blockIdx.x : (int)blockIdx.x * WALK_WAVES + wave;
   const int pieces = STATES ? w.segments - 1 : w.segments;
   const int ji = item % w.jobs; item /= w.jobs;
-  const int tile = item % tiles; item /= tiles;
+  const int tile = SHARED ? wave : item % tiles;
+  if (!SHARED) item /= tiles;
   const int h = item % w.H; item /= w.H;
   const int n = item % w.N, piece = item / w.N;
   if (piece >= pieces) return;
   const WalkJob& job = w.job[ji];
   const int D = job.D, E = job.E, e_tile = tile * 16 * DVT, e_lane = e_tile + DVT * c;
-  if (e_tile >= E) return;
+  const bool idle = e_tile >= E;
+  if (!SHARED && idle) return;
   const bool rev = job.reversed != 0;
   const int lead = rev ? 0 : 1;
   const int len = uniform(sequence_length(w, n));
@@ -491,13 +504,15 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
   }
 
   // The rows of a chunk are asked for while the one before it is worked on.
-  using Keys = Staged<T, DKT * (int)sizeof(T)>;
-  using Values = Staged<T, DVT * (int)sizeof(T)>;
-  constexpr int SIZE = (int)sizeof(T), K_LANES = DKT * SIZE, V_LANES = DVT * SIZE, WAVE_BYTES = (STATES ? 1 : 2) * Keys::BYTES + Values::BYTES;
-  __shared__ __attribute__((aligned(16))) char lds[WALK_WAVES * WAVE_BYTES];
-  char* const lds_b = lds + (threadIdx.x >> 6) * WAVE_BYTES;
-  char* const lds_c = lds_b + Keys::BYTES;
-  char* const lds_a = lds_c + Values::BYTES;
+  constexpr int SIZE = (int)sizeof(T), K_LANES = DKT * SIZE, V_LANES = DVT * SIZE;
+  using Keys = Staged<T, K_LANES, SHARED ? WALK_WAVES : 1>;
+  using Values = Staged<T, V_LANES, 1>;
+  constexpr int KEYS = (STATES ? 1 : 2) * Keys::BYTES;      // of B and A
+  __shared__ __attribute__((aligned(16))) char lds_keys[(SHARED ? 2 : WALK_WAVES) * KEYS], lds_values[WALK_WAVES * Values::BYTES];
+  __shared__ int lds_bad[2][WALK_WAVES];
+  const int k_wave = SHARED ? wave : 0;
+  char* lds_b = lds_keys + (SHARED ? 0 : wave * KEYS);
+  char* const lds_c = lds_values + wave * Values::BYTES;
   Keys sa, sb;
   Values sc;
   uint32_t end = 0;
@@ -510,9 +525,9 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
       const int t = rev ? len - 2 - at - lane : at + lane;
       end = w.dones[(int64_t)min(max(t, 0), len - 1) * w.N + n];
     }
-    sb.template load<PIECE, WHOLE>(B, B.at(lane / K_LANES) + k0 * SIZE, lane, first_slot, exists, k0, D);
-    sc.template load<PIECE, WHOLE>(C, C.at(lane / V_LANES) + v0 * SIZE, lane, first_slot, exists, v0, E);
-    if constexpr (!STATES) sa.template load<PIECE, WHOLE>(A, A.at(lane / K_LANES) + k0 * SIZE, lane, first_slot, exists, k0, D);
+    sb.template load<PIECE, WHOLE>(B, lane, k_wave, first_slot, exists, k0, D);
+    sc.template load<PIECE, WHOLE>(C, lane, 0, first_slot, exists && !idle, v0, E);
+    if constexpr (!STATES) sa.template load<PIECE, WHOLE>(A, lane, k_wave, first_slot, exists, k0, D);
   };
   load(skip, at, chunks > 0);
 
@@ -568,7 +583,10 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     step[r] = __uint_as_float(uniform(__float_as_uint(decay_pow(l2, r))));
-    wp[r] = c >= 4 * g + r ? w.scale * decay_pow(l2, c - 4 * g - r) : 0.f;
+    // (No branch that only some lanes take may enclose work here or in the loop: where registers are short the compiler stores some at such a
+    // branch's end while lanes are still switched off, and gives those lanes stale values back.)
+    const float x = w.scale * decay_pow(l2, max(c - 4 * g - r, 0));
+    wp[r] = c >= 4 * g + r ? x : 0.f;
   }
   wp_next = w.scale * decay_pow(l2, 16 + c - 4 * g - 3);             // (times step[3 - r])
 #pragma unroll
@@ -591,23 +609,38 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
     const bool more = q + 1 < chunks;
     const int skip_now = skip;
     skip = 0;                             // of the next chunk
+    // bit i: an episode ends between slots i and i + 1
+    uint32_t cut = 0;
+    if (w.dones) cut = (uint32_t)__ballot((lane < CHUNK) & (lane >= skip_now) & (end != 0) & !(rev & (at + lane >= len - 1)));
+    bool bad = __any(sc.not_finite());
+    if constexpr (SHARED) lds_b = lds_keys + (q & 1) * KEYS;
+    char* const lds_a = lds_b + Keys::BYTES;
+    sb.store(lds_b, lane, k_wave);
+    sc.store(lds_c, lane, 0);
+    if constexpr (!STATES) sa.store(lds_a, lane, k_wave);
+    if constexpr (SHARED) {
+      if (lane == 0) lds_bad[q & 1][wave] = bad ? 1 : 0;
+      __syncthreads();
+      bad = false;
+#pragma unroll
+      for (int i = 0; i < WALK_WAVES; ++i) bad |= uniform(lds_bad[q & 1][i]) != 0;
+    } else {
+      wave_fence();
+    }
     // A position's weight for an earlier or later one that it has nothing to do with is zero, but zero times infinity is not: from a chunk
     // on whose C holds anything that is not finite, positions are taken one by one, as the recurrence has them.
-    if (__any(sc.not_finite())) {
+    if (bad) {
       careful = at + skip_now;
       break;
     }
-    // bit i: an episode ends between slots i and i + 1
-    uint32_t cut = 0;
-    if (w.dones) cut = (uint32_t)__ballot(lane < CHUNK && lane >= skip_now && end != 0 && !(rev && at + lane >= len - 1));
-    sb.store(lds_b, lane);
-    sc.store(lds_c, lane);
-    if constexpr (!STATES) sa.store(lds_a, lane);
-    wave_fence();
     B.move(CHUNK);
     C.move(CHUNK);
     if constexpr (!STATES) A.move(CHUNK);
     load(0, at + CHUNK, more);
+    if (SHARED && idle) {
+      at += CHUNK;
+      continue;
+    }
     f32x4 o[NB][DVT];
     f32x4 P[NB][NB];                      // [block of j][block of i]
     if constexpr (!STATES) {
@@ -788,6 +821,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
   if constexpr (STATES) {
     if (w.cuts && h == 0 && tile == 0 && lane == 0) w.cuts[((int64_t)ji * w.N + n) * w.segments + piece] = any_cut ? 1 : 0;
   } else {
+    if (SHARED && idle) return;
     // steps that do not exist: zero
     const float zero[DVT] = {};
     const int t0 = max(len, piece * w.seg_len), t1 = piece == w.segments - 1 ? w.T : min((piece + 1) * w.seg_len, w.T);
@@ -912,24 +946,33 @@ __global__ __launch_bounds__(256) void attention_step_kernel(StepArgs a, int LR)
 struct WalkClass { int dkt, dvt; };
 WalkClass walk_class(int D, int E, int size) { return {D <= 32 ? 2 : D <= 64 ? 4 : 8, E <= 32 || (D > 64 && size == 2) ? 2 : 4}; }
 
-template <typename T, int DKT, int DVT, int PIECE, bool WHOLE>
-void run_walk(const WalkArgs& w, int tiles, unsigned blocks, hipStream_t s) {
-  const dim3 grid(blocks), threads(64 * WALK_WAVES);
+template <typename T, int DKT, int DVT, int PIECE, bool WHOLE, bool SHARED = false>
+void run_walk(const WalkArgs& w, int tiles, unsigned items, hipStream_t s) {
+  const dim3 grid(SHARED ? items : (unsigned)(((int64_t)items * tiles + WALK_WAVES - 1) / WALK_WAVES)), threads(64 * WALK_WAVES);
   if (w.states_only)
-    hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, PIECE, WHOLE, true>), grid, threads, 0, s, w, tiles);
+    hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, PIECE, WHOLE, true, SHARED>), grid, threads, 0, s, w, tiles);
   else
-    hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, PIECE, WHOLE, false>), grid, threads, 0, s, w, tiles);
+    hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, PIECE, WHOLE, false, SHARED>), grid, threads, 0, s, w, tiles);
 }
 
 template <typename T, int PIECE, bool WHOLE>
-void dispatch_walk(const WalkArgs& w, WalkClass k, int tiles, unsigned blocks, hipStream_t s) {
+void dispatch_walk(const WalkArgs& w, WalkClass k, int tiles, unsigned items, hipStream_t s) {
   switch (k.dkt * 8 + k.dvt) {
-    case 2 * 8 + 2: run_walk<T, 2, 2, PIECE, WHOLE>(w, tiles, blocks, s); break;
-    case 2 * 8 + 4: run_walk<T, 2, 4, PIECE, WHOLE>(w, tiles, blocks, s); break;
-    case 4 * 8 + 2: run_walk<T, 4, 2, PIECE, WHOLE>(w, tiles, blocks, s); break;
-    case 4 * 8 + 4: run_walk<T, 4, 4, PIECE, WHOLE>(w, tiles, blocks, s); break;
-    case 8 * 8 + 2: run_walk<T, 8, 2, PIECE, WHOLE>(w, tiles, blocks, s); break;
-    default: run_walk<T, 8, 4, PIECE, WHOLE>(w, tiles, blocks, s); break;
+    case 2 * 8 + 2: run_walk<T, 2, 2, PIECE, WHOLE>(w, tiles, items, s); break;
+    case 2 * 8 + 4: run_walk<T, 2, 4, PIECE, WHOLE>(w, tiles, items, s); break;
+    case 4 * 8 + 2: run_walk<T, 4, 2, PIECE, WHOLE>(w, tiles, items, s); break;
+    case 4 * 8 + 4: run_walk<T, 4, 4, PIECE, WHOLE>(w, tiles, items, s); break;
+    case 8 * 8 + 2:
+      if constexpr (sizeof(T) == 2)
+        if (tiles > 2) {
+          run_walk<T, 8, 2, PIECE, WHOLE, true>(w, tiles, items, s);
+          break;
+        }
+      run_walk<T, 8, 2, PIECE, WHOLE>(w, tiles, items, s);
+      break;
+    default:
+      if constexpr (sizeof(T) == 4) run_walk<T, 8, 4, PIECE, WHOLE>(w, tiles, items, s);      // (16-bit types have no such class)
+      break;
   }
 }
 
@@ -960,12 +1003,12 @@ bool walk_whole(const WalkArgs& w, WalkClass k) {
 }
 
 template <typename T>
-void launch_pieces(const WalkArgs& w, WalkClass k, int piece, int tiles, unsigned blocks, hipStream_t s) {
-  if (piece == 16 && walk_whole(w, k)) dispatch_walk<T, 16, true>(w, k, tiles, blocks, s);
-  else if (piece == 16) dispatch_walk<T, 16, false>(w, k, tiles, blocks, s);
-  else if (piece == 4) dispatch_walk<T, 4, false>(w, k, tiles, blocks, s);
-  else if (piece == 0) run_walk<T, 8, 4, 0, false>(w, tiles, blocks, s);       // one class for all widths: rows gigabytes apart are no everyday case
-  else if constexpr (sizeof(T) == 2) dispatch_walk<T, 2, false>(w, k, tiles, blocks, s);
+void launch_pieces(const WalkArgs& w, WalkClass k, int piece, int tiles, unsigned items, hipStream_t s) {
+  if (piece == 16 && walk_whole(w, k)) dispatch_walk<T, 16, true>(w, k, tiles, items, s);
+  else if (piece == 16) dispatch_walk<T, 16, false>(w, k, tiles, items, s);
+  else if (piece == 4) dispatch_walk<T, 4, false>(w, k, tiles, items, s);
+  else if (piece == 0) run_walk<T, 8, 4, 0, false>(w, tiles, items, s);       // one class for all widths: rows gigabytes apart are no everyday case
+  else if constexpr (sizeof(T) == 2) dispatch_walk<T, 2, false>(w, k, tiles, items, s);
 }
 
 }  // namespace
@@ -1016,16 +1059,15 @@ hipError_t launch_walk(const WalkArgs& all, int dtype, hipStream_t stream) {
     const int piece = walk_piece(w, size);
     if (piece == 0)
       for (int i = 0; i < w.jobs; ++i) tiles = max(tiles, (w.job[i].E + 63) / 64);
-    const int64_t waves = (int64_t)(w.states_only ? w.segments - 1 : w.segments) * w.N * w.H * tiles * w.jobs;
-    const int64_t blocks = (waves + WALK_WAVES - 1) / WALK_WAVES;
-    if (blocks > (1 << 23)) return hipErrorInvalidConfiguration;
+    const int64_t items = (int64_t)(w.states_only ? w.segments - 1 : w.segments) * w.N * w.H * w.jobs;
+    if (items * tiles > (int64_t)(1 << 23) * WALK_WAVES || items > (1 << 23) * 2) return hipErrorInvalidConfiguration;
     TraceScope trace(stream, w.states_only ? "linear_attention_states" : "linear_attention_walk", flops, bytes);
     if (dtype == RSLX_F32)
-      launch_pieces<float>(w, k, piece, tiles, (unsigned)blocks, stream);
+      launch_pieces<float>(w, k, piece, tiles, (unsigned)items, stream);
     else if (dtype == RSLX_BF16)
-      launch_pieces<bf16_t>(w, k, piece, tiles, (unsigned)blocks, stream);
+      launch_pieces<bf16_t>(w, k, piece, tiles, (unsigned)items, stream);
     else
-      launch_pieces<__half>(w, k, piece, tiles, (unsigned)blocks, stream);
+      launch_pieces<__half>(w, k, piece, tiles, (unsigned)items, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
