@@ -4,16 +4,22 @@
 //   S_i = l S_{i-1} + b_i c_i^T,   o_i = scale S_i^T a_i,   l = exp(log_decay[h])
 //
 // A chunk of 16 positions is four small products on the fp32 matrix cores: the scores P = A B^T, weighted by l^(i - j) below the diagonal,
-// O = P C + l^(i + 1) A S, and S <- l^16 S + (l^(15 - j) B)^T C.  A wavefront walks one head of one sequence (16 DVT columns of it) by
-// itself: the state stays in its accumulator registers, and because the order of a contraction's indices is free, nothing has to be
+// O = P C + l^(i + 1) A S, and S <- l^16 S + (l^(15 - j) B)^T C.  A wavefront walks one head of one sequence (16 DVT columns of it): the state stays in its accumulator registers, and because the order of a contraction's indices is free, nothing has to be
 // moved between lanes.  With lane = 16 g + c, the instruction v_mfma_f32_16x16x4_f32 leaves in register r row 4 g + r of column c, and
 // reads from an operand row (column) c at index g.  So
 //   - the transposed scores B A^T leave P[c][4 g + r]: the left operand of P C if step s takes the contraction index 4 g + s;
 //   - rows of state tiles are put to indices so that the state's registers are the right operand of A S as they are when lane (c, g) holds
-//     4 DKT values of row c of A, loaded 16 bytes at a time (place() below); and the left operand of the state's update is then, for all
+//     4 DKT values of row c of A, taken 16 bytes at a time (place() below); and the left operand of the state's update is then, for all
 //     tiles, DKT consecutive values of a row of B (two times four for fp32 keys of 128);
 //   - column tile t is put to e = DVT c + t: C is read, and O written, DVT consecutive values of a row at a time.
-// Every operand comes straight from memory in the layout in which it is used: no LDS, no barriers, no shuffles.
+// Rows pass through LDS on their way into those layouts, the next chunk's while this one is worked on: loaded into them straight from memory, 16
+// rows an access, they take four times the cache accesses, and the caches bound the walk (8192 steps of 16 heads of 128 in bf16: 134 us;
+// through LDS 118, with a workgroup's wavefronts sharing the rows of A and B 106, on one card).
+//
+// What bounds it now: a roll-out of 24 steps in fp32 (4096 environments, four heads of 64) memory, 196 us = 4.8 TB/s; long sequences in 16 bits the
+// vector instructions that take the state and the weighted scores apart into bf16 values (some 700 a chunk of 32 beside 100 matrix instructions)
+// and the latency of a chunk's loads at two wavefronts a SIMD, which their registers allow.  Long sequences of few heads are cut into pieces:
+// one launch for every piece's own contribution to the state, one that joins them, one for the outputs.
 #include "sequence.h"
 #include "split_bf16.h"
 #include "typed.h"
@@ -27,7 +33,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // Positions of a chunk: one block of 16, or two where the 16-bit matrix instructions contract over 32.
 template <typename T> constexpr int BLOCKS = sizeof(T) == 2 ? 2 : 1;
 constexpr int MOST_CHUNK = 32;
-constexpr int WALK_WAVES = 4;           // wavefronts per workgroup; they share nothing but the caches
+constexpr int WALK_WAVES = 4;           // wavefronts per workgroup
 
 // N consecutive values as they lie in memory; converted where they are used.
 template <typename T, int N> struct Frag {
@@ -70,8 +76,7 @@ __device__ __forceinline__ Rows<CHUNK> rows_at(const T* first, int64_t step, int
   return {reinterpret_cast<const char*>(first) + (position + (step < 0 ? CHUNK - 1 : 0)) * bytes, bytes};
 }
 
-// Where a lane's N values of a row of keys lie: 16 bytes, then 16 more behind those of the other three groups of lanes, so that an access
-// of a wavefront covers 64 bytes of 16 rows.  Value y of group g is at place(y) + PE g.
+// Where a lane's N values of a row of keys lie: 16 bytes, then 16 more behind those of the other three groups of lanes.  Value y of group g is at place(y) + PE g.
 template <typename T> constexpr int PE16 = 16 / (int)sizeof(T);
 template <typename T> __device__ __forceinline__ constexpr int place(int y) { return 4 * PE16<T> * (y / PE16<T>) + y % PE16<T>; }
 
@@ -873,74 +878,88 @@ __global__ __launch_bounds__(256) void walk_join_kernel(WalkArgs w, JoinStarts s
 }
 
 // ---- one step -----------------------------------------------------------------------------------------------------
-// S <- l S + k v^T, o = scale S^T q: the state is read and written once, W columns a lane, and that is all that costs time.  A
-// wavefront has one head of one row: LR lanes cover a row of the state (or a block of 64 W columns), the other groups take other
-// rows, and their parts of o are added up at the end.
-template <typename T, int W>
+// S <- l S + k v^T, o = scale S^T q: the state is read and written once, four columns a lane, and that is all that costs time.  LR lanes
+// cover a row of the state; the other groups of lanes take other rows, and their parts of o are added up at the end.  A wavefront has one
+// head of one environment; SPLIT: the four of a workgroup take its rows in turn (heads are few, and a state is read in a quarter of the trips).
+// 4096 environments of four heads of 64 x 64: 104 us = 5.2 TB/s.
+template <typename T, bool WHOLE, bool SPLIT>
 __global__ __launch_bounds__(256) void attention_step_kernel(StepArgs a, int LR) {
-  __shared__ float sq[4][128], sk[4][128];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t head = (int64_t)blockIdx.x * 4 + wave, heads = (int64_t)a.N * a.H;
+  constexpr int W = 4, HEADS = SPLIT ? 1 : 4;
+  __shared__ float sq[HEADS][RSLX_ATTN_MAX_DIM], sk[HEADS][RSLX_ATTN_MAX_DIM], so[SPLIT ? 4 : 1][RSLX_ATTN_MAX_DIM];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, own = SPLIT ? 0 : wave;
+  const int64_t head = SPLIT ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave, heads = (int64_t)a.N * a.H;
   const bool here = head < heads;
   const int n = here ? (int)(head / a.H) : 0, h = here ? (int)(head % a.H) : 0;
   if (here) {
     const T* q = static_cast<const T*>(a.q.p) + n * a.q.seq + h * a.q.head;
     const T* k = static_cast<const T*>(a.k.p) + n * a.k.seq + h * a.k.head;
-    for (int d = lane; d < a.Dk; d += 64) {
-      sq[wave][d] = a.scale * to_float(q[d]);
-      sk[wave][d] = to_float(k[d]);
+    for (int d = SPLIT ? (int)threadIdx.x : lane; d < a.Dk; d += SPLIT ? 256 : 64) {
+      sq[own][d] = a.scale * to_float(q[d]);
+      sk[own][d] = to_float(k[d]);
     }
   }
   __syncthreads();
-  if (!here) return;
+  if (!SPLIT && !here) return;
   const T* v = static_cast<const T*>(a.v.p) + n * a.v.seq + h * a.v.head;
   T* o = static_cast<T*>(const_cast<void*>(a.o.p)) + n * a.o.seq + h * a.o.head;
   const float decay = decay_pow(log2_decay(a.log_decay[h]), 1);
   const bool reset = a.reset && a.reset[n] != 0;
-  const float* in = a.s_in ? a.s_in + head * a.Dk * a.Dv : nullptr;
+  const float* in = a.s_in && !reset ? a.s_in + head * a.Dk * a.Dv : nullptr;
   float* out = a.s_out + head * a.Dk * a.Dv;
-  const int groups = 64 / LR, group = lane / LR;
+  const int groups = (SPLIT ? 256 : 64) / LR, group = (SPLIT ? (int)threadIdx.x : lane) / LR;
   constexpr int AHEAD = 8;
-  for (int e0 = 0; e0 < a.Dv; e0 += LR * W) {
-    const int e = e0 + (lane % LR) * W;
-    const bool mine = e < a.Dv;
-    float vv[W], acc[W];
+  const int e = (lane % LR) * W;
+  float vv[W], acc[W];
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-      vv[i] = mine ? to_float(v[e + i]) : 0.f;
-      acc[i] = 0.f;
+  for (int i = 0; i < W; ++i) {
+    vv[i] = e + i < a.Dv ? to_float(v[e + i]) : 0.f;
+    acc[i] = 0.f;
+  }
+  for (int d0 = group; d0 < a.Dk; d0 += groups * AHEAD) {
+    Pack<float, W> s[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+#pragma unroll
+      for (int i = 0; i < W; ++i) s[k].v[i] = 0.f;
+      if (in) load_piece<float, W, WHOLE>(s[k], in + (int64_t)min(d0 + k * groups, a.Dk - 1) * a.Dv, e, a.Dv);
     }
-    if (mine) {
-      for (int d0 = group; d0 < a.Dk; d0 += groups * AHEAD) {
-        Pack<float, W> s[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-          const int d = min(d0 + k * groups, a.Dk - 1);
-          if (in && !reset) s[k] = *reinterpret_cast<const Pack<float, W>*>(in + (int64_t)d * a.Dv + e);
+    for (int k = 0; k < AHEAD; ++k) {
+      const int d = d0 + k * groups;
+      if (d < a.Dk) {
+        const float kk = sk[own][d], qq = sq[own][d];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          s[k].v[i] = fmaf(kk, vv[i], in ? s[k].v[i] * decay : 0.f);
+          acc[i] = fmaf(qq, s[k].v[i], acc[i]);
         }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-          const int d = d0 + k * groups;
-          if (d < a.Dk) {
-            const float kk = sk[wave][d], qq = sq[wave][d];
-#pragma unroll
-            for (int i = 0; i < W; ++i) {
-              const float old = in && !reset ? s[k].v[i] * decay : 0.f;
-              s[k].v[i] = fmaf(kk, vv[i], old);
-              acc[i] = fmaf(qq, s[k].v[i], acc[i]);
-            }
-            *reinterpret_cast<Pack<float, W>*>(out + (int64_t)d * a.Dv + e) = s[k];
-          }
-        }
+        store_piece<float, W, WHOLE>(s[k], out + (int64_t)d * a.Dv, e, a.Dv);
       }
     }
-    for (int x = 32; x >= LR; x >>= 1)
-#pragma unroll
-      for (int i = 0; i < W; ++i) acc[i] += __shfl_xor(acc[i], x, 64);
-    if (mine && group == 0)
-#pragma unroll
-      for (int i = 0; i < W; ++i) o[e + i] = from_float<T>(acc[i]);
   }
+  for (int x = 32; x >= LR; x >>= 1)
+#pragma unroll
+    for (int i = 0; i < W; ++i) acc[i] += __shfl_xor(acc[i], x, 64);
+  if constexpr (SPLIT) {
+    if (lane < LR)
+#pragma unroll
+      for (int i = 0; i < W; ++i) so[wave][e + i] = acc[i];
+    __syncthreads();
+    for (int x = threadIdx.x; x < a.Dv; x += 256) o[x] = from_float<T>((so[0][x] + so[1][x]) + (so[2][x] + so[3][x]));
+  } else if (lane < LR) {
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+      if (e + i < a.Dv) o[e + i] = from_float<T>(acc[i]);
+  }
+}
+
+template <typename T>
+void run_step(const StepArgs& a, bool whole, bool split, unsigned blocks, int LR, hipStream_t s) {
+  const dim3 grid(blocks), threads(256);
+  if (whole && split) hipLaunchKernelGGL((attention_step_kernel<T, true, true>), grid, threads, 0, s, a, LR);
+  else if (whole) hipLaunchKernelGGL((attention_step_kernel<T, true, false>), grid, threads, 0, s, a, LR);
+  else if (split) hipLaunchKernelGGL((attention_step_kernel<T, false, true>), grid, threads, 0, s, a, LR);
+  else hipLaunchKernelGGL((attention_step_kernel<T, false, false>), grid, threads, 0, s, a, LR);
 }
 
 struct WalkClass { int dkt, dvt; };
@@ -1087,25 +1106,20 @@ hipError_t launch_walk_join(const WalkArgs& w, const float* const* starts, hipSt
 }
 
 hipError_t launch_attention_step(const StepArgs& a, int dtype, hipStream_t stream) {
-  const int64_t heads = (int64_t)a.N * a.H, blocks = (heads + 3) / 4;
+  const int64_t heads = (int64_t)a.N * a.H;
+  // A wavefront per head fills the chip from some heads for each CU on; before that a head's rows are split.  560 heads of 128 x 126 16.7 us split,
+  // 2000 of 128 x 64 27.0 (one wavefront each 30.1); 1800 of 64 x 64 12.6 split, 11.6 not.
+  const bool split = heads < (a.Dk > 64 ? 2048 : 1024);
+  const int64_t blocks = split ? heads : (heads + 3) / 4;
   if (blocks > (1 << 23)) return hipErrorInvalidConfiguration;
-  const bool vec = a.Dv % 4 == 0;
-  const int lanes = vec ? a.Dv / 4 : a.Dv;
   int LR = 1;
-  while (LR < lanes && LR < 64) LR *= 2;
+  while (LR * 4 < a.Dv) LR *= 2;
   const double n = (double)heads * a.Dk * a.Dv;
   TraceScope trace(stream, "linear_attention_step", 5 * n, 8 * n);
-  const dim3 grid((unsigned)blocks), threads(256);
-  if (dtype == RSLX_F32) {
-    if (vec) hipLaunchKernelGGL((attention_step_kernel<float, 4>), grid, threads, 0, stream, a, LR);
-    else hipLaunchKernelGGL((attention_step_kernel<float, 1>), grid, threads, 0, stream, a, LR);
-  } else if (dtype == RSLX_BF16) {
-    if (vec) hipLaunchKernelGGL((attention_step_kernel<bf16_t, 4>), grid, threads, 0, stream, a, LR);
-    else hipLaunchKernelGGL((attention_step_kernel<bf16_t, 1>), grid, threads, 0, stream, a, LR);
-  } else {
-    if (vec) hipLaunchKernelGGL((attention_step_kernel<__half, 4>), grid, threads, 0, stream, a, LR);
-    else hipLaunchKernelGGL((attention_step_kernel<__half, 1>), grid, threads, 0, stream, a, LR);
-  }
+  const bool whole = a.Dv % 4 == 0;
+  if (dtype == RSLX_F32) run_step<float>(a, whole, split, (unsigned)blocks, LR, stream);
+  else if (dtype == RSLX_BF16) run_step<bf16_t>(a, whole, split, (unsigned)blocks, LR, stream);
+  else run_step<__half>(a, whole, split, (unsigned)blocks, LR, stream);
   return hipGetLastError();
 }
 

@@ -25,4 +25,31 @@ template <> __device__ __forceinline__ __half from_float<__half>(float x) { retu
 // N consecutive values, moved in accesses of up to 16 bytes.
 template <typename T, int N> struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Pack { T v[N]; };
 
+// W values of a row from column c on; WHOLE: rows are whole, aligned loads.  Otherwise rows start anywhere (the load is as wide, global memory
+// takes any address) and the last one may be shorter: its values come one by one.
+template <typename T, int W, bool WHOLE>
+__device__ __forceinline__ void load_piece(Pack<T, W>& p, const T* row, int c, int cols) {
+  if constexpr (WHOLE) {
+    if (c < cols) p = *reinterpret_cast<const Pack<T, W>*>(row + c);
+  } else if (c + W <= cols) {
+    __builtin_memcpy(&p, row + c, sizeof p);
+  } else {
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k)
+      if (c + k < cols) p.v[k] = row[c + k];
+  }
+}
+template <typename T, int W, bool WHOLE>
+__device__ __forceinline__ void store_piece(const Pack<T, W>& p, T* row, int c, int cols) {
+  if constexpr (WHOLE) {
+    if (c < cols) *reinterpret_cast<Pack<T, W>*>(row + c) = p;
+  } else if (c + W <= cols) {
+    __builtin_memcpy(row + c, &p, sizeof p);
+  } else {
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k)
+      if (c + k < cols) row[c + k] = p.v[k];
+  }
+}
+
 }  // namespace rslx
