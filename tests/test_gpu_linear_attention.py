@@ -122,6 +122,36 @@ def test_what_is_not_finite_stays_where_it_belongs(rx, name, value, T):
         assert np.abs(x[fine] - r[fine]).max(initial=0) <= c.roundings * U * 40 * max(1.0, np.abs(r[fine]).max(initial=0)), what
 
 
+# 16 bits: a wavefront per tile of columns, with the rows of wide keys shared by a workgroup, or by itself
+@pytest.mark.parametrize("T,N,H,Dk,Dv,dtype", [(700, 2, 2, 128, 128, "bf16"), (333, 3, 1, 100, 97, "fp16"), (130, 2, 1, 72, 128, "bf16")])
+def test_wide_heads_in_pieces(rx, T, N, H, Dk, Dv, dtype):
+    c = Attention(T + 1, T, N, H, Dk, Dv, dtype, done_p=0.01, ragged=True)
+    c.check_forward(*c.run_forward(rx))
+    c.check_backward(*c.run_backward(rx))
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "do"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("T,Dk,Dv", [(40, 128, 100), (200, 128, 128), (70, 40, 64)])
+def test_what_is_not_finite_in_16_bits(rx, name, dtype, T, Dk, Dv):
+    c = Attention(T + 2, T, 3, 2, Dk, Dv, dtype, done_p=0.05)
+    for t, n, h, value in ((3, 0, 0, float("inf")), (T // 2, 1, 1, float("nan")), (T - 1, 2, 0, float("-inf"))):
+        getattr(c, name)[t, n, h, 2] = value
+    c.dones[:, 2] = 0
+    c.dones[T // 2 + 5, 1] = 1
+    c.dones[9, 0] = 1
+    more = dict(do=f64(c.do), ds_last=f64(c.ds_last))
+    ref = ola.forward(*c.args(), **c.kw()) + ola.backward(*c.args(), **c.kw(), **more)
+    got = c.run_forward(rx) + c.run_backward(rx)
+    for what, r, x in zip(("o", "s_last", "dq", "dk", "dv", "ds0"), ref, got):
+        x = f64(x)
+        fine = np.isfinite(r)
+        assert np.array_equal(np.isfinite(x), fine), (what, int((np.isfinite(x) != fine).sum()))
+        # the output's own rounding, and the products' (2^-17 of a term at most, and terms of 40 times the largest result in all)
+        size = max(1.0, np.abs(r[fine]).max(initial=0))
+        assert np.abs(x[fine] - r[fine]).max(initial=0) <= (torch.finfo(c.dtype).eps / 2 + 40 * 2.0 ** -17 + c.roundings * U * 40) * size, what
+
+
 def test_two_calls_are_one(rx):
     c = Attention(18, 60, 4, 2, 24, 40, "fp32", done_p=0.05)
     g, la = c.on_gpu(rx)
