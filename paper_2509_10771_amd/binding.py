@@ -578,11 +578,12 @@ class LinearAttn:
                 raise RslxError("LinearAttn: %s has %d values of %s, %d of %s are needed" % (name, t.numel(), t.dtype, n, want))
         self.dtype, self.T, self.N, self.H, self.Dk, self.Dv = dtype, int(T), int(N), int(H), int(Dk), int(Dv)
         self.scale, self.log_decay, self.dones, self.lengths = float(scale), log_decay, dones, lengths
+        self._shapes, self._state = {w: (self.T, self.N, self.H, w) for w in (self.Dk, self.Dv)}, self.N * self.H * self.Dk * self.Dv
         self.c = _CLinearAttn(_DTYPES[dtype], self.T, self.N, self.H, self.Dk, self.Dv, self.scale, _ptr(log_decay), _ptr(dones), _ptr(lengths))
 
     def view(self, name, t, width):
         """t [T, N, H, width] of any strides with its values side by side -> struct rslx_seq_view."""
-        if t.dtype != self.dtype or t.shape != (self.T, self.N, self.H, width):
+        if t.dtype is not self.dtype or t.shape != self._shapes[width]:
             raise RslxError("%s is %s %s, %s %s is needed" % (name, t.dtype, tuple(t.shape), self.dtype, (self.T, self.N, self.H, width)))
         step, seq, head, one = t.stride()
         if one != 1 and width > 1 and t.numel() > 0:
@@ -593,9 +594,10 @@ class LinearAttn:
         """t [N, H, Dk, Dv] float32, contiguous, or None -> address."""
         if t is None:
             return None
-        if t.dtype != torch.float32 or t.numel() != self.N * self.H * self.Dk * self.Dv:
-            raise RslxError("%s has %d values of %s, %d of float32 are needed" % (name, t.numel(), t.dtype, self.N * self.H * self.Dk * self.Dv))
-        return _ptr(t)
+        if t.dtype is not torch.float32 or t.numel() != self._state:
+            raise RslxError("%s has %d values of %s, %d of float32 are needed" % (name, t.numel(), t.dtype, self._state))
+        assert t.is_contiguous(), "rslx needs contiguous tensors"
+        return t.data_ptr()
 
 
 def rslx_linear_attention_workspace_bytes(la):
@@ -637,15 +639,22 @@ def rslx_linear_attention_step(la, q, k, v, reset, s_in, s_out, o):
            "rslx_linear_attention_step")
 
 
-def _rows(name, t, like=None):
-    """A matrix [rows, cols] whose rows may lie apart -> (address, distance)."""
+def _matrix(name, t):
+    """A matrix [rows, cols] -> (type's code, its type, its shape)."""
+    code, shape = _DTYPES.get(t.dtype), t.shape
+    if code is None or len(shape) != 2:
+        raise RslxError("%s is %s %s, a matrix of float32, bfloat16 or float16 is needed" % (name, t.dtype, tuple(shape)))
+    return code, t.dtype, shape
+
+
+def _rows(name, t, dtype, shape):
+    """A matrix of that type and shape, or None, whose rows may lie apart -> (address, distance)."""
     if t is None:
         return None, 0
-    if t.dim() != 2 or t.dtype not in _DTYPES or (like is not None and (t.shape != like.shape or t.dtype != like.dtype)):
-        raise RslxError("%s is %s %s, %s is needed" % (name, t.dtype, tuple(t.shape), "a matrix of float32, bfloat16 or float16" if like is None
-                                                       else "%s %s" % (like.dtype, tuple(like.shape))))
+    if t.dtype is not dtype or t.shape != shape:
+        raise RslxError("%s is %s %s, %s %s is needed" % (name, t.dtype, tuple(t.shape), dtype, tuple(shape)))
     ld, one = t.stride()
-    if one != 1 and t.shape[1] > 1 and t.numel() > 0:
+    if one != 1 and shape[1] > 1 and shape[0] > 0:
         raise RslxError("%s: the values of a row must lie side by side" % name)
     return t.data_ptr(), ld
 
@@ -653,16 +662,18 @@ def _rows(name, t, like=None):
 def _f32(name, t, n):
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.numel() != n:
+    if t.dtype is not torch.float32 or t.numel() != n:
         raise RslxError("%s has %d values of %s, %d of float32 are needed" % (name, t.numel(), t.dtype, n))
-    return _ptr(t)
+    assert t.is_contiguous(), "rslx needs contiguous tensors"
+    return t.data_ptr()
 
 
 def rslx_layer_norm(x, weight, bias, eps, y, mean, rstd):
     """x, y [rows, cols]; weight, bias [cols] and mean, rstd [rows] float32 or None."""
-    rows, cols = x.shape
-    (px, ldx), (py, ldy) = _rows("x", x), _rows("y", y, x)
-    _check(lib.rslx_layer_norm(_DTYPES[x.dtype], px, ldx, rows, cols, _f32("weight", weight, cols), _f32("bias", bias, cols), eps, py, ldy,
+    code, dtype, shape = _matrix("x", x)
+    rows, cols = shape
+    (px, ldx), (py, ldy) = _rows("x", x, dtype, shape), _rows("y", y, dtype, shape)
+    _check(lib.rslx_layer_norm(code, px, ldx, rows, cols, _f32("weight", weight, cols), _f32("bias", bias, cols), eps, py, ldy,
                                _f32("mean", mean, rows), _f32("rstd", rstd, rows), _stream()), "rslx_layer_norm")
 
 
@@ -675,9 +686,10 @@ def rslx_layer_norm_backward_workspace_bytes(rows, cols):
 
 def rslx_layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, ws):
     """dy, x, dx [rows, cols]; mean, rstd [rows] as rslx_layer_norm leaves them; dx, dweight, dbias or None."""
-    rows, cols = x.shape
-    (px, ldx), (pd, lddy), (pg, lddx) = _rows("x", x), _rows("dy", dy, x), _rows("dx", dx, x)
-    _check(lib.rslx_layer_norm_backward(_DTYPES[x.dtype], pd, lddy, px, ldx, rows, cols, _f32("weight", weight, cols), _f32("mean", mean, rows),
+    code, dtype, shape = _matrix("x", x)
+    rows, cols = shape
+    (px, ldx), (pd, lddy), (pg, lddx) = _rows("x", x, dtype, shape), _rows("dy", dy, dtype, shape), _rows("dx", dx, dtype, shape)
+    _check(lib.rslx_layer_norm_backward(code, pd, lddy, px, ldx, rows, cols, _f32("weight", weight, cols), _f32("mean", mean, rows),
                                         _f32("rstd", rstd, rows), pg, lddx, _f32("dweight", dweight, cols), _f32("dbias", dbias, cols), _ptr(ws),
                                         ws.numel() if ws is not None else 0, _stream()), "rslx_layer_norm_backward")
 
