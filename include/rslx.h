@@ -529,8 +529,8 @@ int32_t rslx_linear_attention_step(const rslx_linear_attn* a, const rslx_seq_vie
 /* ---- layer norm ------------------------------------------------------------------------ */
 
 /* Per row:  m = mean x,  r = 1 / sqrt(mean (x - m)^2 + eps),  y = (x - m) r weight + bias.
- * x, y: [rows, cols] of `dtype`, rows ldx and ldy elements apart (y may be x); weight, bias: device fp32 [cols],
- * NULL = 1 and 0.  mean, rstd: device fp32 [rows] or NULL; the backward pass reads them. */
+ * x, y: [rows, cols] of `dtype`, rows ldx and ldy elements apart; y may be x with the same distance, and must not overlap
+ * it otherwise (the columns beside x in one buffer do not).  weight, bias: device fp32 [cols], NULL = 1 and 0.  mean, rstd: device fp32 [rows] or NULL; the backward pass reads them. */
 #define RSLX_NORM_MAX_COLS 16384
 int32_t rslx_layer_norm(int32_t dtype, const void* x, int64_t ldx, int64_t rows, int32_t cols,
                         const float* weight_or_null, const float* bias_or_null, float eps, void* y, int64_t ldy,
@@ -538,7 +538,7 @@ int32_t rslx_layer_norm(int32_t dtype, const void* x, int64_t ldx, int64_t rows,
 
 /* With g = dy weight and h = (x - mean) rstd:  dx = rstd (g - mean(g) - h mean(g h)) per row,
  * dweight = sum over rows of dy h, dbias = sum over rows of dy (device fp32 [cols]; zero where there are no rows).
- * Any of dx, dweight, dbias may be NULL; dx may be dy or x.  The sums are taken in a fixed order: the same inputs give
+ * Any of dx, dweight, dbias may be NULL; dx may be dy or x, with the same distance, and must not overlap them otherwise.  The sums are taken in a fixed order: the same inputs give
  * the same bits.  Without dweight and dbias no workspace is needed. */
 size_t rslx_layer_norm_backward_workspace_bytes(int64_t rows, int32_t cols);
 int32_t rslx_layer_norm_backward(int32_t dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx,

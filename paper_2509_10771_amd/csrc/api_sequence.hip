@@ -1,5 +1,7 @@
 // C ABI of the sequence operators: linear attention with a decay for each head, layer norm.  Argument checks, workspace planning and the
 // order of the launches; the kernels are in linear_attention.hip and layer_norm.hip.
+#include <algorithm>
+
 #include "host.h"
 #include "sequence.h"
 
@@ -40,6 +42,78 @@ int32_t check_view(const rslx_linear_attn& a, const rslx_seq_view* v, int width,
       if (x.count > 1 && (x.stride < 0 ? -x.stride : x.stride) < width)
         return fail(RSLX_ERR_SHAPE, "%s: rows of %s overlap (stride %lld, width %d)", who, name, (long long)x.stride, width);
   }
+  return RSLX_OK;
+}
+
+// Rows of `bytes` bytes each: row (i, j, ..) lies at p + i stride[0] + j stride[1] + .., strides in bytes.
+typedef __int128 wide;                         // (a stride times a count, whatever a caller gives)
+struct RowSet {
+  const void* p;
+  int64_t bytes;
+  wide stride[3];
+  int64_t count[3];
+};
+
+RowSet rows_of(const void* p, int64_t ld, int64_t rows, int64_t cols, int size) { return {p, cols * size, {(wide)ld * size}, {rows, 1, 1}}; }
+
+// Whether some x_i of 0..n_i puts the sum of s_i x_i between lo and hi: terms of the largest s first, each tried where the others can
+// still reach.  Layouts in use leave one or two values to try at each; where it takes too long to tell, the answer is yes.
+struct Term { wide s; wide n; };
+bool reaches(const Term* t, int count, wide lo, wide hi, int& tries) {
+  if (hi < 0) return false;
+  if (lo <= 0) return true;
+  wide reach = 0;
+  for (int i = 1; i < count; ++i) reach += t[i].s * t[i].n;
+  if (count == 0 || lo > reach + t[0].s * t[0].n) return false;
+  const wide first = lo > reach ? (lo - reach + t[0].s - 1) / t[0].s : 0, last = std::min(hi / t[0].s, t[0].n);
+  for (wide x = first; x <= last; ++x)
+    if (--tries < 0 || reaches(t + 1, count - 1, lo - x * t[0].s, hi - x * t[0].s, tries)) return true;
+  return false;
+}
+
+// Whether a row of a and a row of b share a byte.
+bool share_memory(const RowSet& a, const RowSet& b) {
+  struct { wide lo, hi; } range[2];
+  const RowSet* set[2] = {&a, &b};
+  for (int k = 0; k < 2; ++k) {
+    range[k] = {(wide)reinterpret_cast<uintptr_t>(set[k]->p), (wide)reinterpret_cast<uintptr_t>(set[k]->p) + set[k]->bytes};
+    for (int i = 0; i < 3; ++i) {
+      if (set[k]->count[i] < 1) return false;
+      const wide d = set[k]->stride[i] * (set[k]->count[i] - 1);
+      (d < 0 ? range[k].lo : range[k].hi) += d;
+    }
+  }
+  if (range[0].hi <= range[1].lo || range[1].hi <= range[0].lo) return false;
+  // rows meet where address of a's - address of b's is above -(a's width) and below b's; terms that differ in sign alone are one
+  wide lo = (wide)reinterpret_cast<uintptr_t>(b.p) - (wide)reinterpret_cast<uintptr_t>(a.p), hi = lo;
+  lo -= a.bytes - 1;
+  hi += b.bytes - 1;
+  Term t[6];
+  int n = 0;
+  for (int k = 0; k < 2; ++k)
+    for (int i = 0; i < 3; ++i) {
+      wide s = k == 0 ? set[k]->stride[i] : -set[k]->stride[i];
+      const wide most = set[k]->count[i] - 1;
+      if (s == 0 || most == 0) continue;
+      if (s < 0) {                             // x counts down from the most
+        lo -= s * most;
+        hi -= s * most;
+        s = -s;
+      }
+      int j = 0;
+      while (j < n && t[j].s != s) ++j;
+      if (j == n) t[n++] = {s, 0};
+      t[j].n += most;
+    }
+  std::sort(t, t + n, [](const Term& x, const Term& y) { return x.s > y.s; });
+  int tries = 1 << 16;
+  return reaches(t, n, lo, hi, tries);
+}
+
+// A norm's output may be its input, row by row in place; it must not overlap it otherwise (rows are loaded before earlier ones are stored).
+int32_t check_in_place(const RowSet& out, const RowSet& in, const char* who, const char* names) {
+  const bool same = out.p == in.p && (out.count[0] == 1 || out.stride[0] == in.stride[0]);
+  if (!same && share_memory(out, in)) return fail(RSLX_ERR_INVALID_ARG, "%s: %s overlap and are not the same matrix", who, names);
   return RSLX_OK;
 }
 
@@ -243,6 +317,8 @@ int32_t rslx_layer_norm(int32_t dtype, const void* x, int64_t ldx, int64_t rows,
     return fail(RSLX_ERR_INVALID_ARG, "%s: x or y not aligned to its type", who);
   if (rows > 1 && (ldy < 0 ? -ldy : ldy) < cols) return fail(RSLX_ERR_SHAPE, "%s: rows of y overlap (ldy %lld, %d columns)", who, (long long)ldy, cols);
   if (!aligned16(weight_or_null) || !aligned16(bias_or_null)) return fail(RSLX_ERR_INVALID_ARG, "%s: weight or bias not 16-byte aligned", who);
+  const int size = type_size(dtype);
+  RSLX_TRY(check_in_place(rows_of(y, ldy, rows, cols, size), rows_of(x, ldx, rows, cols, size), who, "x and y"));
   NormArgs a;
   memset(&a, 0, sizeof a);
   a.x = x; a.ldx = ldx; a.y = y; a.ldy = ldy;
@@ -275,6 +351,11 @@ int32_t rslx_layer_norm_backward(int32_t dtype, const void* dy, int64_t lddy, co
   if (dx_or_null && rows > 1 && (lddx < 0 ? -lddx : lddx) < cols)
     return fail(RSLX_ERR_SHAPE, "%s: rows of dx overlap (lddx %lld, %d columns)", who, (long long)lddx, cols);
   if (!aligned16(weight_or_null)) return fail(RSLX_ERR_INVALID_ARG, "%s: weight not 16-byte aligned", who);
+  if (dx_or_null && rows > 0) {
+    const RowSet out = rows_of(dx_or_null, lddx, rows, cols, size);
+    RSLX_TRY(check_in_place(out, rows_of(dy, lddy, rows, cols, size), who, "dx and dy"));
+    RSLX_TRY(check_in_place(out, rows_of(x, ldx, rows, cols, size), who, "dx and x"));
+  }
   const bool parameters = dweight_or_null || dbias_or_null;
   if (!parameters && (!dx_or_null || rows == 0)) return RSLX_OK;
   const size_t need = parameters ? rslx_layer_norm_backward_workspace_bytes(rows, cols) : 0;

@@ -1,0 +1,81 @@
+"""Outputs of the sequence operators that share memory with themselves or with inputs are refused on the host, before anything is
+launched; layouts that interleave without sharing any are not."""
+import pytest
+import torch
+
+import paper_2509_10771_amd as rx
+
+
+def _refused(call, match):
+    with pytest.raises(rx.RslxError, match=match):
+        call()
+
+
+def _taken(call):
+    """The arguments are taken: without a GPU the launch fails, and nothing else."""
+    if torch.cuda.is_available():
+        pytest.skip("host tensors are not for a GPU")
+    with pytest.raises(rx.RslxError) as e:
+        call()
+    assert "overlap" not in str(e.value) and "launch" in str(e.value), str(e.value)
+
+
+def _rows(buf, start, ld, rows, cols):
+    return torch.as_strided(buf, (rows, cols), (ld, 1), start)
+
+
+# start and distance of y's rows beside x's (40 rows of 8, 16 apart): every one shares values with another row of x, or with its own from
+# another place
+@pytest.mark.parametrize("start,ld", [(0, 8), (0, 24), (0, 32), (0, 20), (16, 16), (1, 16), (4, 20), (-7, 16), (8, 24), (15, 16)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_with_rows_that_overlap(start, ld, dtype):
+    buf = torch.zeros(4096, dtype=dtype)
+    x, y = _rows(buf, 64, 16, 40, 8), _rows(buf, 64 + start, ld, 40, 8)
+    _refused(lambda: rx.rslx_layer_norm(x, None, None, 1e-5, y, None, None), "x and y overlap")
+    r, other = torch.zeros(40), torch.zeros(40, 8, dtype=dtype)
+    _refused(lambda: rx.rslx_layer_norm_backward(x, other, None, r, r, y, None, None, None), "dx and dy overlap")
+    _refused(lambda: rx.rslx_layer_norm_backward(other, x, None, r, r, y, None, None, None), "dx and x overlap")
+
+
+# the same matrix, columns beside it, rows between its own, buffers of their own
+@pytest.mark.parametrize("start,ld", [(0, 16), (8, 16), (8, 32), (8, 48), (-8, 16), (640, 16), (2000, 9)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_with_rows_that_do_not(start, ld, dtype):
+    buf = torch.zeros(4096, dtype=dtype)
+    x, y = _rows(buf, 64, 16, 40, 8), _rows(buf, 64 + start, ld, 40, 8)
+    _taken(lambda: rx.rslx_layer_norm(x, None, None, 1e-5, y, None, None))
+    r = torch.zeros(40)
+    _taken(lambda: rx.rslx_layer_norm_backward(x, x, None, r, r, y, None, None, None))
+
+
+def test_norm_of_one_row_in_place_at_any_distance():
+    buf = torch.zeros(64)
+    _taken(lambda: rx.rslx_layer_norm(_rows(buf, 0, 16, 1, 8), None, None, 1e-5, _rows(buf, 0, 24, 1, 8), None, None))
+    _refused(lambda: rx.rslx_layer_norm(_rows(buf, 0, 16, 1, 8), None, None, 1e-5, _rows(buf, 4, 24, 1, 8), None, None), "x and y overlap")
+
+
+def test_norm_in_place_of_a_row_for_all():
+    """x one row read for all of y's: y is written where it lies."""
+    buf = torch.zeros(400)
+    _refused(lambda: rx.rslx_layer_norm(buf[:8].expand(40, 8), None, None, 1e-5, _rows(buf, 0, 8, 40, 8), None, None), "x and y overlap")
+    _taken(lambda: rx.rslx_layer_norm(buf[:8].expand(40, 8), None, None, 1e-5, _rows(buf, 8, 8, 40, 8), None, None))
+
+
+def test_norm_against_a_count_of_bytes():
+    """Any two matrices of one buffer: refused where a byte is in both, and they are not the same rows."""
+    import random
+    rng, buf, refused = random.Random(1), torch.zeros(4096), 0
+    for _ in range(600):
+        rows, cols = rng.randint(1, 9), rng.randint(1, 6)
+        ld = [rng.choice([0, cols, cols + 1, 2 * cols, 3 * cols + 1, -cols, -2 * cols, rng.randint(-20, 20)]) for _ in range(2)]
+        if abs(ld[1]) < cols and rows > 1:
+            continue
+        at = [1000, 1000 + rng.choice([0, cols, rng.randint(-40, 40)])]
+        used = [{at[i] + r * ld[i] + c for r in range(rows) for c in range(cols)} for i in range(2)]
+        same = at[0] == at[1] and (rows == 1 or ld[0] == ld[1])
+        code = rx.lib.rslx_layer_norm(0, buf.data_ptr() + 4 * at[0], ld[0], rows, cols, None, None, 1e-5, buf.data_ptr() + 4 * at[1], ld[1], None, None,
+                                      None) if not torch.cuda.is_available() else pytest.skip("host tensors are not for a GPU")
+        want = bool(used[0] & used[1]) and not same
+        assert (code == 1) == want, (rows, cols, ld, at, code)
+        refused += want
+    assert refused > 100
