@@ -32,19 +32,6 @@ int32_t check_attn(const rslx_linear_attn* a, const char* who, bool step) {
   return RSLX_OK;
 }
 
-// A matrix [T, N, H, width] behind a view; written: no two of its elements may be the same memory.
-int32_t check_view(const rslx_linear_attn& a, const rslx_seq_view* v, int width, bool written, const char* who, const char* name) {
-  if (!v || !v->data) return fail(RSLX_ERR_INVALID_ARG, "%s: null %s", who, name);
-  if (reinterpret_cast<uintptr_t>(v->data) % type_size(a.dtype) != 0) return fail(RSLX_ERR_INVALID_ARG, "%s: %s not aligned to its type", who, name);
-  if (written) {
-    const struct { int64_t stride, count; } d[3] = {{v->step, a.T}, {v->seq, a.N}, {v->head, a.H}};
-    for (const auto& x : d)
-      if (x.count > 1 && (x.stride < 0 ? -x.stride : x.stride) < width)
-        return fail(RSLX_ERR_SHAPE, "%s: rows of %s overlap (stride %lld, width %d)", who, name, (long long)x.stride, width);
-  }
-  return RSLX_OK;
-}
-
 // Rows of `bytes` bytes each: row (i, j, ..) lies at p + i stride[0] + j stride[1] + .., strides in bytes.
 typedef __int128 wide;                         // (a stride times a count, whatever a caller gives)
 struct RowSet {
@@ -114,6 +101,55 @@ bool share_memory(const RowSet& a, const RowSet& b) {
 int32_t check_in_place(const RowSet& out, const RowSet& in, const char* who, const char* names) {
   const bool same = out.p == in.p && (out.count[0] == 1 || out.stride[0] == in.stride[0]);
   if (!same && share_memory(out, in)) return fail(RSLX_ERR_INVALID_ARG, "%s: %s overlap and are not the same matrix", who, names);
+  return RSLX_OK;
+}
+
+// Whether two rows of a share a byte.
+bool overlaps_itself(const RowSet& a) {
+  Term t[3];
+  int n = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (a.count[i] < 1) return false;
+    if (a.count[i] > 1) t[n++] = {a.stride[i] < 0 ? -a.stride[i] : a.stride[i], a.count[i] - 1};
+  }
+  std::sort(t, t + n, [](const Term& x, const Term& y) { return x.s > y.s; });
+  // rows inside rows: every distance is longer than what all shorter ones together cover
+  wide covered = a.bytes;
+  bool apart = true;
+  for (int i = n - 1; i >= 0; --i) {
+    apart = apart && t[i].s >= covered;
+    covered += t[i].s * t[i].n;
+  }
+  if (apart) return false;
+  // otherwise two rows whose places differ in dimension i first, upwards: 1 to n there, -n to n in the ones behind it
+  int tries = 1 << 16;
+  for (int i = 0; i < n; ++i) {
+    Term d[3];
+    int m = 0;
+    wide lo = 1 - a.bytes - t[i].s;
+    d[m++] = {t[i].s, t[i].n - 1};
+    for (int j = i + 1; j < n; ++j) {
+      lo += t[j].s * t[j].n;
+      d[m++] = {t[j].s, 2 * t[j].n};
+    }
+    while (m > 0 && d[m - 1].s == 0) --m;
+    if (reaches(d, m, lo, lo + 2 * (a.bytes - 1), tries)) return true;
+  }
+  return false;
+}
+
+RowSet rows_of(const rslx_linear_attn& a, const rslx_seq_view& v, int width) {
+  const int size = type_size(a.dtype);
+  return {v.data, (int64_t)width * size, {(wide)v.step * size, (wide)v.seq * size, (wide)v.head * size}, {a.T, a.N, a.H}};
+}
+
+// A matrix [T, N, H, width] behind a view; written: no two of its elements may be the same memory.
+int32_t check_view(const rslx_linear_attn& a, const rslx_seq_view* v, int width, bool written, const char* who, const char* name) {
+  if (!v || !v->data) return fail(RSLX_ERR_INVALID_ARG, "%s: null %s", who, name);
+  if (reinterpret_cast<uintptr_t>(v->data) % type_size(a.dtype) != 0) return fail(RSLX_ERR_INVALID_ARG, "%s: %s not aligned to its type", who, name);
+  if (written && overlaps_itself(rows_of(a, *v, width)))
+    return fail(RSLX_ERR_SHAPE, "%s: rows of %s overlap (strides %lld, %lld and %lld, width %d)", who, name, (long long)v->step, (long long)v->seq,
+                (long long)v->head, width);
   return RSLX_OK;
 }
 

@@ -79,3 +79,53 @@ def test_norm_against_a_count_of_bytes():
         assert (code == 1) == want, (rows, cols, ld, at, code)
         refused += want
     assert refused > 100
+
+
+def _attn(T, N, H, width, dtype=torch.float32):
+    return rx.LinearAttn(dtype, T, N, H, width, width, torch.zeros(H), 1.0)
+
+
+def _view(data, strides):
+    v = _attn(1, 1, 1, 1).view("x", torch.zeros(1, 1, 1, 1), 1)
+    v.data, v.step, v.seq, v.head = data, *strides
+    return v
+
+
+def _output(la, buf, at, strides):
+    """Status of a forward call whose o lies at `at` with these strides; inputs elsewhere, one row for all."""
+    if torch.cuda.is_available():
+        pytest.skip("host tensors are not for a GPU")
+    x = torch.zeros(la.Dk)
+    same = _view(x.data_ptr(), (0, 0, 0))
+    return rx.lib.rslx_linear_attention(la.c, same, same, same, None, _view(buf.data_ptr() + 4 * at, strides), None, None, 0, None)
+
+
+@pytest.mark.parametrize("strides", [(8, 8, 64), (64, 8, 8), (32, 8, 32), (0, 8, 24), (24, 8, 12), (-8, 8, 64), (24, 8, -24), (1, 24, 300), (30, 15, 8)])
+def test_attention_output_that_overlaps_itself(strides):
+    la, buf = _attn(3, 3, 4, 8), torch.zeros(4096)
+    assert _output(la, buf, 2000, strides) == 2 and b"rows of o overlap" in rx.lib.rslx_last_error()
+
+
+# dense in every order, backwards, and two distances that fall between each other's multiples
+@pytest.mark.parametrize("strides", [(96, 32, 8), (8, 24, 72), (32, 96, 8), (-96, -32, -8), (24, 16, 100), (100, 24, 300)])
+def test_attention_output_that_does_not(strides):
+    la, buf = _attn(2, 2, 4, 8) if strides[0] == 24 else _attn(3, 3, 4, 8), torch.zeros(4096)
+    assert _output(la, buf, 2000, strides) == 4                # no GPU to launch on
+
+
+def test_attention_output_against_a_count_of_bytes():
+    import random
+    rng, buf, refused = random.Random(2), torch.zeros(1 << 14), 0
+    for _ in range(600):
+        T, N, H, width = rng.randint(1, 5), rng.randint(1, 5), rng.randint(1, 5), rng.randint(1, 4)
+        order = rng.sample(range(3), 3)
+        strides, step = [0] * 3, width
+        for i in order:
+            strides[i] = rng.choice([1, 1, 1, -1]) * (step if rng.random() < 0.6 else rng.randint(0, 3 * step))
+            step = max(1, abs(strides[i])) * (T, N, H)[i]
+        rows = [t * strides[0] + n * strides[1] + h * strides[2] for t in range(T) for n in range(N) for h in range(H)]
+        want = len({r + i for r in rows for i in range(width)}) < len(rows) * width
+        la = _attn(T, N, H, width)
+        assert (_output(la, buf, 8192, strides) == 2) == want, (T, N, H, width, strides)
+        refused += want
+    assert 100 < refused < 500
