@@ -499,7 +499,7 @@ typedef struct rslx_linear_attn {
 } rslx_linear_attn;
 
 /* The whole sequence.  q, k: width Dk; v, o: width Dv; s0, s_last: device [N, H, Dk, Dv] or NULL (s_last may be
- * the buffer of s0).  o must not overlap an input.  A few long sequences are walked in pieces side by side, which
+ * the buffer of s0).  Outputs must not overlap inputs or each other otherwise.  A few long sequences are walked in pieces side by side, which
  * takes workspace; otherwise ws may be NULL. */
 size_t rslx_linear_attention_workspace_bytes(const rslx_linear_attn* a);
 int32_t rslx_linear_attention(const rslx_linear_attn* a, const rslx_seq_view* q, const rslx_seq_view* k,
@@ -509,8 +509,8 @@ int32_t rslx_linear_attention(const rslx_linear_attn* a, const rslx_seq_view* q,
 /* Gradients of a loss L through the call above, from those of its outputs, d_o and ds_last (NULL = 0):
  *   dS_t = scale q_t d_o_t^T + keep_t (t + 1 < T ? l dS_{t+1} : ds_last)
  *   dq_t = scale S_t d_o_t,   dk_t = dS_t v_t,   dv_t = dS_t^T k_t,   ds0 = l dS_0 (ds_last where there is no step)
- * Nothing is kept from the forward call: states are walked again.  ds0 (or NULL) must not overlap s0 or ds_last;
- * dq, dk, dv must not overlap an input. */
+ * Nothing is kept from the forward call: states are walked again.  No output (ds0 may be NULL) may
+ * overlap an input or another output. */
 size_t rslx_linear_attention_backward_workspace_bytes(const rslx_linear_attn* a);
 int32_t rslx_linear_attention_backward(const rslx_linear_attn* a, const rslx_seq_view* q, const rslx_seq_view* k,
                                        const rslx_seq_view* v, const float* s0_or_null, const rslx_seq_view* d_o,
@@ -521,7 +521,8 @@ int32_t rslx_linear_attention_backward(const rslx_linear_attn* a, const rslx_seq
 /* One step of every environment, while acting (a->T = 1, dones and lengths NULL; the views' step is not used):
  *   s_out = (reset[n] ? 0 : l s_in) + k v^T,   o = scale s_out^T q
  * reset_or_null (device uint8 [N]) carries the previous step's episode-end flags, as in rslx_act_recurrent;
- * s_in (NULL = 0) and s_out may be one buffer. */
+ * s_in (NULL = 0) and s_out may be one buffer; o may be q, k or v, each row in place of the same head's; nothing else
+ * that is written may overlap what is read or written. */
 int32_t rslx_linear_attention_step(const rslx_linear_attn* a, const rslx_seq_view* q, const rslx_seq_view* k,
                                    const rslx_seq_view* v, const uint8_t* reset_or_null, const float* s_in_or_null,
                                    float* s_out, const rslx_seq_view* o, void* stream);

@@ -164,6 +164,37 @@ bool states_overlap(const rslx_linear_attn& a, const float* x, const float* y) {
   return x && y && p < q + n && q < p + n;
 }
 
+// What a call reads or writes, by name; `p` null: not there.
+struct Named {
+  RowSet rows;
+  const char* name;
+};
+Named named(const rslx_linear_attn& a, const rslx_seq_view* v, int width, const char* name) {
+  return a.T > 0 ? Named{rows_of(a, *v, width), name} : Named{{}, name};
+}
+Named named(const rslx_linear_attn& a, const float* state, const char* name) {
+  return {{state, (int64_t)a.N * a.H * a.Dk * a.Dv * (int64_t)sizeof(float), {}, {1, 1, 1}}, name};
+}
+
+// Outputs (the first of x) must not share memory with inputs or with each other.
+template <int COUNT>
+int32_t check_apart(const Named (&x)[COUNT], int outputs, const char* who) {
+  for (int i = 0; i < outputs; ++i)
+    for (int j = i + 1; j < COUNT; ++j)
+      if (x[i].rows.p && x[j].rows.p && share_memory(x[i].rows, x[j].rows)) return fail(RSLX_ERR_INVALID_ARG, "%s: %s overlaps %s", who, x[i].name, x[j].name);
+  return RSLX_OK;
+}
+
+// Whether an output's row lies where an input's row of the same sequence and head begins, and meets no other.
+bool same_rows(const RowSet& out, const RowSet& in) {
+  if (out.p != in.p) return false;
+  for (int i = 0; i < 3; ++i)
+    if (out.count[i] > 1 && out.stride[i] != in.stride[i]) return false;
+  RowSet wider = out;
+  wider.bytes = std::max(out.bytes, in.bytes);
+  return !overlaps_itself(wider);
+}
+
 WalkMatrix matrix(const rslx_seq_view* v) { return v ? WalkMatrix{v->data, v->step, v->seq, v->head} : WalkMatrix{}; }
 
 WalkArgs walk_args(const rslx_linear_attn& a) {
@@ -248,6 +279,11 @@ int32_t rslx_linear_attention(const rslx_linear_attn* a, const rslx_seq_view* q,
   RSLX_TRY(check_state(s0_or_null, who, "s0"));
   RSLX_TRY(check_state(s_last_or_null, who, "s_last"));
   if (s0_or_null != s_last_or_null && states_overlap(*a, s0_or_null, s_last_or_null)) return fail(RSLX_ERR_INVALID_ARG, "%s: s0 and s_last overlap", who);
+  const Named all[] = {named(*a, o, a->Dv, "o"), named(*a, s_last_or_null, "s_last"), named(*a, q, a->Dk, "q"), named(*a, k, a->Dk, "k"),
+                       named(*a, v, a->Dv, "v")};
+  RSLX_TRY(check_apart(all, 2, who));
+  const Named read[] = {all[0], named(*a, s0_or_null, "s0")};
+  RSLX_TRY(check_apart(read, 1, who));
   AttnPlan p;
   RSLX_TRY(attn_plan(*a, false, ws, ws_bytes, who, p));
   const hipStream_t s = (hipStream_t)stream;
@@ -292,6 +328,10 @@ int32_t rslx_linear_attention_backward(const rslx_linear_attn* a, const rslx_seq
   RSLX_TRY(check_state(ds0_or_null, who, "ds0"));
   if (states_overlap(*a, ds0_or_null, ds_last_or_null) || states_overlap(*a, ds0_or_null, s0_or_null))
     return fail(RSLX_ERR_INVALID_ARG, "%s: ds0 overlaps an input", who);
+  const Named all[] = {named(*a, dq, a->Dk, "dq"), named(*a, dk, a->Dk, "dk"), named(*a, dv, a->Dv, "dv"), named(*a, ds0_or_null, "ds0"),
+                       named(*a, q, a->Dk, "q"), named(*a, k, a->Dk, "k"), named(*a, v, a->Dv, "v"), named(*a, d_o, a->Dv, "do"),
+                       named(*a, s0_or_null, "s0"), named(*a, ds_last_or_null, "ds_last")};
+  RSLX_TRY(check_apart(all, 4, who));
   AttnPlan p;
   RSLX_TRY(attn_plan(*a, true, ws, ws_bytes, who, p));
   const hipStream_t s = (hipStream_t)stream;
@@ -328,6 +368,13 @@ int32_t rslx_linear_attention_step(const rslx_linear_attn* a, const rslx_seq_vie
   RSLX_TRY(check_state(s_in_or_null, who, "s_in"));
   RSLX_TRY(check_state(s_out, who, "s_out"));
   if (s_in_or_null != s_out && states_overlap(*a, s_in_or_null, s_out)) return fail(RSLX_ERR_INVALID_ARG, "%s: s_in and s_out overlap", who);
+  const Named out = named(*a, o, a->Dv, "o"), in[] = {named(*a, q, a->Dk, "q"), named(*a, k, a->Dk, "k"), named(*a, v, a->Dv, "v")};
+  const Named states[] = {named(*a, s_out, "s_out"), out, in[0], in[1], in[2]}, read[] = {out, named(*a, s_in_or_null, "s_in")};
+  RSLX_TRY(check_apart(states, 1, who));
+  RSLX_TRY(check_apart(read, 1, who));
+  for (const Named& x : in)                    // (a head's q, k and v are read before its o is written)
+    if (!same_rows(out.rows, x.rows) && share_memory(out.rows, x.rows))
+      return fail(RSLX_ERR_INVALID_ARG, "%s: o overlaps %s, and not row by row", who, x.name);
   StepArgs t;
   memset(&t, 0, sizeof t);
   t.q = matrix(q); t.k = matrix(k); t.v = matrix(v); t.o = matrix(o);

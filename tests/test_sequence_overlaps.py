@@ -129,3 +129,90 @@ def test_attention_output_against_a_count_of_bytes():
         assert (_output(la, buf, 8192, strides) == 2) == want, (T, N, H, width, strides)
         refused += want
     assert 100 < refused < 500
+
+
+def _forward(at, T=3, N=2, H=4, D=8):
+    """A forward call whose tensors lie at these places of one buffer, the others apart."""
+    la, buf, z = _attn(T, N, H, D), torch.zeros(1 << 14), lambda: torch.zeros(T, N, H, D)  # noqa: E731
+    dense = lambda x: torch.as_strided(buf, (T, N, H, D), (N * H * D, H * D, D, 1), x)  # noqa: E731
+    state = lambda x: None if x is None else buf[x:x + N * H * D * D]  # noqa: E731
+    a = {n: dense(at[n]) if n in at else z() for n in "qkvo"}
+    return lambda: rx.rslx_linear_attention(la, a["q"], a["k"], a["v"], state(at.get("s0")), a["o"], state(at.get("s_last")), None)
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v"])
+@pytest.mark.parametrize("apart", [0, 8, -64, 191, 100])
+def test_attention_output_over_an_input(name, apart):
+    _refused(_forward({name: 4000, "o": 4000 + apart}), "o overlaps " + name)
+
+
+def test_attention_states_over_rows():
+    _refused(_forward(dict(q=4100, s_last=4000)), "s_last overlaps q")
+    _refused(_forward(dict(o=4500, s_last=4000)), "o overlaps s_last")
+    _refused(_forward(dict(o=4500, s0=4000)), "o overlaps s0")
+    _taken(_forward(dict(q=4000, k=4000, v=4000, o=4192, s0=4384, s_last=4384)))      # (a state has 512 values)
+    _taken(_forward(dict(q=4192, k=4180, v=4100, o=4512, s0=4000)))      # inputs may overlap each other
+
+
+def test_attention_output_between_the_rows_of_an_input():
+    la, buf = _attn(5, 2, 3, 8), torch.zeros(4096)
+    side = buf[:5 * 2 * 4 * 24].view(5, 2, 96)                 # q, k, v and o of a step side by side
+    q, k, v, o = (x.unflatten(2, (3, 8)) for x in side.chunk(4, 2))
+    _taken(lambda: rx.rslx_linear_attention(la, q, k, v, None, o, None, None))
+    _refused(lambda: rx.rslx_linear_attention(la, q, k, v, None, k, None, None), "o overlaps k")
+    back = buf[:5 * 2 * 4 * 24].view(2, 5, 96).transpose(0, 1)[..., 72:].unflatten(2, (3, 8))      # the same memory, sequences first
+    _refused(lambda: rx.rslx_linear_attention(la, q, k, back, None, o, None, None), "o overlaps v")
+
+
+def _backward(at, T=3, N=2, H=4, D=8):
+    la, buf, z = _attn(T, N, H, D), torch.zeros(1 << 14), lambda: torch.zeros(T, N, H, D)  # noqa: E731
+    dense = lambda x: torch.as_strided(buf, (T, N, H, D), (N * H * D, H * D, D, 1), x)  # noqa: E731
+    state = lambda x: None if x is None else buf[x:x + N * H * D * D]  # noqa: E731
+    a = {n: dense(at[n]) if n in at else z() for n in ("q", "k", "v", "do", "dq", "dk", "dv")}
+    s = {n: state(at.get(n)) for n in ("s0", "ds_last", "ds0")}
+    return lambda: rx.rslx_linear_attention_backward(la, a["q"], a["k"], a["v"], s["s0"], a["do"], s["ds_last"], a["dq"], a["dk"], a["dv"], s["ds0"], None)
+
+
+@pytest.mark.parametrize("out", ["dq", "dk", "dv"])
+@pytest.mark.parametrize("other", ["q", "k", "v", "do", "s0", "ds_last", "ds0", "dq", "dk", "dv"])
+def test_gradients_over_other_tensors(out, other):
+    if out != other:
+        _refused(_backward({out: 4040, other: 4000}), "overlaps")
+        _taken(_backward({out: 5000, other: 4000}))
+
+
+def _step(o, N=3, H=4, D=8, s_in=None, s_out=None, **inputs):
+    la, z = _attn(1, N, H, D), lambda: torch.zeros(1, N, H, D)  # noqa: E731
+    a = {n: inputs.get(n, z()) for n in "qkv"}
+    s = torch.zeros(N, H, D, D) if s_out is None else s_out
+    return lambda: rx.rslx_linear_attention_step(la, a["q"], a["k"], a["v"], None, s if s_in is None else s_in, s, o)
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v"])
+def test_step_in_place_and_over_other_rows(name):
+    buf = torch.zeros(4096)
+    rows = lambda at, strides: torch.as_strided(buf, (1, 3, 4, 8), (0, *strides, 1), at)  # noqa: E731
+    o = rows(2000, (32, 8))
+    _taken(_step(o, **{name: o}))
+    _taken(_step(o, **{name: rows(2096, (32, 8))}))
+    _refused(_step(o, **{name: rows(2008, (32, 8))}), "o overlaps " + name)
+    _refused(_step(o, **{name: rows(2000, (0, 8))}), "o overlaps " + name)
+    _refused(_step(o, **{name: rows(2000, (8, 24))}), "o overlaps " + name)
+
+
+def test_step_over_states():
+    buf, o = torch.zeros(4096), torch.zeros(1, 3, 4, 8)
+    state = buf[:768]
+    _refused(_step(buf[400:496].view(1, 3, 4, 8), s_out=state), "s_out overlaps o")
+    _refused(_step(o, s_out=state, k=buf[400:496].view(1, 3, 4, 8)), "s_out overlaps k")
+    _refused(_step(buf[400:496].view(1, 3, 4, 8), s_in=state), "o overlaps s_in")
+    _taken(_step(buf[768:864].view(1, 3, 4, 8), s_out=state))
+
+
+def test_step_in_place_of_wider_rows():
+    """Rows of q that reach into the next head's row of o."""
+    buf, la, s = torch.zeros(4096), rx.LinearAttn(torch.float32, 1, 3, 4, 16, 8, torch.zeros(4), 1.0), torch.zeros(3, 4, 16, 8)
+    rows = lambda width, head: torch.as_strided(buf, (1, 3, 4, width), (0, 4 * head, head, 1), 0)  # noqa: E731
+    k, v = torch.zeros(1, 3, 4, 16), torch.zeros(1, 3, 4, 8)
+    _taken(lambda: rx.rslx_linear_attention_step(la, rows(16, 16), k, v, None, s, s, rows(8, 16)))
+    _refused(lambda: rx.rslx_linear_attention_step(la, rows(16, 8), k, v, None, s, s, rows(8, 8)), "o overlaps q")
