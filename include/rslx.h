@@ -488,9 +488,10 @@ typedef struct rslx_seq_view {
  * What is not finite stays where the recurrence above puts it: a step's values reach no earlier step
  * and no other episode. */
 #define RSLX_ATTN_MAX_DIM 128
+#define RSLX_ATTN_MAX_STEPS 2147483583 /* 2^31 - 65 */
 typedef struct rslx_linear_attn {
   int32_t dtype;                 /* RSLX_F32, RSLX_BF16, RSLX_F16: q, k, v, o and their gradients */
-  int32_t T, N, H;
+  int32_t T, N, H;               /* T: 0..RSLX_ATTN_MAX_STEPS */
   int32_t Dk, Dv;                /* 1..RSLX_ATTN_MAX_DIM */
   float scale;
   const float* log_decay;        /* device [H] */

@@ -22,7 +22,7 @@ int32_t check_dtype(int32_t dtype, const char* who) {
 int32_t check_attn(const rslx_linear_attn* a, const char* who, bool step) {
   if (!a) return fail(RSLX_ERR_INVALID_ARG, "%s: null description", who);
   RSLX_TRY(check_dtype(a->dtype, who));
-  if (a->T < 0 || a->N < 0 || a->H < 0) return fail(RSLX_ERR_SHAPE, "%s: T = %d, N = %d, H = %d", who, a->T, a->N, a->H);
+  if (a->T < 0 || a->T > RSLX_ATTN_MAX_STEPS || a->N < 0 || a->H < 0) return fail(RSLX_ERR_SHAPE, "%s: T = %d, N = %d, H = %d", who, a->T, a->N, a->H);
   if (a->Dk < 1 || a->Dk > RSLX_ATTN_MAX_DIM || a->Dv < 1 || a->Dv > RSLX_ATTN_MAX_DIM)
     return fail(RSLX_ERR_SHAPE, "%s: head widths %d and %d, 1 to %d are taken", who, a->Dk, a->Dv, RSLX_ATTN_MAX_DIM);
   if ((int64_t)a->N * a->H > MAX_HEADS) return fail(RSLX_ERR_SHAPE, "%s: N * H = %lld exceeds %lld", who, (long long)a->N * a->H, (long long)MAX_HEADS);
@@ -398,7 +398,7 @@ int32_t rslx_layer_norm(int32_t dtype, const void* x, int64_t ldx, int64_t rows,
   if (!x || !y) return fail(RSLX_ERR_INVALID_ARG, "%s: null x or y", who);
   if (reinterpret_cast<uintptr_t>(x) % type_size(dtype) || reinterpret_cast<uintptr_t>(y) % type_size(dtype))
     return fail(RSLX_ERR_INVALID_ARG, "%s: x or y not aligned to its type", who);
-  if (rows > 1 && (ldy < 0 ? -ldy : ldy) < cols) return fail(RSLX_ERR_SHAPE, "%s: rows of y overlap (ldy %lld, %d columns)", who, (long long)ldy, cols);
+  if (rows > 1 && ldy < cols && ldy > -cols) return fail(RSLX_ERR_SHAPE, "%s: rows of y overlap (ldy %lld, %d columns)", who, (long long)ldy, cols);
   if (!aligned16(weight_or_null) || !aligned16(bias_or_null)) return fail(RSLX_ERR_INVALID_ARG, "%s: weight or bias not 16-byte aligned", who);
   const int size = type_size(dtype);
   RSLX_TRY(check_in_place(rows_of(y, ldy, rows, cols, size), rows_of(x, ldx, rows, cols, size), who, "x and y"));
@@ -431,7 +431,7 @@ int32_t rslx_layer_norm_backward(int32_t dtype, const void* dy, int64_t lddy, co
   const int size = type_size(dtype);
   if (reinterpret_cast<uintptr_t>(dy) % size || reinterpret_cast<uintptr_t>(x) % size || reinterpret_cast<uintptr_t>(dx_or_null) % size)
     return fail(RSLX_ERR_INVALID_ARG, "%s: dy, x or dx not aligned to its type", who);
-  if (dx_or_null && rows > 1 && (lddx < 0 ? -lddx : lddx) < cols)
+  if (dx_or_null && rows > 1 && lddx < cols && lddx > -cols)
     return fail(RSLX_ERR_SHAPE, "%s: rows of dx overlap (lddx %lld, %d columns)", who, (long long)lddx, cols);
   if (!aligned16(weight_or_null)) return fail(RSLX_ERR_INVALID_ARG, "%s: weight not 16-byte aligned", who);
   if (dx_or_null && rows > 0) {

@@ -306,7 +306,7 @@ bool norm_whole(const NormArgs& a, int size) {
 // many, half as many workgroups where they are long; where rows are few, one set each up to a workgroup per CU (595 rows of 6229 in fp32: 22 us
 // both launches, 38 workgroups of 16 rows 41).
 int norm_backward_blocks(int64_t rows, int cols) {
-  const int64_t per = norm_rows_per_block(norm_shape(cols, 4).tpr), sets = (rows + per - 1) / per;
+  const int64_t per = norm_rows_per_block(norm_shape(cols, 4).tpr), sets = rows / per + (rows % per != 0);
   const int64_t most = cols <= 512 ? NORM_MAX_BLOCKS : NORM_MAX_BLOCKS / 2;
   const int64_t many = sets / 4 < most ? sets / 4 : most, few = sets < 256 ? sets : 256;
   const int64_t blocks = many > few ? many : few;
@@ -321,7 +321,7 @@ hipError_t launch_layer_norm(const NormArgs& a, int dtype, bool backward, hipStr
   const double n = (double)a.rows * a.cols;
   if (a.rows > 0 || backward) {
     TraceScope trace(stream, backward ? "layer_norm_backward" : "layer_norm", (backward ? 12 : 8) * n, (backward ? 3 : 2) * n * size);
-    const int64_t sets = (a.rows + per - 1) / per;
+    const int64_t sets = a.rows / per + (a.rows % per != 0);
     const int blocks = backward ? norm_backward_blocks(a.rows, a.cols) : (int)(sets < NORM_MAX_FORWARD ? sets : NORM_MAX_FORWARD);
     if (dtype == RSLX_F32)
       whole ? dispatch_norm<float, true>(a, backward, blocks, stream) : dispatch_norm<float, false>(a, backward, blocks, stream);

@@ -492,7 +492,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
   const bool rev = job.reversed != 0;
   const int lead = rev ? 0 : 1;
   const int len = uniform(sequence_length(w, n));
-  const int p0 = min(piece * w.seg_len, len), p1 = min(p0 + w.seg_len, len);
+  const int p0 = min(piece * w.seg_len, len), p1 = p0 + min(w.seg_len, len - p0);
   // The first chunk is the one that may be short: it fills the last slots, so that the weights towards the state behind a chunk are
   // the same for every chunk.
   const int chunks = (p1 - p0 + CHUNK - 1) / CHUNK;
@@ -1001,9 +1001,9 @@ int walk_piece(const WalkArgs& w, int size) {
   bool near = true;
   auto add = [&](const WalkMatrix& m, int width) {
     if (!m.p) return;
-    bits |= reinterpret_cast<uintptr_t>(m.p) | (uintptr_t)(m.step * size) | (uintptr_t)(m.seq * size) | (uintptr_t)(m.head * size) | (uintptr_t)(width * size);
-    const int64_t step = m.step < 0 ? -m.step : m.step;
-    near = near && step < MAX_OFFSET / (size * MOST_CHUNK);
+    bits |= reinterpret_cast<uintptr_t>(m.p) | (uintptr_t)m.step * size | (uintptr_t)m.seq * size | (uintptr_t)m.head * size | (uintptr_t)width * size;
+    constexpr int64_t MOST = MAX_OFFSET / MOST_CHUNK;
+    near = near && m.step < MOST / size && m.step > -(MOST / size);
   };
   for (int j = 0; j < w.jobs; ++j) {
     add(w.job[j].a, w.job[j].D);
@@ -1037,7 +1037,7 @@ int walk_waves_per_head(int D, int E, int size) {
   return (E + 16 * k.dvt - 1) / (16 * k.dvt);
 }
 
-// Pieces of a long sequence where the sequences' heads are too few to fill the chip.
+// Pieces of a long sequence (of RSLX_ATTN_MAX_STEPS at most: what is rounded up to whole chunks has 32 bits) where the sequences' heads are too few to fill the chip.
 int walk_segments(int64_t waves, int32_t T, int32_t* seg_len) {
   constexpr int64_t TARGET = 2048;        // two wavefronts for each of the 1024 SIMDs
   constexpr int LEAST = 64;
@@ -1045,10 +1045,10 @@ int walk_segments(int64_t waves, int32_t T, int32_t* seg_len) {
   m = m < T / LEAST ? m : T / LEAST;
   m = m < JOIN_MAX ? m : JOIN_MAX;
   if (m <= 1) {
-    *seg_len = T < 1 ? MOST_CHUNK : (T + MOST_CHUNK - 1) / MOST_CHUNK * MOST_CHUNK;
+    *seg_len = T < 1 ? MOST_CHUNK : (T - 1) / MOST_CHUNK * MOST_CHUNK + MOST_CHUNK;
     return 1;
   }
-  const int64_t len = ((T + m - 1) / m + MOST_CHUNK - 1) / MOST_CHUNK * MOST_CHUNK;
+  const int64_t len = ((T + m - 1) / m + MOST_CHUNK - 1) / MOST_CHUNK * MOST_CHUNK;      // (m has 64 bits)
   *seg_len = (int32_t)len;
   return (int)((T + len - 1) / len);
 }
