@@ -20,6 +20,8 @@
 // vector instructions that take the state and the weighted scores apart into bf16 values (some 700 a chunk of 32 beside 100 matrix instructions)
 // and the latency of a chunk's loads at two wavefronts a SIMD, which their registers allow.  Long sequences of few heads are cut into pieces:
 // one launch for every piece's own contribution to the state, one that joins them, one for the outputs.
+#include <algorithm>
+
 #include "sequence.h"
 #include "split_bf16.h"
 #include "typed.h"
@@ -34,6 +36,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <typename T> constexpr int BLOCKS = sizeof(T) == 2 ? 2 : 1;
 constexpr int MOST_CHUNK = 32;
 constexpr int WALK_WAVES = 4;           // wavefronts per workgroup
+constexpr int64_t WALK_MAX_BLOCKS = 1 << 23;      // workgroups of a launch (2^31 threads); more take further launches
 
 // N consecutive values as they lie in memory; converted where they are used.
 template <typename T, int N> struct Frag {
@@ -473,11 +476,12 @@ __device__ __forceinline__ void add_state(f32x4 (&S)[DKT][DVT], const Frag<T, DK
 // registers for them.  LDS then holds two chunks of A and B, so that one barrier a chunk is enough; a wavefront beyond the last column
 // helps with the loads.
 template <typename T, int DKT, int DVT, int PIECE, bool WHOLE, bool STATES, bool SHARED>
-__global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_kernel(WalkArgs w, int tiles) {
+__global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_kernel(WalkArgs w, int tiles, int first_block) {
   constexpr int NB = BLOCKS<T>, CHUNK = 16 * NB;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = uniform((int)(threadIdx.x >> 6));
-  int item = SHARED ? (int)blockIdx.x : (int)blockIdx.x * WALK_WAVES + wave;
+  const int block = first_block + (int)blockIdx.x;
+  int item = SHARED ? block : block * WALK_WAVES + wave;
   const int pieces = STATES ? w.segments - 1 : w.segments;
   const int ji = item % w.jobs; item /= w.jobs;
   const int tile = SHARED ? wave : item % tiles;
@@ -966,16 +970,19 @@ struct WalkClass { int dkt, dvt; };
 WalkClass walk_class(int D, int E, int size) { return {D <= 32 ? 2 : D <= 64 ? 4 : 8, E <= 32 || (D > 64 && size == 2) ? 2 : 4}; }
 
 template <typename T, int DKT, int DVT, int PIECE, bool WHOLE, bool SHARED = false>
-void run_walk(const WalkArgs& w, int tiles, unsigned items, hipStream_t s) {
-  const dim3 grid(SHARED ? items : (unsigned)(((int64_t)items * tiles + WALK_WAVES - 1) / WALK_WAVES)), threads(64 * WALK_WAVES);
-  if (w.states_only)
-    hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, PIECE, WHOLE, true, SHARED>), grid, threads, 0, s, w, tiles);
-  else
-    hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, PIECE, WHOLE, false, SHARED>), grid, threads, 0, s, w, tiles);
+void run_walk(const WalkArgs& w, int tiles, int64_t items, hipStream_t s) {
+  const int64_t blocks = SHARED ? items : (items * tiles + WALK_WAVES - 1) / WALK_WAVES;
+  for (int64_t first = 0; first < blocks; first += WALK_MAX_BLOCKS) {
+    const dim3 grid((unsigned)std::min(blocks - first, WALK_MAX_BLOCKS)), threads(64 * WALK_WAVES);
+    if (w.states_only)
+      hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, PIECE, WHOLE, true, SHARED>), grid, threads, 0, s, w, tiles, (int)first);
+    else
+      hipLaunchKernelGGL((walk_kernel<T, DKT, DVT, PIECE, WHOLE, false, SHARED>), grid, threads, 0, s, w, tiles, (int)first);
+  }
 }
 
 template <typename T, int PIECE, bool WHOLE>
-void dispatch_walk(const WalkArgs& w, WalkClass k, int tiles, unsigned items, hipStream_t s) {
+void dispatch_walk(const WalkArgs& w, WalkClass k, int tiles, int64_t items, hipStream_t s) {
   switch (k.dkt * 8 + k.dvt) {
     case 2 * 8 + 2: run_walk<T, 2, 2, PIECE, WHOLE>(w, tiles, items, s); break;
     case 2 * 8 + 4: run_walk<T, 2, 4, PIECE, WHOLE>(w, tiles, items, s); break;
@@ -1022,7 +1029,7 @@ bool walk_whole(const WalkArgs& w, WalkClass k) {
 }
 
 template <typename T>
-void launch_pieces(const WalkArgs& w, WalkClass k, int piece, int tiles, unsigned items, hipStream_t s) {
+void launch_pieces(const WalkArgs& w, WalkClass k, int piece, int tiles, int64_t items, hipStream_t s) {
   if (piece == 16 && walk_whole(w, k)) dispatch_walk<T, 16, true>(w, k, tiles, items, s);
   else if (piece == 16) dispatch_walk<T, 16, false>(w, k, tiles, items, s);
   else if (piece == 4) dispatch_walk<T, 4, false>(w, k, tiles, items, s);
@@ -1079,14 +1086,13 @@ hipError_t launch_walk(const WalkArgs& all, int dtype, hipStream_t stream) {
     if (piece == 0)
       for (int i = 0; i < w.jobs; ++i) tiles = max(tiles, (w.job[i].E + 63) / 64);
     const int64_t items = (int64_t)(w.states_only ? w.segments - 1 : w.segments) * w.N * w.H * w.jobs;
-    if (items * tiles > (int64_t)(1 << 23) * WALK_WAVES || items > (1 << 23) * 2) return hipErrorInvalidConfiguration;
     TraceScope trace(stream, w.states_only ? "linear_attention_states" : "linear_attention_walk", flops, bytes);
     if (dtype == RSLX_F32)
-      launch_pieces<float>(w, k, piece, tiles, (unsigned)items, stream);
+      launch_pieces<float>(w, k, piece, tiles, items, stream);
     else if (dtype == RSLX_BF16)
-      launch_pieces<bf16_t>(w, k, piece, tiles, (unsigned)items, stream);
+      launch_pieces<bf16_t>(w, k, piece, tiles, items, stream);
     else
-      launch_pieces<__half>(w, k, piece, tiles, (unsigned)items, stream);
+      launch_pieces<__half>(w, k, piece, tiles, items, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -1111,7 +1117,6 @@ hipError_t launch_attention_step(const StepArgs& a, int dtype, hipStream_t strea
   // 2000 of 128 x 64 27.0 (one wavefront each 30.1); 1800 of 64 x 64 12.6 split, 11.6 not.
   const bool split = heads < (a.Dk > 64 ? 2048 : 1024);
   const int64_t blocks = split ? heads : (heads + 3) / 4;
-  if (blocks > (1 << 23)) return hipErrorInvalidConfiguration;
   int LR = 1;
   while (LR * 4 < a.Dv) LR *= 2;
   const double n = (double)heads * a.Dk * a.Dv;
