@@ -566,6 +566,13 @@ def rslx_rnd(target, predictor, obs, N, D, subset_idx, n_subset, running, weight
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
+def _int32(name, n):
+    """The number itself; ctypes would cut what has more than 32 bits off without a word."""
+    if not -1 << 31 <= n < 1 << 31:
+        raise RslxError("%s = %d has more than 32 bits" % (name, n))
+    return int(n)
+
+
 class LinearAttn:
     """Sizes and constants of a linear-attention layer (struct rslx_linear_attn): T steps of N sequences, H heads, keys Dk and values
     Dv wide, in `dtype`; log_decay [H] float32; dones uint8 [T, N] and lengths int32 [N] or None."""
@@ -576,7 +583,8 @@ class LinearAttn:
         for name, t, want, n in (("log_decay", log_decay, torch.float32, H), ("dones", dones, torch.uint8, T * N), ("lengths", lengths, torch.int32, N)):
             if t is not None and (t.dtype != want or t.numel() != n):
                 raise RslxError("LinearAttn: %s has %d values of %s, %d of %s are needed" % (name, t.numel(), t.dtype, n, want))
-        self.dtype, self.T, self.N, self.H, self.Dk, self.Dv = dtype, int(T), int(N), int(H), int(Dk), int(Dv)
+        self.dtype = dtype
+        self.T, self.N, self.H, self.Dk, self.Dv = (_int32(name, n) for name, n in (("T", T), ("N", N), ("H", H), ("Dk", Dk), ("Dv", Dv)))
         self.scale, self.log_decay, self.dones, self.lengths = float(scale), log_decay, dones, lengths
         self._shapes, self._state = {w: (self.T, self.N, self.H, w) for w in (self.Dk, self.Dv)}, self.N * self.H * self.Dk * self.Dv
         self.c = _CLinearAttn(_DTYPES[dtype], self.T, self.N, self.H, self.Dk, self.Dv, self.scale, _ptr(log_decay), _ptr(dones), _ptr(lengths))
@@ -644,6 +652,8 @@ def _matrix(name, t):
     code, shape = _DTYPES.get(t.dtype), t.shape
     if code is None or len(shape) != 2:
         raise RslxError("%s is %s %s, a matrix of float32, bfloat16 or float16 is needed" % (name, t.dtype, tuple(shape)))
+    if shape[1] > NORM_MAX_COLS:                               # (the C call's number of columns has 32 bits)
+        raise RslxError("%s has %d columns, 1 to %d columns are taken" % (name, shape[1], NORM_MAX_COLS))
     return code, t.dtype, shape
 
 
@@ -678,7 +688,7 @@ def rslx_layer_norm(x, weight, bias, eps, y, mean, rstd):
 
 
 def rslx_layer_norm_backward_workspace_bytes(rows, cols):
-    n = lib.rslx_layer_norm_backward_workspace_bytes(rows, cols)
+    n = lib.rslx_layer_norm_backward_workspace_bytes(rows, _int32("cols", cols))
     if n == 0:
         raise RslxError("rslx_layer_norm_backward_workspace_bytes: %s" % lib.rslx_last_error().decode())
     return n

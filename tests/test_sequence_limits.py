@@ -60,3 +60,22 @@ def test_heads_whose_rows_a_workgroup_shares():
     # the output's rounding; a score of 72 products, in two bf16 parts
     assert ((o[:, :1].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + (2.0 ** -16 + 80 * 2.0 ** -24) * size).all()
     assert torch.equal(o, o[:, :1].expand_as(o))
+
+
+@pytest.mark.parametrize("name", ["T", "N", "H", "Dk", "Dv"])
+def test_sizes_of_more_than_32_bits(name):
+    sizes = dict(T=3, N=2, H=2, Dk=4, Dv=8)
+    sizes[name] += 1 << 32
+    with pytest.raises(rx.RslxError, match=name + " = .* more than 32 bits"):
+        rx.LinearAttn(torch.float32, log_decay=torch.zeros(1).expand(sizes["H"]), **sizes)
+
+
+def test_columns_of_more_than_32_bits():
+    x = torch.empty(2, (1 << 32) + 8, device="meta")           # (no memory behind it)
+    r = torch.zeros(2)
+    with pytest.raises(rx.RslxError, match="columns are taken"):
+        rx.rslx_layer_norm(x, None, None, 1e-5, x, None, None)
+    with pytest.raises(rx.RslxError, match="columns are taken"):
+        rx.rslx_layer_norm_backward(x, x, None, r, r, x, None, None, None)
+    with pytest.raises(rx.RslxError, match="more than 32 bits"):
+        rx.rslx_layer_norm_backward_workspace_bytes(2, (1 << 32) + 8)
