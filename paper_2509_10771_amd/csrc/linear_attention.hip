@@ -603,13 +603,17 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
     wq[b] = o_scale * decay_pow(l2, 16 * b + 4 * g + lead);          // (times step[r])
     wk[b] = b_scale * decay_pow(l2, CHUNK - lead - 16 * b - 4 * g - 3);    // (times step[3 - r])
   }
-  // The state is multiplied by the same number once a chunk, and its rounding would add up over a long sequence (3e-8 a chunk): every
-  // eighth chunk takes off what eight of them left.
-  constexpr int CORRECT = 8;
+  // The state is multiplied by l^CHUNK once a chunk.  Rounded to one float, that would err the same way every time (up to 6e-8 a chunk); so it
+  // is one of the two floats beside the number, the upper one as often as the number lies towards it: the product of any chunks in a row
+  // is off by one step of fp32 at most, however many they are.
   const double chunk_decay = exp2(l2 * CHUNK);
+  const float nearest = (float)chunk_decay;
+  const bool between = nearest < 1e30f;
+  const uint32_t keep_low = uniform(__float_as_uint(nearest) - ((between & ((double)nearest > chunk_decay)) ? 1 : 0));
+  const double below = __uint_as_float(keep_low), above = __uint_as_float(keep_low + 1);
+  const uint32_t keep_rise = uniform(between ? (uint32_t)fmin((chunk_decay - below) / (above - below) * 0x1p32, 0x1p32 - 1) : 0u);
+  uint32_t keep_turn = 0x80000000u;
   float keep = decay_pow(l2, CHUNK - skip);
-  const float keep_whole = (float)chunk_decay;
-  const float off = keep_whole > 0.f && keep_whole < 1e30f ? (float)(CORRECT * (chunk_decay / (double)keep_whole - 1.0)) : 0.f;
 
   const bool wants_state = STATES || (job.s_out != nullptr && piece == w.segments - 1);
   bool any_cut = false;
@@ -739,14 +743,6 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
           for (int t = 0; t < DVT; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) S[a][t][r] *= keep;
-        if (q % CORRECT == CORRECT - 1) {
-#pragma unroll
-          for (int a = 0; a < DKT; ++a)
-#pragma unroll
-            for (int t = 0; t < DVT; ++t)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) S[a][t][r] = fmaf(S[a][t][r], off, S[a][t][r]);
-        }
       }
     }
     Frag<T, DKT> fk[NB][4];
@@ -764,7 +760,8 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
     wave_fence();
     at += CHUNK;
     if constexpr (STATES) any_cut |= cut != 0;
-    keep = keep_whole;
+    keep_turn += keep_rise;               // (a carry out of 32 bits: the upper one)
+    keep = __uint_as_float(keep_low + (keep_turn < keep_rise ? 1u : 0u));
   }
 
   if (careful < p1) {
