@@ -842,18 +842,21 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
   }
 }
 
-// One thread per element of a head's state: slot 0 takes the start, then every slot what it adds to the decayed one before it.
+// One thread per element of a head's state: slot 0 takes the start, then every slot what it adds to the decayed one before it.  A piece's decay
+// is two floats, so that its rounding does not add up over hundreds of pieces (a state that is not finite needs no second one).
 constexpr int JOIN_MAX = 512;
 struct JoinStarts { const float* start[WALK_MAX_JOBS]; };
 __global__ __launch_bounds__(256) void walk_join_kernel(WalkArgs w, JoinStarts starts) {
-  __shared__ float f[JOIN_MAX];
+  __shared__ float f[JOIN_MAX], f_rest[JOIN_MAX];
   __shared__ int cut[JOIN_MAX];
   const int ji = blockIdx.z, n = blockIdx.x / w.H, h = blockIdx.x % w.H;
   const WalkJob& job = w.job[ji];
   const int len = sequence_length(w, n);
   const double l2 = log2_decay(w.log_decay[h]);
   for (int m = threadIdx.x; m < w.segments - 1; m += 256) {
-    f[m] = decay_pow(l2, min(max(len - m * w.seg_len, 0), w.seg_len));
+    const double decay = exp2(l2 * (double)min(max(len - m * w.seg_len, 0), w.seg_len));
+    f[m] = (float)decay;
+    f_rest[m] = f[m] < 1e30f ? (float)(decay - (double)f[m]) : 0.f;
     cut[m] = w.cuts[((int64_t)ji * w.N + n) * w.segments + m];
   }
   __syncthreads();
@@ -872,7 +875,8 @@ __global__ __launch_bounds__(256) void walk_join_kernel(WalkArgs w, JoinStarts s
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       if (m0 + k >= w.segments - 1) break;
-      run = cut[m0 + k] ? x[k] : fmaf(run, f[m0 + k], x[k]);
+      const float finite = fabsf(run) < 3.4e38f ? run : 0.f;
+      run = cut[m0 + k] ? x[k] : fmaf(run, f[m0 + k], fmaf(finite, f_rest[m0 + k], x[k]));
       slot[(int64_t)(m0 + k + 1) * size] = run;
     }
   }

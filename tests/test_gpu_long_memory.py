@@ -70,3 +70,23 @@ def test_a_long_sum_is_not_cut_off_in_one_direction(rx, dtype):
     off, size = f64(s[0, 0]) - ref, np.sqrt((ref ** 2).mean())
     assert np.sqrt((off ** 2).mean()) <= np.sqrt(T) * U * size, np.sqrt((off ** 2).mean()) / size
     assert abs(off.mean()) <= 5 * np.sqrt(T) * U / D * size, off.mean() / size
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_a_state_through_many_pieces(rx, dtype):
+    """A start state alone through one long sequence, which is walked in pieces of 96 steps (at least 64: one rounding each), and the
+    last piece's chunks (at most eight, two steps of fp32 for their decays).  Roundings are independent: the root of their number."""
+    T, D = 38400, 64
+    tries = np.float32(-np.linspace(1e-5, 2e-4, 20001))
+    f = np.exp(96 * tries.astype(np.float64))
+    # pieces' decays that lie in the middle between two floats
+    worst = tries[np.argsort(np.abs(f.astype(np.float32).astype(np.float64) - f) / f)[-4:]]
+    zero = torch.zeros(T, 1, 1, D, dtype=TYPES[dtype], device="cuda")
+    s0 = typed(np.random.default_rng(6).normal(size=(1, 1, D, D)), torch.float32)
+    for ld in worst:
+        log_decay = typed(np.array([ld]), torch.float32)
+        s, pieces = _last_state(rx, TYPES[dtype], zero, zero, zero, log_decay, s0.cuda())
+        assert pieces
+        ref = f64(s0) * np.exp(T * f64(log_decay)[0])
+        off = np.linalg.norm(f64(s) - ref) / np.linalg.norm(ref)
+        assert off <= (np.sqrt(T / 64) + 4 + 8) * U, off / U
