@@ -614,6 +614,17 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
   const uint32_t keep_rise = uniform(between ? (uint32_t)fmin((chunk_decay - below) / (above - below) * 0x1p32, 0x1p32 - 1) : 0u);
   uint32_t keep_turn = 0x80000000u;
   float keep = decay_pow(l2, CHUNK - skip);
+  // The bf16 matrix instructions cut what they add off downwards (see split_bf16.h), which would add up over the chunks of a long memory (a
+  // state of 20 000 steps came out low by 2e-7 of its rms in bf16, 6e-7 in fp16): the state changes its sign with every chunk.
+  constexpr bool TURNS = sizeof(T) == 2;
+  // (Pieces' own states, which start at zero, end with their own sign.)
+  uint32_t sign = TURNS && STATES && chunks % 2 ? 0x80000000u : 0u;      // of the state before the chunk
+  if constexpr (TURNS) {
+    keep = -keep;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) wk[b] = -wk[b];
+  }
+  auto turned = [&](float x) { return TURNS ? __uint_as_float(__float_as_uint(x) ^ sign) : x; };
 
   const bool wants_state = STATES || (job.s_out != nullptr && piece == w.segments - 1);
   bool any_cut = false;
@@ -678,7 +689,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float x = q == 0 ? o_scale * decay_pow(l2, max(16 * b + 4 * g + r - skip_now, 0) + lead) : opaque(wq[b]) * step[r];
+            const float x = q == 0 ? o_scale * decay_pow(l2, max(16 * b + 4 * g + r - skip_now, 0) + lead) : opaque(wq[b]) * turned(step[r]);
 #pragma unroll
             for (int t = 0; t < DVT; ++t) o[b][t][r] *= x;
           }
@@ -754,7 +765,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) weight[b][r] = opaque(wk[b]) * step[3 - r];
+      for (int r = 0; r < 4; ++r) weight[b][r] = opaque(wk[b]) * turned(step[3 - r]);
     add_state<T, DKT, DVT>(S, fk, fv, weight, cut, g);
     live = true;
     wave_fence();
@@ -762,6 +773,16 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
     if constexpr (STATES) any_cut |= cut != 0;
     keep_turn += keep_rise;               // (a carry out of 32 bits: the upper one)
     keep = __uint_as_float(keep_low + (keep_turn < keep_rise ? 1u : 0u));
+    if constexpr (TURNS) {
+      keep = -keep;
+      sign ^= 0x80000000u;
+    }
+  }
+  if (sign && (wants_state || careful < p1)) {
+#pragma unroll
+    for (int a = 0; a < DKT; ++a)
+#pragma unroll
+      for (int t = 0; t < DVT; ++t) S[a][t] = -S[a][t];
   }
 
   if (careful < p1) {

@@ -51,13 +51,9 @@ def test_a_young_state_is_decayed_as_often_as_it_is_old(rx, dtype):
     assert (off <= bound[:, None]).all(), [(int(a), float(off[age == a].max() / U)) for a in range(8)]
 
 
-@pytest.mark.parametrize("dtype", list(TYPES))
-def test_a_long_sum_is_not_cut_off_in_one_direction(rx, dtype):
-    """20 000 steps of a memory that hardly forgets, in one walk.
-
-    At most one rounding a step, each at most U of the state and independent of the others: sqrt(T) U of the state's norm in all, and the
-    mean over its 4096 elements 64 times less (times 5: five standard deviations)."""
-    T, N, D = 20000, 1030, 64
+def _long_sum(rx, dtype, T=20000, N=1030, D=64):
+    """What the elements of a state are off by, in units of their root mean square, behind T steps of a memory that hardly forgets, in one
+    walk."""
     g = np.random.default_rng(5)
     k, v = (typed(g.normal(size=(T, 1, 1, D)), TYPES[dtype]) for _ in range(2))
     log_decay = typed(np.array([-1e-5]), torch.float32)
@@ -67,9 +63,23 @@ def test_a_long_sum_is_not_cut_off_in_one_direction(rx, dtype):
     assert torch.equal(s, s[:1].expand_as(s))
     w = np.exp(f64(log_decay) * np.arange(T - 1, -1, -1))
     ref = (f64(k)[:, 0, 0] * w[:, None]).T @ f64(v)[:, 0, 0]
-    off, size = f64(s[0, 0]) - ref, np.sqrt((ref ** 2).mean())
-    assert np.sqrt((off ** 2).mean()) <= np.sqrt(T) * U * size, np.sqrt((off ** 2).mean()) / size
-    assert abs(off.mean()) <= 5 * np.sqrt(T) * U / D * size, off.mean() / size
+    return (f64(s[0, 0]) - ref) / np.sqrt((ref ** 2).mean())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_a_long_sum_is_not_cut_off_in_one_direction(rx, dtype):
+    """At most one rounding a step, each at most U of the state and independent of the others: sqrt(T) U of the state's norm in all, and the
+    mean over its 4096 elements 64 times less (times 5: five standard deviations)."""
+    off = _long_sum(rx, dtype)
+    assert np.sqrt((off ** 2).mean()) <= np.sqrt(20000) * U
+    assert abs(off.mean()) <= 5 * np.sqrt(20000) * U / 64
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_the_mean_of_a_long_sum_is_noise(rx, dtype):
+    """Beside what its elements are off by, whatever that is: within five standard errors."""
+    off = _long_sum(rx, dtype)
+    assert abs(off.mean()) <= 5 * off.std() / 64, off.mean() / (off.std() / 64)
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
