@@ -217,11 +217,17 @@ __device__ __forceinline__ void store_frag(Descriptor d, uint32_t at, int there,
     else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, p), d, o, 0, 0);
   }
 }
+// N values of one row, whose address all lanes have, one by one; a lane's that are not `wanted` go beyond the descriptor's range.
 template <typename T, int N>
-__device__ __forceinline__ void store_far(const char* row, bool exists, int e0, int width, const float (&v)[N]) {
+__device__ __forceinline__ void store_far(const char* row, bool wanted, int e0, int width, const float (&v)[N]) {
+  const Descriptor d = descriptor(row, true, width * (int)sizeof(T));
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (exists && e0 + i < width) reinterpret_cast<T*>(const_cast<char*>(row))[e0 + i] = from_float<T>(v[i]);
+  for (int i = 0; i < N; ++i) {
+    const int o = (int)(wanted & (e0 + i < width) ? (uint32_t)((e0 + i) * (int)sizeof(T)) : NOWHERE);
+    const T x = from_float<T>(v[i]);
+    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), d, o, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, x), d, o, 0, 0);
+  }
 }
 
 // N values of a state, BYTES at a time.
@@ -592,8 +598,9 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     step[r] = __uint_as_float(uniform(__float_as_uint(decay_pow(l2, r))));
-    // (No branch that only some lanes take may enclose work here or in the loop: where registers are short the compiler stores some at such a
-    // branch's end while lanes are still switched off, and gives those lanes stale values back.)
+    // (No branch that only some lanes take may stand in this kernel: where registers are short the compiler stores some at such a branch's
+    // end while lanes are still switched off, and gives those lanes stale values back.  Lanes that have nothing to load or store do it
+    // out of range, or all the same; tests/test_kernel_listing.py looks for instructions that switch lanes off.)
     const float x = w.scale * decay_pow(l2, max(c - 4 * g - r, 0));
     wp[r] = c >= 4 * g + r ? x : 0.f;
   }
@@ -643,7 +650,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
     sc.store(lds_c, lane, 0);
     if constexpr (!STATES) sa.store(lds_a, lane, k_wave);
     if constexpr (SHARED) {
-      if (lane == 0) lds_bad[q & 1][wave] = bad ? 1 : 0;
+      lds_bad[q & 1][wave] = bad ? 1 : 0;
       __syncthreads();
       bad = false;
 #pragma unroll
@@ -736,7 +743,9 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
 #pragma unroll
           for (int t = 0; t < DVT; ++t) v[t] = o[b][t][r];
           if constexpr (PIECE != 0) store_frag<T, DVT, PIECE, WHOLE>(descriptor(O.low), slot >= skip_now ? from_o + (uint32_t)((16 * b + r) * (int)O.step) : NOWHERE, there_o, v);
-          else store_far<T, DVT>(O.address(slot), slot >= skip_now, e_lane, E, v);
+          else
+#pragma unroll
+            for (int x = 0; x < 4; ++x) store_far<T, DVT>(O.address(16 * b + 4 * x + r), (g == x) & (slot >= skip_now), e_lane, E, v);
         }
       O.move(CHUNK);
     }
@@ -846,7 +855,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
       }
   }
   if constexpr (STATES) {
-    if (w.cuts && h == 0 && tile == 0 && lane == 0) w.cuts[((int64_t)ji * w.N + n) * w.segments + piece] = any_cut ? 1 : 0;
+    if (w.cuts && h == 0 && tile == 0) w.cuts[((int64_t)ji * w.N + n) * w.segments + piece] = any_cut ? 1 : 0;
   } else {
     if (SHARED && idle) return;
     // steps that do not exist: zero
@@ -858,7 +867,9 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
       for (int r = 0; r < 4; ++r) {
         const bool exists = 4 * g + r < t1 - t;
         if constexpr (PIECE != 0) store_frag<T, DVT, PIECE, WHOLE>(descriptor(Z.low), exists ? Z.at(4 * g + r) + e_lane * SIZE : NOWHERE, E - e_lane, zero);
-        else store_far<T, DVT>(Z.address(4 * g + r), exists, e_lane, E, zero);
+        else
+#pragma unroll
+          for (int x = 0; x < 4; ++x) store_far<T, DVT>(Z.address(4 * x + r), (g == x) & exists, e_lane, E, zero);
       }
   }
 }
