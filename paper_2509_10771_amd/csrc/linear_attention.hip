@@ -617,8 +617,8 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
   const float nearest = (float)chunk_decay;
   const bool between = nearest < 1e30f;
   const uint32_t keep_low = uniform(__float_as_uint(nearest) - ((between & ((double)nearest > chunk_decay)) ? 1 : 0));
-  const double below = __uint_as_float(keep_low), above = __uint_as_float(keep_low + 1);
-  const uint32_t keep_rise = uniform(between ? (uint32_t)fmin((chunk_decay - below) / (above - below) * 0x1p32, 0x1p32 - 1) : 0u);
+  // (floats beside each other are 2^(E - 150) apart, E the exponent's bits, at least 1)
+  const uint32_t keep_rise = uniform(between ? (uint32_t)ldexp(chunk_decay - (double)__uint_as_float(keep_low), 182 - max((int)(keep_low >> 23), 1)) : 0u);
   uint32_t keep_turn = 0x80000000u;
   float keep = decay_pow(l2, CHUNK - skip);
   // The bf16 matrix instructions cut what they add off downwards (see split_bf16.h), which would add up over the chunks of a long memory (a
