@@ -149,13 +149,20 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void layer_norm_backward_kernel(No
   };
   load(row);
   Pack<float, W> w[ITEMS];
+  // 1024 lanes have 128 registers each: with 16 values a lane the gradients' sums lie in LDS, where nobody else reads or writes a lane's.  With
+  // them in registers the compiler kept others on the stack, and stored some inside branches that only some lanes take (2048 rows of 16384
+  // in fp32 112 us both launches, in bf16 76; on the stack 155 and 105).
+  constexpr bool IN_LDS = TPR == 1024 && ITEMS * W > 8;
+  __shared__ __attribute__((aligned(16))) float sums[IN_LDS ? 2 * ITEMS * W * TPR : 4];
   float dw[ITEMS * W], db[ITEMS * W];
+  auto sum_at = [&](int pass, int x) -> float4& { return *reinterpret_cast<float4*>(sums + ((pass * ITEMS * W + x) / 4 * TPR + lane) * 4); };
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
 #pragma unroll
     for (int k = 0; k < W; ++k) {
       w[i].v[k] = 1.f;
       dw[i * W + k] = db[i * W + k] = 0.f;
+      if (IN_LDS && k % 4 == 0) sum_at(0, i * W + k) = sum_at(1, i * W + k) = float4{0.f, 0.f, 0.f, 0.f};
     }
     if (a.weight) load_piece<float, W, WHOLE>(w[i], a.weight, (i * TPR + lane) * W, a.cols);
   }
@@ -171,8 +178,18 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void layer_norm_backward_kernel(No
         const float d = here ? to_float(pd[i].v[k]) : 0.f;
         h[x] = here ? (to_float(px[i].v[k]) - mean) * rstd : 0.f;
         g[x] = here ? d * w[i].v[k] : 0.f;
-        dw[x] += d * h[x];
-        db[x] += d;
+        if constexpr (!IN_LDS) {
+          dw[x] += d * h[x];
+          db[x] += d;
+        } else {
+          dw[x % 4] = d * h[x];
+          db[x % 4] = d;
+          if (x % 4 == 3) {
+            float4 &to_w = sum_at(0, x), &to_b = sum_at(1, x);
+            to_w = float4{to_w.x + dw[0], to_w.y + dw[1], to_w.z + dw[2], to_w.w + dw[3]};
+            to_b = float4{to_b.x + db[0], to_b.y + db[1], to_b.z + db[2], to_b.w + db[3]};
+          }
+        }
         s[0] += g[x];
         s[1] += g[x] * h[x];
       }
@@ -195,6 +212,15 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void layer_norm_backward_kernel(No
 #pragma unroll
   for (int pass = 0; pass < 2; ++pass) {
     float(&v)[ITEMS * W] = pass == 0 ? dw : db;
+    if constexpr (IN_LDS)
+#pragma unroll
+      for (int x = 0; x < ITEMS * W; x += 4) {
+        const float4 f = sum_at(pass, x);
+        v[x] = f.x;
+        v[x + 1] = f.y;
+        v[x + 2] = f.z;
+        v[x + 3] = f.w;
+      }
     if constexpr (ROWS > 1) {
       __syncthreads();
       if (sub > 0)

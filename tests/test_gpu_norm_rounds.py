@@ -26,7 +26,7 @@ def rx():
 # every number of lanes a row has: parts of a wavefront, a wavefront, workgroups of 256 to 1024; rows of whole loads and rows that start anywhere
 @pytest.mark.parametrize("rows,cols,dtype", [(40000, 64, "fp32"), (33333, 61, "bf16"), (18000, 128, "fp16"), (9001, 240, "fp32"), (8300, 500, "fp32"),
                                              (2100, 1100, "fp32"), (2100, 1101, "fp16"), (2085, 2048, "bf16"), (2070, 4100, "fp32"), (2060, 4099, "fp16"),
-                                             (2055, 9000, "bf16")])
+                                             (2055, 9000, "bf16"), (1100, 9001, "fp32"), (1030, 12001, "fp16"), (1040, 16384, "fp32")])
 def test_rounds(rx, rows, cols, dtype):
     x, dy, w, b = _case(rows + cols, rows, cols, dtype)
     gx, gd, gw, gb = x.cuda(), dy.cuda(), w.cuda(), b.cuda()

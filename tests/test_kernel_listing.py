@@ -63,3 +63,11 @@ def test_the_walk_switches_no_lane_off(kernels):
         assert len(code) > 200
         found = [x for x in code if writes.match(x)]
         assert not found, (name, found[:3])
+
+
+def test_the_other_kernels_keep_nothing_on_the_stack(kernels):
+    others = {n: k for n, k in kernels.items() if "walk_kernel" not in n and ("norm" in n or "attention_step" in n or "walk_join" in n)}
+    assert len(others) > 90
+    for name, code in others.items():
+        found = [x for x in code if x.startswith("scratch_") or "v_accvgpr" in x]
+        assert not found, (name, len(found), found[0])
