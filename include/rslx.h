@@ -461,7 +461,10 @@ int32_t rslx_rnd(const rslx_mlp* target, const rslx_mlp* predictor, const float*
 
 /* ---- linear attention with a decay for each head (a memory over whole sequences) ------------- */
 
-/* Types of the activations of the operators from here on; parameters, states and statistics are fp32. */
+/* Types of the activations of the operators from here on; parameters, states and statistics are fp32, and so is arithmetic, with one
+ * exception: over whole sequences in 16 bits, outputs and gradients are made of states and weighted scores with 16
+ * significant bits (errors up to 2^-17 of a term in bf16, 2^-15 in fp16, beside the result's own rounding of 2^-8 and
+ * 2^-11).  What is added to a state has fp32's. */
 #define RSLX_F32 0
 #define RSLX_BF16 1
 #define RSLX_F16 2
@@ -500,8 +503,8 @@ typedef struct rslx_linear_attn {
 } rslx_linear_attn;
 
 /* The whole sequence.  q, k: width Dk; v, o: width Dv; s0, s_last: device [N, H, Dk, Dv] or NULL (s_last may be
- * the buffer of s0).  Outputs must not overlap inputs or each other otherwise.  A few long sequences are walked in pieces side by side, which
- * takes workspace; otherwise ws may be NULL. */
+ * the buffer of s0).  Outputs must not overlap inputs or each other otherwise.  A few long sequences are walked in
+ * pieces side by side, which takes workspace; otherwise ws may be NULL. */
 size_t rslx_linear_attention_workspace_bytes(const rslx_linear_attn* a);
 int32_t rslx_linear_attention(const rslx_linear_attn* a, const rslx_seq_view* q, const rslx_seq_view* k,
                               const rslx_seq_view* v, const float* s0_or_null, const rslx_seq_view* o,
@@ -532,7 +535,8 @@ int32_t rslx_linear_attention_step(const rslx_linear_attn* a, const rslx_seq_vie
 
 /* Per row:  m = mean x,  r = 1 / sqrt(mean (x - m)^2 + eps),  y = (x - m) r weight + bias.
  * x, y: [rows, cols] of `dtype`, rows ldx and ldy elements apart; y may be x with the same distance, and must not overlap
- * it otherwise (the columns beside x in one buffer do not).  weight, bias: device fp32 [cols], NULL = 1 and 0.  mean, rstd: device fp32 [rows] or NULL; the backward pass reads them. */
+ * it otherwise (the columns beside x in one buffer do not).  weight, bias: device fp32 [cols], NULL = 1 and 0.
+ * mean, rstd: device fp32 [rows] or NULL; the backward pass reads them. */
 #define RSLX_NORM_MAX_COLS 16384
 int32_t rslx_layer_norm(int32_t dtype, const void* x, int64_t ldx, int64_t rows, int32_t cols,
                         const float* weight_or_null, const float* bias_or_null, float eps, void* y, int64_t ldy,
@@ -540,8 +544,9 @@ int32_t rslx_layer_norm(int32_t dtype, const void* x, int64_t ldx, int64_t rows,
 
 /* With g = dy weight and h = (x - mean) rstd:  dx = rstd (g - mean(g) - h mean(g h)) per row,
  * dweight = sum over rows of dy h, dbias = sum over rows of dy (device fp32 [cols]; zero where there are no rows).
- * Any of dx, dweight, dbias may be NULL; dx may be dy or x, with the same distance, and must not overlap them otherwise.  The sums are taken in a fixed order: the same inputs give
- * the same bits.  Without dweight and dbias no workspace is needed. */
+ * Any of dx, dweight, dbias may be NULL; dx may be dy or x, with the same distance, and must not overlap them otherwise.
+ * The sums are taken in a fixed order: the same inputs give the same bits.  Without dweight and dbias no workspace is
+ * needed. */
 size_t rslx_layer_norm_backward_workspace_bytes(int64_t rows, int32_t cols);
 int32_t rslx_layer_norm_backward(int32_t dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx,
                                  int64_t rows, int32_t cols, const float* weight_or_null, const float* mean,

@@ -3,8 +3,9 @@
 //
 //   S_i = l S_{i-1} + b_i c_i^T,   o_i = scale S_i^T a_i,   l = exp(log_decay[h])
 //
-// A chunk of 16 positions is four small products on the fp32 matrix cores: the scores P = A B^T, weighted by l^(i - j) below the diagonal,
-// O = P C + l^(i + 1) A S, and S <- l^16 S + (l^(15 - j) B)^T C.  A wavefront walks one head of one sequence (16 DVT columns of it): the state stays in its accumulator registers, and because the order of a contraction's indices is free, nothing has to be
+// A chunk of n = 16 positions (in 16-bit types 32: two blocks of 16) is four small products on the matrix cores: the scores P = A B^T, weighted by
+// l^(i - j) below the diagonal, O = P C + l^(i + 1) A S, and S <- l^n S + (l^(n - 1 - j) B)^T C.  A wavefront walks one head of one sequence
+// (16 DVT columns of it): the state stays in its accumulator registers, and because the order of a contraction's indices is free, nothing has to be
 // moved between lanes.  With lane = 16 g + c, the instruction v_mfma_f32_16x16x4_f32 leaves in register r row 4 g + r of column c, and
 // reads from an operand row (column) c at index g.  So
 //   - the transposed scores B A^T leave P[c][4 g + r]: the left operand of P C if step s takes the contraction index 4 g + s;
@@ -16,10 +17,11 @@
 // rows an access, they take four times the cache accesses, and the caches bound the walk (8192 steps of 16 heads of 128 in bf16: 134 us;
 // through LDS 118, with a workgroup's wavefronts sharing the rows of A and B 106, on one card).
 //
-// What bounds it now: a roll-out of 24 steps in fp32 (4096 environments, four heads of 64) memory, 196 us = 4.8 TB/s; long sequences in 16 bits the
-// vector instructions that take the state and the weighted scores apart into bf16 values (some 700 a chunk of 32 beside 100 matrix instructions)
-// and the latency of a chunk's loads at two wavefronts a SIMD, which their registers allow.  Long sequences of few heads are cut into pieces:
-// one launch for every piece's own contribution to the state, one that joins them, one for the outputs.
+// What bounds it now: a roll-out of 24 steps in fp32 (4096 environments, four heads of 64) memory, 193 us = 4.9 TB/s; long sequences in 16 bits
+// (8192 steps of 16 heads of 128 in bf16: 91 us, three launches) the vector instructions that take the state and the weighted scores apart
+// into bf16 values (some 700 a chunk of 32 beside 100 matrix instructions) and the latency of a chunk's loads at two wavefronts a SIMD, which
+// their registers allow.  Long sequences of few heads are cut into pieces: one launch for every piece's own contribution to the state, one that
+// joins them, one for the outputs.
 #include <algorithm>
 
 #include "sequence.h"
@@ -223,7 +225,7 @@ __device__ __forceinline__ void store_far(const char* row, bool wanted, int e0, 
   const Descriptor d = descriptor(row, true, width * (int)sizeof(T));
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int o = (int)(wanted & (e0 + i < width) ? (uint32_t)((e0 + i) * (int)sizeof(T)) : NOWHERE);
+    const int o = (int)((wanted & (e0 + i < width)) ? (uint32_t)((e0 + i) * (int)sizeof(T)) : NOWHERE);
     const T x = from_float<T>(v[i]);
     if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), d, o, 0, 0);
     else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, x), d, o, 0, 0);
@@ -275,8 +277,9 @@ __device__ __forceinline__ int sequence_length(const WalkArgs& w, int n) {
 // the widths, the lane's 4 DKT consecutive values as they lie in memory, eight by eight (value DKT r + a is row r of state tile a: pairs
 // of tiles fill a register); of the positions, 4 g + s of the first block, then of the second.  What is exact in 16 bits is multiplied as it
 // is; what is not (weighted scores, the state, the weighted C) is taken apart into bf16 values: two for results that are rounded to 16
-// bits (what is left out is 2^-17 of a term, far below that rounding), three for the state, which stays exact to fp32.  fp16 inputs reach
-// products with such parts as two bf16 values of their own, which hold them exactly.
+// bits (what is left out is 2^-17 of a term at most, where that rounding is 2^-8 or 2^-11 of the result), three, as many bits as fp32 has, for
+// what is added to the state.  fp16 inputs reach products with such parts as two bf16 values of their own, which hold them exactly; the
+// product of the two second parts is left out (2^-16 of a term at most).
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 template <typename T> constexpr int PARTS = __is_same(T, __half) ? 2 : 1;      // bf16 values that make an input
@@ -742,7 +745,8 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
           float v[DVT];
 #pragma unroll
           for (int t = 0; t < DVT; ++t) v[t] = o[b][t][r];
-          if constexpr (PIECE != 0) store_frag<T, DVT, PIECE, WHOLE>(descriptor(O.low), slot >= skip_now ? from_o + (uint32_t)((16 * b + r) * (int)O.step) : NOWHERE, there_o, v);
+          if constexpr (PIECE != 0)
+            store_frag<T, DVT, PIECE, WHOLE>(descriptor(O.low), slot >= skip_now ? from_o + (uint32_t)((16 * b + r) * (int)O.step) : NOWHERE, there_o, v);
           else
 #pragma unroll
             for (int x = 0; x < 4; ++x) store_far<T, DVT>(O.address(16 * b + 4 * x + r), (g == x) & (slot >= skip_now), e_lane, E, v);
@@ -1035,7 +1039,9 @@ void dispatch_walk(const WalkArgs& w, WalkClass k, int tiles, int64_t items, hip
   }
 }
 
-// The largest access that every row of every matrix allows.
+// The largest access that every row of every matrix allows.  16 / 4 / 2 bytes, rows of the same width further apart: 8192 steps of 16 heads of 128 in bf16
+// 88 / 104 / 135 us, gradients 179 / 229 / 343; a roll-out of 24 steps of 4096, four heads of 64, in bf16 148 / 187 / 291, in fp32 206 / 249.  Rows too far
+// apart for 32-bit offsets: 24 steps of 1024 in fp32 139 us, 53 where they are not.
 int walk_piece(const WalkArgs& w, int size) {
   uintptr_t bits = 0;
   bool near = true;
@@ -1080,6 +1086,8 @@ int walk_waves_per_head(int D, int E, int size) {
 // Pieces of a long sequence (of RSLX_ATTN_MAX_STEPS at most: what is rounded up to whole chunks has 32 bits) where the sequences' heads are too few to fill the chip.
 int walk_segments(int64_t waves, int32_t T, int32_t* seg_len) {
   constexpr int64_t TARGET = 2048;        // two wavefronts for each of the 1024 SIMDs
+  // Shorter pieces are more of them side by side, and more states to move: of at least 32 / 64 / 128 positions, 512 steps of 16 heads of 64 in
+  // fp32 27 / 35 / 54 us, 2048 of 8 of 128 in bf16 46 / 38 / 42, 100 of 4 of 32 in fp32 22 / 15 / 15 (in one piece).
   constexpr int LEAST = 64;
   int64_t m = waves > 0 ? TARGET / waves : 1;
   m = m < T / LEAST ? m : T / LEAST;

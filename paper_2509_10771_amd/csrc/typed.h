@@ -1,4 +1,5 @@
-// Activations of the sequence operators (linear attention, layer norm) come in three types; arithmetic is fp32.
+// Activations of the sequence operators (linear attention, layer norm) come in three types; arithmetic is fp32, but for the 16-bit walks' products,
+// which linear_attention.hip describes.
 #pragma once
 
 #include <hip/hip_fp16.h>
