@@ -889,6 +889,20 @@ __global__ __launch_bounds__(256) void walk_join_kernel(WalkArgs w, JoinStarts s
   const WalkJob& job = w.job[ji];
   const int len = sequence_length(w, n);
   const double l2 = log2_decay(w.log_decay[h]);
+  // The first slots are on their way while the decays are made.
+  const int size = job.D * job.E, e = min((int)(blockIdx.y * 256 + threadIdx.x), size - 1);
+  const bool here = (int)(blockIdx.y * 256 + threadIdx.x) < size;
+  const int64_t head = (int64_t)n * w.H + h;
+  float* slot = job.s_out + head * w.segments * size + e;
+  constexpr int AHEAD = 8;
+  float x[AHEAD];
+  auto load = [&](int m0) {
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) x[k] = slot[(int64_t)(min(m0 + k, w.segments - 2) + 1) * size];
+  };
+  load(0);
+  float run = starts.start[ji] ? starts.start[ji][head * size + e] : 0.f;
+  if (job.reversed && len > 0 && w.dones && w.dones[(int64_t)(len - 1) * w.N + n]) run = 0.f;
   for (int m = threadIdx.x; m < w.segments - 1; m += 256) {
     const double decay = exp2(l2 * (double)min(max(len - m * w.seg_len, 0), w.seg_len));
     f[m] = (float)decay;
@@ -896,18 +910,9 @@ __global__ __launch_bounds__(256) void walk_join_kernel(WalkArgs w, JoinStarts s
     cut[m] = w.cuts[((int64_t)ji * w.N + n) * w.segments + m];
   }
   __syncthreads();
-  const int e = blockIdx.y * 256 + threadIdx.x, size = job.D * job.E;
-  if (e >= size) return;
-  const int64_t head = (int64_t)n * w.H + h;
-  float* slot = job.s_out + head * w.segments * size + e;
-  float run = starts.start[ji] ? starts.start[ji][head * size + e] : 0.f;
-  if (job.reversed && len > 0 && w.dones && w.dones[(int64_t)(len - 1) * w.N + n]) run = 0.f;
+  if (!here) return;
   slot[0] = run;
-  constexpr int AHEAD = 8;
   for (int m0 = 0; m0 < w.segments - 1; m0 += AHEAD) {
-    float x[AHEAD];
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) x[k] = slot[(int64_t)(min(m0 + k, w.segments - 2) + 1) * size];
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       if (m0 + k >= w.segments - 1) break;
@@ -915,6 +920,7 @@ __global__ __launch_bounds__(256) void walk_join_kernel(WalkArgs w, JoinStarts s
       run = cut[m0 + k] ? x[k] : fmaf(run, f[m0 + k], fmaf(finite, f_rest[m0 + k], x[k]));
       slot[(int64_t)(m0 + k + 1) * size] = run;
     }
+    if (m0 + AHEAD < w.segments - 1) load(m0 + AHEAD);
   }
 }
 
