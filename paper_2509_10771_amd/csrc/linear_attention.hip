@@ -115,15 +115,15 @@ __device__ __forceinline__ void load_frag(Frag<T, N>& f, Descriptor d, uint32_t 
     }
   }
 }
-// N values of a row from value e0 on, one by one; zero where not `wanted`.  The row exists.  APART: in the order of place().
-template <typename T, int N, bool APART = false>
+// N values of a row from value e0 on, one by one; zero where not `wanted`.  The row exists.
+template <typename T, int N>
 __device__ __forceinline__ void load_far(Frag<T, N>& f, const char* row, bool wanted, int e0, int width) {
 #pragma unroll
   for (int k = 0; k < Frag<T, N>::WORDS; ++k) {
     f.w[k] = 0;
 #pragma unroll
     for (int h = 0; h < 4 / (int)sizeof(T); ++h) {
-      const int y = k * (4 / (int)sizeof(T)) + h, e = e0 + (APART ? place<T>(y) : y);
+      const int e = e0 + k * (4 / (int)sizeof(T)) + h;
       const bool here = wanted & (e < width);
       const int from = here ? e : 0;
       uint32_t x;
@@ -219,13 +219,32 @@ __device__ __forceinline__ void store_frag(Descriptor d, uint32_t at, int there,
     else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, p), d, o, 0, 0);
   }
 }
-// N values of one row, whose address all lanes have, one by one; a lane's that are not `wanted` go beyond the descriptor's range.
+// N values from value e0 on of one row, whose address all lanes have, in the order of place() where APART; zero past the row's width.
+template <typename T, int N, bool APART>
+__device__ __forceinline__ void load_row(Frag<T, N>& f, const char* row, int e0, int width) {
+  const Descriptor d = descriptor(row, true, width * (int)sizeof(T));
+  const int at = e0 * (int)sizeof(T);
+#pragma unroll
+  for (int y = 0; y < N; ++y) {
+    const int o = at + (APART ? place<T>(y) : y) * (int)sizeof(T);
+    if constexpr (sizeof(T) == 4) {
+      f.w[y] = __builtin_amdgcn_raw_buffer_load_b32(d, o, 0, 0);
+    } else {
+      const uint32_t x = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(d, o, 0, 0);
+      f.w[y / 2] = y % 2 ? f.w[y / 2] | x << 16 : x;
+    }
+  }
+}
+
+// N values of one row, whose address all lanes have, one by one.  Values past the row's width lie beyond the descriptor's range, and so do
+// those of a lane that has none `wanted`.
 template <typename T, int N>
 __device__ __forceinline__ void store_far(const char* row, bool wanted, int e0, int width, const float (&v)[N]) {
   const Descriptor d = descriptor(row, true, width * (int)sizeof(T));
+  const uint32_t at = wanted ? (uint32_t)(e0 * (int)sizeof(T)) : NOWHERE;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int o = (int)((wanted & (e0 + i < width)) ? (uint32_t)((e0 + i) * (int)sizeof(T)) : NOWHERE);
+    const int o = (int)(at + (uint32_t)(i * (int)sizeof(T)));
     const T x = from_float<T>(v[i]);
     if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), d, o, 0, 0);
     else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, x), d, o, 0, 0);
@@ -801,7 +820,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
   if (careful < p1) {
     const int g = opaque(lane >> 4), c = opaque(lane & 15), e_lane = e_tile + DVT * c;
     const float l1 = decay_pow(l2, 1);
-    at = careful;
+    at = STATES ? uniform(careful) : careful;      // (without outputs the compiler does not see that it is the same for all lanes)
     Rows<CHUNK> a{}, b = rows(job.b), z = rows(job.c), out{};
     if constexpr (!STATES) {
       a = rows(job.a);
@@ -812,9 +831,9 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
       const bool cut = w.dones && t >= 0 && w.dones[(int64_t)t * w.N + n] != 0;
       Frag<T, 4 * DKT> xa, xb;
       Frag<T, DVT> xc;
-      load_far<T, 4 * DKT, true>(xb, b.address(0), true, PE16<T> * g, D);
-      load_far<T, DVT>(xc, z.address(0), true, e_lane, E);
-      if constexpr (!STATES) load_far<T, 4 * DKT, true>(xa, a.address(0), true, PE16<T> * g, D);
+      load_row<T, 4 * DKT, true>(xb, b.address(0), PE16<T> * g, D);
+      load_row<T, DVT, false>(xc, z.address(0), e_lane, E);
+      if constexpr (!STATES) load_row<T, 4 * DKT, true>(xa, a.address(0), PE16<T> * g, D);
       float sum[DVT] = {};
 #pragma unroll
       for (int x = 0; x < DKT; ++x)
@@ -833,7 +852,7 @@ __global__ __launch_bounds__(64 * WALK_WAVES, DKT * DVT > 16 ? 1 : 2) void walk_
           sum[t] += __shfl_xor(sum[t], 16, 64);
           sum[t] = (sum[t] + __shfl_xor(sum[t], 32, 64)) * o_scale;
         }
-        store_far<T, DVT>(out.address(0), g == 0, e_lane, E, sum);
+        store_far<T, DVT>(out.address(0), lane < 16, e_lane, E, sum);
         a.move(1);
         out.move(1);
       }
