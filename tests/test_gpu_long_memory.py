@@ -100,3 +100,12 @@ def test_a_state_through_many_pieces(rx, dtype):
         ref = f64(s0) * np.exp(T * f64(log_decay)[0])
         off = np.linalg.norm(f64(s) - ref) / np.linalg.norm(ref)
         assert off <= (np.sqrt(T / 64) + 4 + 8) * U, off / U
+
+
+@pytest.mark.parametrize("name", ["k", "v", "do"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("T", [200, 231, 290])
+def test_what_is_not_finite_behind_an_odd_or_even_chunk(rx, name, dtype, T):
+    """The state's sign turns with every chunk; positions taken one by one start with its own.  In pieces, a wavefront for a tile."""
+    import test_gpu_linear_attention as attention
+    attention.test_what_is_not_finite_in_16_bits(rx, name, dtype, T, 40, 64)
