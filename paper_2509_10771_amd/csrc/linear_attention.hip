@@ -17,8 +17,8 @@
 // rows an access, they take four times the cache accesses, and the caches bound the walk (8192 steps of 16 heads of 128 in bf16: 134 us;
 // through LDS 118, with a workgroup's wavefronts sharing the rows of A and B 106, on one card).
 //
-// What bounds it now: a roll-out of 24 steps in fp32 (4096 environments, four heads of 64) memory, 193 us = 4.9 TB/s; long sequences in 16 bits
-// (8192 steps of 16 heads of 128 in bf16: 91 us, three launches) the vector instructions that take the state and the weighted scores apart
+// What bounds it now: a roll-out of 24 steps in fp32 (4096 environments, four heads of 64) memory, 192 us = 4.9 TB/s; long sequences in 16 bits
+// (8192 steps of 16 heads of 128 in bf16: 89 us, three launches) the vector instructions that take the state and the weighted scores apart
 // into bf16 values (some 700 a chunk of 32 beside 100 matrix instructions) and the latency of a chunk's loads at two wavefronts a SIMD, which
 // their registers allow.  Long sequences of few heads are cut into pieces: one launch for every piece's own contribution to the state, one that
 // joins them, one for the outputs.
