@@ -461,10 +461,10 @@ int32_t rslx_rnd(const rslx_mlp* target, const rslx_mlp* predictor, const float*
 
 /* ---- linear attention with a decay for each head (a memory over whole sequences) ------------- */
 
-/* Types of the activations of the operators from here on; parameters, states and statistics are fp32, and so is arithmetic, with one
- * exception: over whole sequences in 16 bits, outputs and gradients are made of states and weighted scores with 16
- * significant bits (errors up to 2^-17 of a term in bf16, 2^-15 in fp16, beside the result's own rounding of 2^-8 and
- * 2^-11).  What is added to a state has fp32's. */
+/* Types of the activations of the operators from here on; parameters, states and statistics are fp32, and so is
+ * arithmetic, with one exception: over whole sequences in 16 bits, outputs and gradients are made of states and weighted
+ * scores with 16 significant bits (errors up to 2^-17 of a term in bf16, 2^-15 in fp16, beside the result's own rounding
+ * of 2^-8 and 2^-11).  What is added to a state has fp32's. */
 #define RSLX_F32 0
 #define RSLX_BF16 1
 #define RSLX_F16 2
@@ -494,7 +494,7 @@ typedef struct rslx_seq_view {
 #define RSLX_ATTN_MAX_STEPS 2147483583 /* 2^31 - 65 */
 typedef struct rslx_linear_attn {
   int32_t dtype;                 /* RSLX_F32, RSLX_BF16, RSLX_F16: q, k, v, o and their gradients */
-  int32_t T, N, H;               /* T: 0..RSLX_ATTN_MAX_STEPS */
+  int32_t T, N, H;               /* T: 0..RSLX_ATTN_MAX_STEPS; N * H: 0..2^24 */
   int32_t Dk, Dv;                /* 1..RSLX_ATTN_MAX_DIM */
   float scale;
   const float* log_decay;        /* device [H] */

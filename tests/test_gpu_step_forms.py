@@ -40,3 +40,20 @@ def test_forms_of_the_step(rx, N, H, Dk, Dv, dtype):
             s2, o2 = g["s0"].clone(), c.empty(Dv)
             rx.rslx_linear_attention_step(la, g["q"], g["k"], g["v"], gpu_reset, s2, s2, o2)
             assert torch.equal(s, s2) and torch.equal(o, o2)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N,H,Dk,Dv", [(33, 3, 64, 64), (700, 3, 64, 64), (40, 4, 100, 36), (900, 3, 100, 36), (3, 2, 128, 128)])
+@pytest.mark.parametrize("name", ["q", "k", "v"])
+def test_output_in_place(rx, name, N, H, Dk, Dv, dtype):
+    """o where q, k or v lies (the first values of wider rows): the same bits, and nothing beside them."""
+    c = Attention(N + Dk, 1, N, H, Dk, Dv, dtype)
+    g, la = c.on_gpu(rx)
+    want, s = c.empty(Dv), c.state()
+    rx.rslx_linear_attention_step(la, g["q"], g["k"], g["v"], None, g["s0"], s, want)
+    x = {n: g[n].clone() for n in "qkv"}
+    s2 = c.state()
+    rx.rslx_linear_attention_step(la, x["q"], x["k"], x["v"], None, g["s0"], s2, x[name][..., :Dv])
+    assert torch.equal(x[name][..., :Dv], want) and torch.equal(s, s2)
+    assert torch.equal(x[name][..., Dv:], g[name][..., Dv:])
+    assert all(torch.equal(x[n], g[n]) for n in "qkv" if n != name)
