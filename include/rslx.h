@@ -553,6 +553,108 @@ int32_t rslx_layer_norm_backward(int32_t dtype, const void* dy, int64_t lddy, co
                                  const float* rstd, void* dx_or_null, int64_t lddx, float* dweight_or_null,
                                  float* dbias_or_null, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- gated linear recurrence (a memory of one state per channel) ------------------------ */
+
+/* Per sequence n and channel d, with f = sigmoid(g):
+ *   h_t = f_t keep_{t-1} h_{t-1} + (1 - f_t) x_t,   h_{-1} = s0 (0 if NULL), keep_{-1} = 1
+ * keep_t = 0 where dones[t, n] is set, s_last = keep_{T-1} h_{T-1}, and lengths: all as in linear attention above.  1 - f is
+ * sigmoid(-g), so gates next to one keep their digits; g = +inf holds the state and -inf takes x as it is.
+ * x, g and h (and their gradients) are matrices [T, N, D]: views whose `head` is not used, under the conditions above.
+ * A step's values reach no earlier step and no other episode, whatever they are; an infinite state may be a NaN some
+ * steps later, where the product of the gates between is zero in fp32. */
+#define RSLX_REC_MAX_CHANNELS (1 << 30)
+typedef struct rslx_gated_rec {
+  int32_t dtype;                 /* RSLX_F32, RSLX_BF16, RSLX_F16: x, g, h and their gradients; states are fp32 */
+  int32_t T, N, D;               /* T: 0..RSLX_ATTN_MAX_STEPS; N: 0 or more; D: 1 or more; N * D: to RSLX_REC_MAX_CHANNELS */
+  const uint8_t* dones;          /* device [T, N] or NULL */
+  const int32_t* lengths;        /* device [N] or NULL */
+} rslx_gated_rec;
+
+/* The whole sequence.  s0, s_last: device [N, D] or NULL (s_last may be the buffer of s0).  Outputs must not overlap inputs
+ * or each other otherwise. */
+size_t rslx_gated_recurrence_workspace_bytes(const rslx_gated_rec* a);
+int32_t rslx_gated_recurrence(const rslx_gated_rec* a, const rslx_seq_view* x, const rslx_seq_view* g, const float* s0_or_null,
+                              const rslx_seq_view* h, float* s_last_or_null, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients of a loss through the call above, from those of its outputs, dh and ds_last (NULL = 0):
+ *   d_t = dh_t + keep_t (t + 1 < T ? f_{t+1} d_{t+1} : ds_last)
+ *   dx_t = (1 - f_t) d_t,   dg_t = f_t (1 - f_t) d_t (keep_{t-1} h_{t-1} - x_t),   ds0 = f_0 d_0 (ds_last where there is no step)
+ * Nothing is kept from the forward call: states are walked again, in fp32.  No output (ds0 may be NULL) may overlap an
+ * input or another output. */
+size_t rslx_gated_recurrence_backward_workspace_bytes(const rslx_gated_rec* a);
+int32_t rslx_gated_recurrence_backward(const rslx_gated_rec* a, const rslx_seq_view* x, const rslx_seq_view* g,
+                                       const float* s0_or_null, const rslx_seq_view* dh, const float* ds_last_or_null,
+                                       const rslx_seq_view* dx, const rslx_seq_view* dg, float* ds0_or_null, void* ws,
+                                       size_t ws_bytes, void* stream);
+
+/* One step of every environment, while acting (a->T = 1, dones and lengths NULL; the views' step is not used):
+ *   s_out = f (reset[n] ? 0 : s_in) + (1 - f) x,   h = s_out in its type
+ * reset_or_null, s_in and s_out as in rslx_linear_attention_step; h may be x or g, each row in place of the same sequence's;
+ * nothing else that is written may overlap what is read or written. */
+int32_t rslx_gated_recurrence_step(const rslx_gated_rec* a, const rslx_seq_view* x, const rslx_seq_view* g,
+                                   const uint8_t* reset_or_null, const float* s_in_or_null, float* s_out,
+                                   const rslx_seq_view* h, void* stream);
+
+/* ---- root-mean-square norm with the residual's addition --------------------------------- */
+
+/* Per row:  z = x + residual (x alone where that is NULL),  r = 1 / sqrt(mean z^2 + eps),  y = z r weight.
+ * x, residual, total, y: [rows, cols] of `dtype`, rows ldx, ldr, ldt and ldy elements apart.  total (or NULL) receives z, rounded
+ * to the type: the stream that goes on behind the block, and what the backward pass reads; y is made of z before that
+ * rounding.  weight: device fp32 [cols] or NULL = 1; rstd: device fp32 [rows] or NULL receives r.  total and y may each
+ * be x or residual, with the same distance, and overlap nothing otherwise.
+ * Squares are fp32: a row whose sum of squares passes 3e38 gives zeros (NaN where a value is not finite). */
+int32_t rslx_rms_norm(int32_t dtype, const void* x, int64_t ldx, const void* residual_or_null, int64_t ldr, int64_t rows,
+                      int32_t cols, const float* weight_or_null, float eps, void* total_or_null, int64_t ldt, void* y,
+                      int64_t ldy, float* rstd_or_null, void* stream);
+
+/* The same with y in a byte a value: e4m3 (4 bits of exponent, 3 of fraction, largest value 448; OCP's, without infinities),
+ * y = scales[row] * y8, scales[row] = max |y| / 448 of the row (at least 2^-126: a row of zeros has zeros).  y8 is rounded to nearest, ties to
+ * even; it overlaps nothing.  A row that holds a NaN is NaN, its scale too. */
+int32_t rslx_rms_norm_e4m3(int32_t dtype, const void* x, int64_t ldx, const void* residual_or_null, int64_t ldr, int64_t rows,
+                           int32_t cols, const float* weight_or_null, float eps, void* total_or_null, int64_t ldt, void* y8,
+                           int64_t ldy, float* scales, float* rstd_or_null, void* stream);
+
+/* With h = total rstd and k = dy weight:  dx = dtotal + rstd (k - h mean(k h)) per row (dtotal, the gradient of the stream behind
+ * the block: NULL = 0), dweight = sum over rows of dy h (device fp32 [cols]; zero where there are no rows).  dx is the gradient of x and
+ * of residual.  Either of dx, dweight may be NULL; dx may be dy, total or dtotal, with the same distance, and must not overlap them otherwise.
+ * Sums are taken in a fixed order.  Without dweight no workspace is needed. */
+size_t rslx_rms_norm_backward_workspace_bytes(int64_t rows, int32_t cols);
+int32_t rslx_rms_norm_backward(int32_t dtype, const void* dy, int64_t lddy, const void* total, int64_t ldt, int64_t rows,
+                               int32_t cols, const float* weight_or_null, const float* rstd, const void* dtotal_or_null,
+                               int64_t lddt, void* dx_or_null, int64_t lddx, float* dweight_or_null, void* ws,
+                               size_t ws_bytes, void* stream);
+
+/* ---- Muon: momentum whose update is made orthogonal ------------------------------------- */
+
+/* For every matrix [rows, cols] (dense, row-major, fp32; a layer's weights inside a flat parameter buffer among them):
+ *   m_out = momentum m_in + grad,   u = nesterov ? grad + momentum m_out : m_out
+ *   X = u / |u|_F,   `steps` times  X <- a X + (b A + c A^2) X  with A = X X^T      (a, b, c = 3.4445, -4.7750, 2.0315)
+ *   w_out = (1 - lr weight_decay) w_in - lr scale X
+ * (Jordan et al. 2024: quintic Newton-Schulz steps, which bring every singular value near one).  Each product is fp32's in effect:
+ * operands are held as pairs of fp16 values (22 significant bits), sums in fp32.  u = 0 leaves X = 0; a matrix whose u
+ * holds a value that is not finite gets NaN, the others of the call nothing of it.
+ * w_in NULL: 0; m_in NULL: 0; m_out NULL: not kept (w_in = m_in = m_out = NULL, lr = -1: X itself).  w_out may be w_in and m_out
+ * may be m_in; nothing else that is written may overlap what is read or written.  Pointers are aligned to 4 bytes; the descriptions are host memory. */
+#define RSLX_MUON_MAX_MATRICES 32
+#define RSLX_MUON_MAX_DIM 65536
+#define RSLX_MUON_MAX_STEPS 32
+typedef struct rslx_muon_matrix {
+  const float* w_in;
+  float* w_out;
+  const float* grad;
+  const float* m_in;
+  float* m_out;
+  int32_t rows, cols;            /* 1..RSLX_MUON_MAX_DIM */
+  float scale;
+} rslx_muon_matrix;
+typedef struct rslx_muon_cfg {
+  float lr, momentum, weight_decay;
+  int32_t nesterov, steps;       /* steps: 1..RSLX_MUON_MAX_STEPS */
+} rslx_muon_cfg;
+size_t rslx_muon_step_workspace_bytes(const rslx_muon_matrix* matrices, int32_t count, const rslx_muon_cfg* cfg);
+int32_t rslx_muon_step(const rslx_muon_matrix* matrices, int32_t count, const rslx_muon_cfg* cfg, void* ws, size_t ws_bytes,
+                       void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,6 +19,10 @@ __all__ = [
     "LinearAttn", "ATTN_MAX_DIM", "NORM_MAX_COLS", "rslx_linear_attention_workspace_bytes", "rslx_linear_attention",
     "rslx_linear_attention_backward_workspace_bytes", "rslx_linear_attention_backward", "rslx_linear_attention_step",
     "rslx_layer_norm", "rslx_layer_norm_backward_workspace_bytes", "rslx_layer_norm_backward",
+    "GatedRec", "Muon", "rslx_gated_recurrence_workspace_bytes", "rslx_gated_recurrence",
+    "rslx_gated_recurrence_backward_workspace_bytes", "rslx_gated_recurrence_backward", "rslx_gated_recurrence_step",
+    "rslx_rms_norm", "rslx_rms_norm_e4m3", "rslx_rms_norm_backward_workspace_bytes", "rslx_rms_norm_backward",
+    "rslx_muon_step_workspace_bytes", "rslx_muon_step",
 ]
 
 MAX_LAYERS = 8
@@ -38,6 +42,10 @@ EXPORTS = [
     "rslx_ppo_update_recurrent_dc", "rslx_gae_noalloc", "rslx_linear_attention_workspace_bytes", "rslx_linear_attention",
     "rslx_linear_attention_backward_workspace_bytes", "rslx_linear_attention_backward", "rslx_linear_attention_step",
     "rslx_layer_norm", "rslx_layer_norm_backward_workspace_bytes", "rslx_layer_norm_backward",
+    "rslx_gated_recurrence_workspace_bytes", "rslx_gated_recurrence", "rslx_gated_recurrence_backward_workspace_bytes",
+    "rslx_gated_recurrence_backward", "rslx_gated_recurrence_step", "rslx_rms_norm", "rslx_rms_norm_e4m3",
+    "rslx_rms_norm_backward_workspace_bytes", "rslx_rms_norm_backward", "rslx_muon_step_workspace_bytes",
+    "rslx_muon_step",
 ]
 GAE_NOALLOC_MAX_ENVS = 1 << 20
 ATTN_MAX_DIM = 128
@@ -106,6 +114,19 @@ class _CTraceRecord(C.Structure):
 
 class _CSeqView(C.Structure):
     _fields_ = [("data", _vp), ("step", C.c_int64), ("seq", C.c_int64), ("head", C.c_int64)]
+
+
+class _CGatedRec(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("T", C.c_int32), ("N", C.c_int32), ("D", C.c_int32), ("dones", _vp), ("lengths", _vp)]
+
+
+class _CMuonMatrix(C.Structure):
+    _fields_ = [("w_in", _vp), ("w_out", _vp), ("grad", _vp), ("m_in", _vp), ("m_out", _vp), ("rows", C.c_int32), ("cols", C.c_int32),
+                ("scale", C.c_float)]
+
+
+class _CMuonCfg(C.Structure):
+    _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float), ("nesterov", C.c_int32), ("steps", C.c_int32)]
 
 
 class _CLinearAttn(C.Structure):
@@ -186,6 +207,21 @@ _sig("rslx_layer_norm", C.c_int32, [C.c_int32, _vp, C.c_int64, C.c_int64, C.c_in
 _sig("rslx_layer_norm_backward_workspace_bytes", C.c_size_t, [C.c_int64, C.c_int32])
 _sig("rslx_layer_norm_backward", C.c_int32, [C.c_int32, _vp, C.c_int64, _vp, C.c_int64, C.c_int64, C.c_int32, _vp, _vp, _vp, _vp, C.c_int64, _vp,
                                              _vp, _vp, C.c_size_t, _vp])
+_sig("rslx_gated_recurrence_workspace_bytes", C.c_size_t, [_P(_CGatedRec)])
+_sig("rslx_gated_recurrence", C.c_int32, [_P(_CGatedRec), _P(_CSeqView), _P(_CSeqView), _vp, _P(_CSeqView), _vp, _vp, C.c_size_t, _vp])
+_sig("rslx_gated_recurrence_backward_workspace_bytes", C.c_size_t, [_P(_CGatedRec)])
+_sig("rslx_gated_recurrence_backward", C.c_int32, [_P(_CGatedRec), _P(_CSeqView), _P(_CSeqView), _vp, _P(_CSeqView), _vp, _P(_CSeqView),
+                                                   _P(_CSeqView), _vp, _vp, C.c_size_t, _vp])
+_sig("rslx_gated_recurrence_step", C.c_int32, [_P(_CGatedRec), _P(_CSeqView), _P(_CSeqView), _vp, _vp, _vp, _P(_CSeqView), _vp])
+_sig("rslx_rms_norm", C.c_int32, [C.c_int32, _vp, C.c_int64, _vp, C.c_int64, C.c_int64, C.c_int32, _vp, C.c_float, _vp, C.c_int64, _vp, C.c_int64,
+                                  _vp, _vp])
+_sig("rslx_rms_norm_e4m3", C.c_int32, [C.c_int32, _vp, C.c_int64, _vp, C.c_int64, C.c_int64, C.c_int32, _vp, C.c_float, _vp, C.c_int64, _vp,
+                                       C.c_int64, _vp, _vp, _vp])
+_sig("rslx_rms_norm_backward_workspace_bytes", C.c_size_t, [C.c_int64, C.c_int32])
+_sig("rslx_rms_norm_backward", C.c_int32, [C.c_int32, _vp, C.c_int64, _vp, C.c_int64, C.c_int64, C.c_int32, _vp, _vp, _vp, C.c_int64, _vp, C.c_int64,
+                                           _vp, _vp, C.c_size_t, _vp])
+_sig("rslx_muon_step_workspace_bytes", C.c_size_t, [_P(_CMuonMatrix), C.c_int32, _P(_CMuonCfg)])
+_sig("rslx_muon_step", C.c_int32, [_P(_CMuonMatrix), C.c_int32, _P(_CMuonCfg), _vp, C.c_size_t, _vp])
 _sig("rslx_trace_begin", C.c_int32, [C.c_int32])
 _sig("rslx_trace_end", C.c_int32, [_P(_CTraceRecord), C.c_int32, _P(C.c_int32)])
 
@@ -702,6 +738,138 @@ def rslx_layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, ws):
     _check(lib.rslx_layer_norm_backward(code, pd, lddy, px, ldx, rows, cols, _f32("weight", weight, cols), _f32("mean", mean, rows),
                                         _f32("rstd", rstd, rows), pg, lddx, _f32("dweight", dweight, cols), _f32("dbias", dbias, cols), _ptr(ws),
                                         ws.numel() if ws is not None else 0, _stream()), "rslx_layer_norm_backward")
+
+
+class GatedRec:
+    """Sizes of a gated linear recurrence (struct rslx_gated_rec): T steps of N sequences, D channels, in `dtype`; dones uint8 [T, N] and
+    lengths int32 [N] or None."""
+
+    def __init__(self, dtype, T, N, D, dones=None, lengths=None):
+        if dtype not in _DTYPES:
+            raise RslxError("GatedRec: dtype %s is not one of float32, bfloat16, float16" % dtype)
+        for name, t, want, n in (("dones", dones, torch.uint8, T * N), ("lengths", lengths, torch.int32, N)):
+            if t is not None and (t.dtype != want or t.numel() != n):
+                raise RslxError("GatedRec: %s has %d values of %s, %d of %s are needed" % (name, t.numel(), t.dtype, n, want))
+        self.dtype, self.dones, self.lengths = dtype, dones, lengths
+        self.T, self.N, self.D = (_int32(name, n) for name, n in (("T", T), ("N", N), ("D", D)))
+        self._shape = (self.T, self.N, self.D)
+        self.c = _CGatedRec(_DTYPES[dtype], self.T, self.N, self.D, _ptr(dones), _ptr(lengths))
+
+    def view(self, name, t):
+        """t [T, N, D] of any strides with its values side by side -> struct rslx_seq_view."""
+        if t.dtype is not self.dtype or t.shape != self._shape:
+            raise RslxError("%s is %s %s, %s %s is needed" % (name, t.dtype, tuple(t.shape), self.dtype, self._shape))
+        step, seq, one = t.stride()
+        if one != 1 and self.D > 1 and t.numel() > 0:
+            raise RslxError("%s: the values of a row must lie side by side" % name)
+        return _CSeqView(t.data_ptr(), step, seq, 0)
+
+    def state(self, name, t):
+        """t [N, D] float32, contiguous, or None -> address."""
+        return _f32(name, t, self.N * self.D)
+
+
+def rslx_gated_recurrence_workspace_bytes(gr):
+    n = lib.rslx_gated_recurrence_workspace_bytes(C.byref(gr.c))
+    if n == 0:
+        raise RslxError("rslx_gated_recurrence_workspace_bytes: %s" % lib.rslx_last_error().decode())
+    return n
+
+
+def rslx_gated_recurrence(gr, x, g, s0, h, s_last, ws):
+    """x, g, h [T, N, D]; s0, s_last [N, D] float32 or None."""
+    _check(lib.rslx_gated_recurrence(gr.c, gr.view("x", x), gr.view("g", g), gr.state("s0", s0), gr.view("h", h), gr.state("s_last", s_last), _ptr(ws),
+                                     ws.numel() if ws is not None else 0, _stream()), "rslx_gated_recurrence")
+
+
+def rslx_gated_recurrence_backward_workspace_bytes(gr):
+    n = lib.rslx_gated_recurrence_backward_workspace_bytes(C.byref(gr.c))
+    if n == 0:
+        raise RslxError("rslx_gated_recurrence_backward_workspace_bytes: %s" % lib.rslx_last_error().decode())
+    return n
+
+
+def rslx_gated_recurrence_backward(gr, x, g, s0, dh, ds_last, dx, dg, ds0, ws):
+    """Gradients of rslx_gated_recurrence from dh [T, N, D] and ds_last [N, D] (or None)."""
+    _check(lib.rslx_gated_recurrence_backward(gr.c, gr.view("x", x), gr.view("g", g), gr.state("s0", s0), gr.view("dh", dh), gr.state("ds_last", ds_last),
+                                              gr.view("dx", dx), gr.view("dg", dg), gr.state("ds0", ds0), _ptr(ws),
+                                              ws.numel() if ws is not None else 0, _stream()), "rslx_gated_recurrence_backward")
+
+
+def rslx_gated_recurrence_step(gr, x, g, reset, s_in, s_out, h):
+    """One step (gr.T == 1): x, g, h [1, N, D]; reset uint8 of N values or None; s_in (or None), s_out [N, D]."""
+    if reset is not None and (reset.dtype != torch.uint8 or reset.numel() != gr.N):
+        raise RslxError("reset has %d values of %s, %d of uint8 are needed" % (reset.numel(), reset.dtype, gr.N))
+    _check(lib.rslx_gated_recurrence_step(gr.c, gr.view("x", x), gr.view("g", g), _ptr(reset), gr.state("s_in", s_in), gr.state("s_out", s_out),
+                                          gr.view("h", h), _stream()), "rslx_gated_recurrence_step")
+
+
+def rslx_rms_norm(x, residual, weight, eps, total, y, rstd):
+    """x, y [rows, cols], residual and total (x + residual, written) likewise or None; weight [cols] and rstd [rows] float32 or None."""
+    code, dtype, shape = _matrix("x", x)
+    rows, cols = shape
+    (px, ldx), (pr, ldr) = _rows("x", x, dtype, shape), _rows("residual", residual, dtype, shape)
+    (pt, ldt), (py, ldy) = _rows("total", total, dtype, shape), _rows("y", y, dtype, shape)
+    _check(lib.rslx_rms_norm(code, px, ldx, pr, ldr, rows, cols, _f32("weight", weight, cols), eps, pt, ldt, py, ldy, _f32("rstd", rstd, rows),
+                             _stream()), "rslx_rms_norm")
+
+
+def rslx_rms_norm_e4m3(x, residual, weight, eps, total, y, scales, rstd):
+    """As rslx_rms_norm with y in float8_e4m3fn and a scale for each row, scales [rows] float32: the output is scales[:, None] * y."""
+    code, dtype, shape = _matrix("x", x)
+    rows, cols = shape
+    (px, ldx), (pr, ldr) = _rows("x", x, dtype, shape), _rows("residual", residual, dtype, shape)
+    (pt, ldt), (py, ldy) = _rows("total", total, dtype, shape), _rows("y", y, torch.float8_e4m3fn, shape)
+    _check(lib.rslx_rms_norm_e4m3(code, px, ldx, pr, ldr, rows, cols, _f32("weight", weight, cols), eps, pt, ldt, py, ldy,
+                                  _f32("scales", scales, rows), _f32("rstd", rstd, rows), _stream()), "rslx_rms_norm_e4m3")
+
+
+def rslx_rms_norm_backward_workspace_bytes(rows, cols):
+    n = lib.rslx_rms_norm_backward_workspace_bytes(rows, _int32("cols", cols))
+    if n == 0:
+        raise RslxError("rslx_rms_norm_backward_workspace_bytes: %s" % lib.rslx_last_error().decode())
+    return n
+
+
+def rslx_rms_norm_backward(dy, total, weight, rstd, dtotal, dx, dweight, ws):
+    """dy, total, dx [rows, cols], dtotal (the gradient of total) likewise or None; rstd [rows] as rslx_rms_norm leaves it; dx, dweight or None."""
+    code, dtype, shape = _matrix("total", total)
+    rows, cols = shape
+    (pt, ldt), (pd, lddy) = _rows("total", total, dtype, shape), _rows("dy", dy, dtype, shape)
+    (ps, lddt), (pg, lddx) = _rows("dtotal", dtotal, dtype, shape), _rows("dx", dx, dtype, shape)
+    _check(lib.rslx_rms_norm_backward(code, pd, lddy, pt, ldt, rows, cols, _f32("weight", weight, cols), _f32("rstd", rstd, rows), ps, lddt, pg, lddx,
+                                      _f32("dweight", dweight, cols), _ptr(ws), ws.numel() if ws is not None else 0, _stream()),
+           "rslx_rms_norm_backward")
+
+
+class Muon:
+    """Matrices of a Muon step (struct rslx_muon_matrix) and its constants (struct rslx_muon_cfg).  `matrices`: tuples (w_in, w_out, grad, m_in, m_out,
+    scale) of contiguous float32 [rows, cols] (views into flat parameter buffers among them); w_in, m_in and m_out may be None."""
+
+    def __init__(self, matrices, lr, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5):
+        self.matrices = [tuple(m) for m in matrices]
+        self.c = (_CMuonMatrix * max(len(self.matrices), 1))()
+        for i, (w_in, w_out, grad, m_in, m_out, scale) in enumerate(self.matrices):
+            if grad is None or grad.dim() != 2:
+                raise RslxError("Muon: grad of matrix %d is not a matrix" % i)
+            for name, t in (("w_in", w_in), ("w_out", w_out), ("grad", grad), ("m_in", m_in), ("m_out", m_out)):
+                if t is not None and (t.dtype is not torch.float32 or t.shape != grad.shape):
+                    raise RslxError("Muon: %s of matrix %d is %s %s, float32 %s is needed" % (name, i, t.dtype, tuple(t.shape), tuple(grad.shape)))
+            rows, cols = (_int32("a side of matrix %d" % i, n) for n in grad.shape)
+            self.c[i] = _CMuonMatrix(_ptr(w_in), _ptr(w_out), _ptr(grad), _ptr(m_in), _ptr(m_out), rows, cols, scale)
+        self.cfg = _CMuonCfg(lr, momentum, weight_decay, int(bool(nesterov)), _int32("steps", steps))
+
+
+def rslx_muon_step_workspace_bytes(muon):
+    n = lib.rslx_muon_step_workspace_bytes(muon.c, len(muon.matrices), muon.cfg)
+    if n == 0:
+        raise RslxError("rslx_muon_step_workspace_bytes: %s" % lib.rslx_last_error().decode())
+    return n
+
+
+def rslx_muon_step(muon, ws):
+    """One step of every matrix; lr may be changed between steps (muon.cfg.lr)."""
+    _check(lib.rslx_muon_step(muon.c, len(muon.matrices), muon.cfg, _ptr(ws), ws.numel() if ws is not None else 0, _stream()), "rslx_muon_step")
 
 
 def rslx_trace_begin(max_records):

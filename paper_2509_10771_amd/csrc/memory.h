@@ -1,0 +1,76 @@
+// Internal interface between the entry points and the kernels of the operators around a gated memory (gated linear recurrence, root-mean-square
+// norm with the residual's addition, Muon step).  Not part of the public ABI (that is include/rslx.h).
+#pragma once
+
+#include "../../include/rslx.h"
+#include "host.h"
+#include "kernels.h"
+
+namespace rslx {
+
+// ---- gated linear recurrence ----------------------------------------------------------------------------------------
+struct RecMatrix { void* p; int64_t step, seq; };
+struct RecArgs {
+  RecMatrix x, g, h;            // forward; one step: step is not used
+  RecMatrix dh, dx, dg;         // backward
+  int32_t T, N, D;
+  const uint8_t* dones;         // one step: the reset flags
+  const int32_t* lengths;
+  const float* s0;              // or null = 0
+  float* s_last;                // or null
+  const float* ds_last;         // or null = 0
+  float* ds0;                   // or null
+  float* entered;               // backward: the states that steps start from, [T, N, D]
+};
+// Carves the workspace of a call and enters its places.
+void plan_recurrence(host::Carver& c, RecArgs& a, int dtype, bool backward);
+hipError_t launch_recurrence(const RecArgs& a, int dtype, bool backward, hipStream_t stream);
+hipError_t launch_recurrence_step(const RecArgs& a, int dtype, hipStream_t stream);
+
+// ---- root-mean-square norm --------------------------------------------------------------------------------------------
+constexpr int RMS_MAX_BLOCKS = 1024;      // workgroups of a backward launch: each leaves a row of partial sums
+
+struct RmsArgs {
+  const void* x; int64_t ldx;             // forward: x; backward: total
+  const void* residual; int64_t ldr;      // forward: or null; backward: dtotal or null
+  const void* dy; int64_t lddy;           // backward
+  void* total; int64_t ldt;               // forward: or null
+  void* y; int64_t ldy;                   // forward: y; backward: dx or null
+  int64_t rows;
+  int32_t cols;
+  const float* weight;                    // or null: 1
+  float eps;
+  float* scales;                          // forward in 8 bits
+  float* rstd;                            // forward: or null
+  float* partials;                        // backward: [blocks][cols], or null where dweight is not asked for
+  float* dweight;
+};
+int rms_backward_blocks(int64_t rows, int cols);
+hipError_t launch_rms_norm(const RmsArgs& a, int dtype, bool e4m3, hipStream_t stream);
+hipError_t launch_rms_norm_backward(const RmsArgs& a, int dtype, hipStream_t stream);
+
+// ---- Muon step --------------------------------------------------------------------------------------------------------
+// p <= q are a matrix's sides, X [p, q] (the transposed update where the matrix is tall), in 32 x 16 blocks of 64 lanes: see muon.hip.
+struct MuonItem {
+  const float* w_in;
+  float* w_out;
+  const float* grad;
+  const float* m_in;
+  float* m_out;
+  float* u;                     // the update before it is made orthogonal, [rows, cols]
+  double* norm;                 // partial sums of its squares
+  uint16_t *x, *xt[2], *a, *b;  // X; X transposed, two in turn; A = X X^T; a I + b A + c A^2
+  int32_t rows, cols, p, q;
+  float scale;
+  int32_t first;                // of the launch's workgroups
+};
+struct MuonArgs {
+  MuonItem item[RSLX_MUON_MAX_MATRICES];
+  int32_t count;
+  float lr, momentum, decay;
+  int32_t nesterov;
+};
+constexpr int MUON_NORM_BLOCKS = 64;      // workgroups at most that sum a matrix's squares
+hipError_t launch_muon(MuonArgs& a, int steps, hipStream_t stream);
+
+}  // namespace rslx

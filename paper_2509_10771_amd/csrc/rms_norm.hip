@@ -1,0 +1,315 @@
+// Root-mean-square norm over the rows of a matrix with the residual's addition, forward (in the inputs' type or in 8 bits) and backward, gfx950.
+//
+//   z = x + residual,  r = 1 / sqrt(mean z^2 + eps),  y = z r w;      8 bits: s = max |y| / 448,  y8 = y / s
+//   h = z r,  k = dy w:   dx = dtotal + r (k - h mean(k h)),   dw = sum over rows dy h
+//
+// Bound by memory, and built like layer norm: a row is read once into the registers of the TPR lanes that share it, the next one is on its way while
+// this one is reduced, results are written once.  Squares and products are summed in fp32: a lane's values in order, then a fixed tree.
+#include "memory.h"
+#include "norm_rows.h"
+
+namespace rslx {
+
+namespace {
+
+constexpr int RMS_MAX_FORWARD = 2048;         // workgroups of a forward launch: eight for each CU; more rows go round
+constexpr float E4M3_MAX = 448.f;
+
+// The largest of the TPR lanes' values, as the bits of numbers without a sign: a NaN's are above those of every number.
+template <int TPR>
+__device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* lds) {
+  constexpr int IN_WAVE = TPR < 64 ? TPR : 64;
+#pragma unroll
+  for (int o = IN_WAVE / 2; o > 0; o >>= 1) {
+    const uint32_t u = __shfl_xor(v, o, 64);
+    v = u > v ? u : v;
+  }
+  if constexpr (TPR > 64) {
+    constexpr int WAVES = TPR / 64;
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v = lds[w] > v ? lds[w] : v;
+  }
+  return v;
+}
+
+// Four values rounded to e4m3 (nearest even).
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  int p = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, p, true);
+}
+
+template <typename T, int W, int ITEMS, int TPR, bool WHOLE, bool E4M3>
+__global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_kernel(RmsArgs a) {
+  constexpr int ROWS = THREADS_OF<TPR> / TPR;
+  __shared__ float lds[2][TPR > 64 ? TPR / 64 : 1];
+  __shared__ uint32_t lds_max[TPR > 64 ? TPR / 64 : 1];
+  const int lane = threadIdx.x % TPR;
+  const float n = (float)a.cols;
+  const int64_t stride = (int64_t)gridDim.x * ROWS;
+  int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  Pack<T, W> px[ITEMS], pr[ITEMS];
+  auto load = [&](int64_t r) {
+    if (r < a.rows)
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        load_piece<T, W, WHOLE>(px[i], static_cast<const T*>(a.x) + r * a.ldx, (i * TPR + lane) * W, a.cols);
+        if (a.residual) load_piece<T, W, WHOLE>(pr[i], static_cast<const T*>(a.residual) + r * a.ldr, (i * TPR + lane) * W, a.cols);
+      }
+  };
+  load(row);
+  Pack<float, W> w[ITEMS];
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+#pragma unroll
+    for (int k = 0; k < W; ++k) w[i].v[k] = 1.f;
+    if (a.weight) load_piece<float, W, WHOLE>(w[i], a.weight, (i * TPR + lane) * W, a.cols);
+  }
+  // (TPR <= 64: lanes leave the loop in whole rows, and the shuffles stay inside a row; above, the workgroup has one row)
+  for (int turn = 0; row < a.rows; row += stride, turn ^= 1) {
+    float f[ITEMS * W], s[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        float z = to_float(px[i].v[k]);
+        if (a.residual) z += to_float(pr[i].v[k]);
+        f[i * W + k] = in_row<W, WHOLE>((i * TPR + lane) * W, k, a.cols) ? z : 0.f;
+        s[0] += f[i * W + k] * f[i * W + k];
+      }
+    load(row + stride);
+    if (a.total) {
+      T* to = static_cast<T*>(a.total) + row * a.ldt;
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        Pack<T, W> out;
+#pragma unroll
+        for (int k = 0; k < W; ++k) out.v[k] = from_float<T>(f[i * W + k]);
+        store_piece<T, W, WHOLE>(out, to, (i * TPR + lane) * W, a.cols);
+      }
+    }
+    row_sum<TPR, 1>(s, lds[turn]);
+    const float rstd = 1.f / sqrtf(s[0] / n + a.eps);
+    if constexpr (!E4M3) {
+      T* y = static_cast<T*>(a.y) + row * a.ldy;
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        Pack<T, W> out;
+#pragma unroll
+        for (int k = 0; k < W; ++k) out.v[k] = from_float<T>(f[i * W + k] * rstd * w[i].v[k]);
+        store_piece<T, W, WHOLE>(out, y, (i * TPR + lane) * W, a.cols);
+      }
+    } else {
+      uint32_t most = 0;
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+          f[i * W + k] = in_row<W, WHOLE>((i * TPR + lane) * W, k, a.cols) ? f[i * W + k] * rstd * w[i].v[k] : 0.f;
+          const uint32_t bits = __float_as_uint(f[i * W + k]) & 0x7fffffffu;
+          most = bits > most ? bits : most;
+        }
+      most = row_max<TPR>(most, lds_max);
+      float scale = __uint_as_float(most) / E4M3_MAX;
+      if (scale < 0x1p-126f) scale = 0x1p-126f;
+      const float inv = 1.f / scale;
+      uint8_t* y = static_cast<uint8_t*>(a.y) + row * a.ldy;
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        Pack<uint8_t, W> out;
+#pragma unroll
+        for (int k = 0; k < W; k += 4) {
+          const float* v = f + i * W + k;
+          const uint32_t four = pack_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+          __builtin_memcpy(out.v + k, &four, 4);
+        }
+        store_piece<uint8_t, W, WHOLE>(out, y, (i * TPR + lane) * W, a.cols);
+      }
+      if (lane == 0) a.scales[row] = scale;
+    }
+    if (lane == 0 && a.rstd) a.rstd[row] = rstd;
+  }
+}
+
+// A lane's columns stay the same from row to row, and their gradients of the weight add up in its registers; what the workgroup holds in the end is one
+// row of partial sums, which norm_fold_kernel adds up in a fixed order.  Long rows (1024 lanes have 128 registers each) are not loaded ahead.
+template <typename T, int W, int ITEMS, int TPR, bool WHOLE>
+__global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_backward_kernel(RmsArgs a) {
+  constexpr int ROWS = THREADS_OF<TPR> / TPR;
+  constexpr bool AHEAD = TPR < 1024 || ITEMS * W <= 8;
+  __shared__ float lds[2][TPR > 64 ? TPR / 64 : 1];
+  __shared__ float join[ROWS > 1 ? (ROWS - 1) * TPR * ITEMS * W : 1];
+  const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const float inv = 1.f / (float)a.cols;
+  const int64_t stride = (int64_t)gridDim.x * ROWS;
+  int64_t row = (int64_t)blockIdx.x * ROWS + sub;
+  Pack<T, W> px[ITEMS], pd[ITEMS], pt[ITEMS];
+  float rstd = 0.f;
+  auto load = [&](int64_t r) {
+    if (r < a.rows) {
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        load_piece<T, W, WHOLE>(px[i], static_cast<const T*>(a.x) + r * a.ldx, (i * TPR + lane) * W, a.cols);
+        load_piece<T, W, WHOLE>(pd[i], static_cast<const T*>(a.dy) + r * a.lddy, (i * TPR + lane) * W, a.cols);
+        if (a.y && a.residual) load_piece<T, W, WHOLE>(pt[i], static_cast<const T*>(a.residual) + r * a.ldr, (i * TPR + lane) * W, a.cols);
+      }
+      rstd = a.rstd[r];
+    }
+  };
+  if (AHEAD) load(row);
+  Pack<float, W> w[ITEMS];
+  float dw[ITEMS * W];
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      w[i].v[k] = 1.f;
+      dw[i * W + k] = 0.f;
+    }
+    if (a.weight) load_piece<float, W, WHOLE>(w[i], a.weight, (i * TPR + lane) * W, a.cols);
+  }
+  for (int turn = 0; row < a.rows; row += stride, turn ^= 1) {
+    if (!AHEAD) load(row);
+    float s[1] = {0.f}, h[ITEMS * W], g[ITEMS * W];
+    const float scale = rstd;
+    Pack<T, W> t[ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      t[i] = pt[i];
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        const int x = i * W + k;
+        const bool here = in_row<W, WHOLE>((i * TPR + lane) * W, k, a.cols);
+        const float d = here ? to_float(pd[i].v[k]) : 0.f;
+        h[x] = here ? to_float(px[i].v[k]) * scale : 0.f;
+        g[x] = here ? d * w[i].v[k] : 0.f;
+        dw[x] += d * h[x];
+        s[0] += g[x] * h[x];
+      }
+    }
+    if (AHEAD) load(row + stride);
+    if (a.y) {
+      row_sum<TPR, 1>(s, lds[turn]);
+      const float mean = s[0] * inv;
+      T* dx = static_cast<T*>(a.y) + row * a.ldy;
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        Pack<T, W> out;
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+          float v = scale * (g[i * W + k] - h[i * W + k] * mean);
+          if (a.residual) v += to_float(t[i].v[k]);
+          out.v[k] = from_float<T>(v);
+        }
+        store_piece<T, W, WHOLE>(out, dx, (i * TPR + lane) * W, a.cols);
+      }
+    }
+  }
+  if (!a.partials) return;
+  if constexpr (ROWS > 1) {
+    if (sub > 0)
+#pragma unroll
+      for (int i = 0; i < ITEMS * W; ++i) join[((sub - 1) * ITEMS * W + i) * TPR + lane] = dw[i];
+    __syncthreads();
+    if (sub == 0)
+      for (int r = 0; r < ROWS - 1; ++r)
+#pragma unroll
+        for (int i = 0; i < ITEMS * W; ++i) dw[i] += join[(r * ITEMS * W + i) * TPR + lane];
+  }
+  if (sub == 0) {
+    float* to = a.partials + (int64_t)blockIdx.x * a.cols;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      Pack<float, W> out;
+#pragma unroll
+      for (int k = 0; k < W; ++k) out.v[k] = dw[i * W + k];
+      store_piece<float, W, WHOLE>(out, to, (i * TPR + lane) * W, a.cols);
+    }
+  }
+}
+
+enum RmsKind { RMS_FORWARD, RMS_FORWARD_E4M3, RMS_BACKWARD };
+
+template <typename T, int W, int ITEMS, int TPR, bool WHOLE>
+void run_rms(const RmsArgs& a, RmsKind kind, int blocks, hipStream_t s) {
+  const dim3 grid(blocks), block(THREADS_OF<TPR>);
+  if (kind == RMS_FORWARD) hipLaunchKernelGGL((rms_norm_kernel<T, W, ITEMS, TPR, WHOLE, false>), grid, block, 0, s, a);
+  else if (kind == RMS_FORWARD_E4M3) hipLaunchKernelGGL((rms_norm_kernel<T, W, ITEMS, TPR, WHOLE, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((rms_norm_backward_kernel<T, W, ITEMS, TPR, WHOLE>), grid, block, 0, s, a);
+}
+
+template <typename T, bool WHOLE>
+void dispatch_rms(const RmsArgs& a, RmsKind kind, int blocks, hipStream_t s) {
+  constexpr int W = 16 / (int)sizeof(T);
+  const NormShape f = norm_shape(a.cols, W);
+  switch (f.tpr * 32 + f.items) {
+    case 16 * 32 + 1: run_rms<T, W, 1, 16, WHOLE>(a, kind, blocks, s); break;
+    case 32 * 32 + 1: run_rms<T, W, 1, 32, WHOLE>(a, kind, blocks, s); break;
+    case 64 * 32 + 1: run_rms<T, W, 1, 64, WHOLE>(a, kind, blocks, s); break;
+    case 64 * 32 + 2: run_rms<T, W, 2, 64, WHOLE>(a, kind, blocks, s); break;
+    case 256 * 32 + 1: run_rms<T, W, 1, 256, WHOLE>(a, kind, blocks, s); break;
+    case 256 * 32 + 2: run_rms<T, W, 2, 256, WHOLE>(a, kind, blocks, s); break;
+    case 512 * 32 + 2: run_rms<T, W, 2, 512, WHOLE>(a, kind, blocks, s); break;
+    case 1024 * 32 + 2: run_rms<T, W, 2, 1024, WHOLE>(a, kind, blocks, s); break;
+    default:
+      if constexpr (W == 4) run_rms<T, W, 4, 1024, WHOLE>(a, kind, blocks, s);      // (16384 values are 2048 loads of eight)
+      break;
+  }
+}
+
+template <typename T>
+void run_type(const RmsArgs& a, RmsKind kind, int blocks, hipStream_t s) {
+  // whether every row of every matrix is a number of whole, aligned loads
+  constexpr int W = 16 / (int)sizeof(T);
+  auto fits = [&](const void* p, int64_t ld, int bytes) { return !p || ((reinterpret_cast<uintptr_t>(p) % bytes) == 0 && ld % W == 0); };
+  const bool whole = a.cols % W == 0 && fits(a.x, a.ldx, 16) && fits(a.residual, a.ldr, 16) && fits(a.dy, a.lddy, 16) && fits(a.total, a.ldt, 16) &&
+                     fits(a.y, a.ldy, kind == RMS_FORWARD_E4M3 ? W : 16);
+  whole ? dispatch_rms<T, true>(a, kind, blocks, s) : dispatch_rms<T, false>(a, kind, blocks, s);
+}
+
+hipError_t run(const RmsArgs& a, int dtype, RmsKind kind, int blocks, hipStream_t s) {
+  if (dtype == RSLX_F32) run_type<float>(a, kind, blocks, s);
+  else if (dtype == RSLX_BF16) run_type<bf16_t>(a, kind, blocks, s);
+  else run_type<__half>(a, kind, blocks, s);
+  return hipGetLastError();
+}
+
+int64_t sets_of(int64_t rows, int cols, int w) {
+  const int64_t per = norm_rows_per_block(norm_shape(cols, w).tpr);
+  return rows / per + (rows % per != 0);
+}
+
+}  // namespace
+
+// Workgroups of a backward launch: as for layer norm.
+int rms_backward_blocks(int64_t rows, int cols) {
+  const int64_t sets = sets_of(rows, cols, 4);
+  const int64_t most = cols <= 512 ? RMS_MAX_BLOCKS : RMS_MAX_BLOCKS / 2;
+  const int64_t many = sets / 4 < most ? sets / 4 : most, few = sets < 256 ? sets : 256;
+  const int64_t blocks = many > few ? many : few;
+  return (int)(blocks < 1 ? 1 : blocks);
+}
+
+hipError_t launch_rms_norm(const RmsArgs& a, int dtype, bool e4m3, hipStream_t stream) {
+  const double n = (double)a.rows * a.cols, size = dtype == RSLX_F32 ? 4 : 2;
+  TraceScope trace(stream, e4m3 ? "rms_norm_e4m3" : "rms_norm", 6 * n, n * (size * (1 + (a.residual != nullptr) + (a.total != nullptr)) + (e4m3 ? 1 : size)));
+  const int64_t sets = sets_of(a.rows, a.cols, dtype == RSLX_F32 ? 4 : 8);
+  return run(a, dtype, e4m3 ? RMS_FORWARD_E4M3 : RMS_FORWARD, (int)(sets < RMS_MAX_FORWARD ? sets : RMS_MAX_FORWARD), stream);
+}
+
+hipError_t launch_rms_norm_backward(const RmsArgs& a, int dtype, hipStream_t stream) {
+  const double n = (double)a.rows * a.cols, size = dtype == RSLX_F32 ? 4 : 2;
+  const int blocks = rms_backward_blocks(a.rows, a.cols);
+  {
+    TraceScope trace(stream, "rms_norm_backward", 10 * n, n * size * (2 + (a.residual != nullptr) + (a.y != nullptr)));
+    const hipError_t e = run(a, dtype, RMS_BACKWARD, blocks, stream);
+    if (e != hipSuccess) return e;
+  }
+  if (!a.partials) return hipSuccess;
+  TraceScope trace(stream, "rms_norm_fold", (double)blocks * a.cols, 4.0 * blocks * a.cols);
+  hipLaunchKernelGGL(norm_fold_kernel, dim3((a.cols + 15) / 16, 1), dim3(16 * FOLD_LANES), 0, stream, a.partials, blocks, a.cols, a.dweight, nullptr);
+  return hipGetLastError();
+}
+
+}  // namespace rslx
