@@ -1,7 +1,14 @@
 // Gated linear recurrence, gfx950.
 //
 //   f = sigmoid(g),  h_t = f_t keep_{t-1} h_{t-1} + (1 - f_t) x_t
-//   d_t = dh_t + keep_t f_{t+1} d_{t+1},  dx = (1 - f) d,  dg = f (1 - f) d (keep_{t-1} h_{t-1} - x)
+//   q_t = f_t (dh_t + keep_t q_{t+1}),  d_t = dh_t + keep_t q_{t+1},  dx = (1 - f) d,  dg = f (1 - f) d (keep_{t-1} h_{t-1} - x)
+//
+// Both directions are scans of maps s -> A s + B, whose compositions are such maps again; an episode's end is the map that forgets s, held as a flag of its
+// own, so that no 0 times infinity arises.  A lane takes LANE_STEPS steps of four channels into registers and composes their maps; 16 lanes side by side
+// read 64 channels, 128 to 256 bytes of a row; the wavefront's four sets of lanes and the workgroup's wavefronts compose theirs through shuffles and
+// LDS; then every lane walks its steps again from the state that enters them.  Every value is read once and every result written once, as long as a
+// workgroup's steps hold the sequence, or channels are many enough for workgroups to go along whole sequences (forward).  Otherwise sequences
+// are cut into pieces: one launch leaves every piece's map, a second (a lane per channel) the states between the pieces, a third makes the results.
 #include "memory.h"
 #include "typed.h"
 
@@ -10,98 +17,514 @@ namespace rslx {
 namespace {
 
 constexpr int REC_THREADS = 256;
+constexpr int W = 4;                      // channels of a lane
+constexpr int ROW = 16;                   // lanes side by side
+constexpr int TILE = W * ROW;             // channels of a workgroup
+constexpr int SETS = 64 / ROW;            // sets of lanes of a wavefront, one after another in time
 
-// sigmoid(g) and 1 - sigmoid(g), each with its own digits: one is e / (1 + e), the other 1 / (1 + e), of e = exp(-|g|) <= 1.
+// sigmoid(g) and 1 - sigmoid(g), each with its own digits: one is e / (1 + e), the other 1 / (1 + e), of e = exp(-|g|) <= 1.  The exponential is that of
+// the product -|g| log2(e) in two parts: the rounded one for the instruction, what rounding left as a factor.  exp(-128) is zero in fp32.
 __device__ __forceinline__ void gate(float g, float& f, float& rest) {
-  const float e = expf(-fabsf(g)), high = 1.f / (1.f + e), low = e * high;
+  constexpr float LOG2E = 1.44269504f, LOG2E_REST = 1.92596299e-8f, LN2 = 0.693147181f;
+  const float a = fabsf(g), m = a > 128.f ? 128.f : a, p = -m * LOG2E, left = fmaf(-m, LOG2E, -p) - m * LOG2E_REST;
+  float e = __builtin_amdgcn_exp2f(p);
+  e = fmaf(e, left * LN2, e);
+  const float high = __builtin_amdgcn_rcpf(1.f + e), low = e * high;
   f = g >= 0.f ? high : low;
   rest = g >= 0.f ? low : high;
+  if (g != g) f = rest = g;
 }
 
 template <typename T> __device__ __forceinline__ T* row_of(const RecMatrix& m, int64_t t, int64_t n) {
   return static_cast<T*>(m.p) + t * m.step + n * m.seq;
 }
 
-template <typename T, bool BACKWARD>
-__global__ __launch_bounds__(REC_THREADS) void recurrence_kernel(RecArgs a) {
-  const int64_t c = (int64_t)blockIdx.x * REC_THREADS + threadIdx.x;
-  if (c >= (int64_t)a.N * a.D) return;
-  const int n = (int)(c / a.D), d = (int)(c % a.D);
-  int len = a.T;
+struct Four { float v[W]; };
+__device__ __forceinline__ Four all(float x) { return {{x, x, x, x}}; }
+
+// s -> A s + B, or s -> B where an episode ends inside.
+struct Map {
+  Four a, b;
+  int cut;
+  __device__ __forceinline__ Four operator()(const Four& s) const {
+    Four r;
+#pragma unroll
+    for (int k = 0; k < W; ++k) r.v[k] = cut ? b.v[k] : fmaf(a.v[k], s.v[k], b.v[k]);
+    return r;
+  }
+  // this one behind `first`
+  __device__ __forceinline__ void after(const Map& first) {
+    b = (*this)(first.b);
+#pragma unroll
+    for (int k = 0; k < W; ++k) a.v[k] *= first.a.v[k];
+    cut |= first.cut;
+  }
+};
+__device__ __forceinline__ Map same() { return {all(1.f), all(0.f), 0}; }
+
+// The map of another lane.
+template <bool UP>
+__device__ __forceinline__ Map from_lane(const Map& m, int distance) {
+  Map r;
+#pragma unroll
+  for (int k = 0; k < W; ++k) {
+    r.a.v[k] = UP ? __shfl_up(m.a.v[k], distance, 64) : __shfl_down(m.a.v[k], distance, 64);
+    r.b.v[k] = UP ? __shfl_up(m.b.v[k], distance, 64) : __shfl_down(m.b.v[k], distance, 64);
+  }
+  r.cut = UP ? __shfl_up(m.cut, distance, 64) : __shfl_down(m.cut, distance, 64);
+  return r;
+}
+
+// Maps of a workgroup's wavefronts.
+template <int WAVES>
+struct WaveMaps {
+  float4 a[WAVES][ROW], b[WAVES][ROW];
+  int cut[WAVES];
+  __device__ __forceinline__ void put(int wave, int lane, const Map& m) {
+    a[wave][lane] = *reinterpret_cast<const float4*>(&m.a);
+    b[wave][lane] = *reinterpret_cast<const float4*>(&m.b);
+    if (lane == 0) cut[wave] = m.cut;
+  }
+  __device__ __forceinline__ Map get(int wave, int lane) const {
+    Map m;
+    *reinterpret_cast<float4*>(&m.a) = a[wave][lane];
+    *reinterpret_cast<float4*>(&m.b) = b[wave][lane];
+    m.cut = cut[wave];
+    return m;
+  }
+};
+
+// Every set of lanes has the map of its steps; `s` is the state in front of the first (FORWARD) or behind the last one of the workgroup's steps.  Returns the
+// state in front of (behind) the lane's own, and leaves the one at the other end in s.  `maps` is free again after the next such call with other maps.
+template <int WAVES, bool FORWARD>
+__device__ __forceinline__ Four enter(Map m, Four& s, WaveMaps<WAVES>& maps) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & (ROW - 1);
+#pragma unroll
+  for (int o = ROW; o < 64; o *= 2) {
+    const Map other = from_lane<FORWARD>(m, o);
+    if (FORWARD ? lane >= o : lane + o < 64) m.after(other);
+  }
+  const Map before = from_lane<FORWARD>(m, ROW);
+  const bool first = FORWARD ? lane < ROW : lane >= 64 - ROW, last = FORWARD ? lane >= 64 - ROW : lane < ROW;
+  Four mine = s;
+  if constexpr (WAVES > 1) {
+    if (last) maps.put(wave, col, m);
+    __syncthreads();
+#pragma unroll 2
+    for (int i = 0; i < WAVES; ++i) {
+      const int w = FORWARD ? i : WAVES - 1 - i;
+      if (w == wave) mine = s;
+      s = maps.get(w, col)(s);
+    }
+  } else {
+    const Four end = m(s);
+#pragma unroll
+    for (int k = 0; k < W; ++k) s.v[k] = __shfl(end.v[k], (FORWARD ? 64 - ROW : 0) + col, 64);
+  }
+  return first ? mine : before(mine);
+}
+
+// The map of all of the workgroup's steps, from those of its sets of lanes.
+template <int WAVES, bool FORWARD>
+__device__ __forceinline__ Map whole(Map m, WaveMaps<WAVES>& maps) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & (ROW - 1);
+#pragma unroll
+  for (int o = ROW; o < 64; o *= 2) {
+    const Map other = from_lane<FORWARD>(m, o);
+    if (FORWARD ? lane >= o : lane + o < 64) m.after(other);
+  }
+  if (FORWARD ? lane >= 64 - ROW : lane < ROW) maps.put(wave, col, m);
+  __syncthreads();
+  m = maps.get(FORWARD ? 0 : WAVES - 1, col);
+#pragma unroll 1
+  for (int i = 1; i < WAVES; ++i) {
+    Map next = maps.get(FORWARD ? i : WAVES - 1 - i, col);
+    next.after(m);
+    m = next;
+  }
+  return m;
+}
+
+// A workgroup's place: a tile of channels of a sequence, a piece of the steps.
+struct Place {
+  int64_t n;
+  int d, len, piece;
+};
+__device__ __forceinline__ Place place_of(const RecArgs& a) {
+  const int tiles = (a.D + TILE - 1) / TILE;
+  const int64_t all_tiles = (int64_t)a.N * tiles, at = blockIdx.x % all_tiles;
+  Place p;
+  p.piece = (int)(blockIdx.x / all_tiles);
+  p.n = at / tiles;
+  p.d = (int)(at % tiles) * TILE + (threadIdx.x & (ROW - 1)) * W;
+  p.len = a.T;
   if (a.lengths) {
-    len = a.lengths[n];
-    len = len < 0 ? 0 : len > a.T ? a.T : len;
+    const int len = a.lengths[p.n];
+    p.len = len < 0 ? 0 : len > a.T ? a.T : len;
   }
-  float h = a.s0 ? a.s0[c] : 0.f;
-  for (int64_t t = 0; t < len; ++t) {
-    float f, rest;
-    gate(to_float(row_of<T>(a.g, t, n)[d]), f, rest);
-    if (BACKWARD) a.entered[t * a.N * a.D + c] = h;
-    h = f * h + rest * to_float(row_of<T>(a.x, t, n)[d]);
-    if (!BACKWARD) row_of<T>(a.h, t, n)[d] = from_float<T>(h);
-    if (a.dones && a.dones[t * a.N + n]) h = 0.f;
+  return p;
+}
+
+template <bool WHOLE>
+__device__ __forceinline__ Four load_state(const float* s, const RecArgs& a, const Place& p) {
+  Pack<float, W> v;
+#pragma unroll
+  for (int k = 0; k < W; ++k) v.v[k] = 0.f;
+  if (s) load_piece<float, W, WHOLE>(v, s + p.n * a.D, p.d, a.D);
+  return *reinterpret_cast<const Four*>(&v);
+}
+template <bool WHOLE>
+__device__ __forceinline__ void store_state(float* s, const RecArgs& a, const Place& p, const Four& f) {
+  if (s) store_piece<float, W, WHOLE>(*reinterpret_cast<const Pack<float, W>*>(&f), s + p.n * a.D, p.d, a.D);
+}
+// A piece's entry of a workspace array [pieces, N, D rounded up to four].
+__device__ __forceinline__ float4* piece_at(float* base, const RecArgs& a, const Place& p) {
+  return reinterpret_cast<float4*>(base + ((int64_t)p.piece * a.N + p.n) * ((a.D + W - 1) / W * W) + p.d);
+}
+
+// A lane's steps: gates, and the part (1 - f) x of the new state.  Steps that do not exist hand the state on.
+template <typename T, int L, bool WHOLE>
+struct Steps {
+  float f[L][W], v[L][W];
+  uint32_t ends;
+  __device__ __forceinline__ void load(const RecArgs& a, const Place& p, int64_t t0) {
+    Pack<T, W> px[L], pg[L];
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (t0 + i < p.len) {
+        load_piece<T, W, WHOLE>(pg[i], row_of<T>(a.g, t0 + i, p.n), p.d, a.D);
+        load_piece<T, W, WHOLE>(px[i], row_of<T>(a.x, t0 + i, p.n), p.d, a.D);
+      }
+    ends = 0;
+    if (a.dones)
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (t0 + i < p.len && a.dones[(t0 + i) * a.N + p.n]) ends |= 1u << i;
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        float rest;
+        gate(to_float(pg[i].v[k]), f[i][k], rest);
+        v[i][k] = rest * to_float(px[i].v[k]);
+        if (t0 + i >= p.len) f[i][k] = 1.f, v[i][k] = 0.f;
+      }
   }
-  if (!BACKWARD) {
-    for (int64_t t = len; t < a.T; ++t) row_of<T>(a.h, t, n)[d] = from_float<T>(0.f);
-    if (a.s_last) a.s_last[c] = h;
+  __device__ __forceinline__ Map map() const {
+    Map m = same();
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const int end = ends >> i & 1;
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        m.b.v[k] = end ? 0.f : fmaf(f[i][k], m.b.v[k], v[i][k]);
+        m.a.v[k] *= f[i][k];
+      }
+      m.cut |= end;
+    }
+    return m;
+  }
+};
+
+// Forward: a workgroup goes along its piece, WAVES * SETS * L steps at a time.  MAPS: no results, the piece's map alone.
+template <typename T, int L, int WAVES, bool WHOLE, bool MAPS>
+__global__ __launch_bounds__(WAVES * 64) void recurrence_kernel(RecArgs a) {
+  __shared__ WaveMaps<WAVES> maps[2];
+  const Place p = place_of(a);
+  const int slot = threadIdx.x / ROW;
+  const int64_t begin = (int64_t)p.piece * a.piece_steps, end = begin + a.piece_steps < a.T ? begin + a.piece_steps : a.T;
+  Four s = all(0.f);
+  Map piece = same();
+  if (!MAPS) {
+    if (a.pieces > 1 && p.d < a.D) *reinterpret_cast<float4*>(&s) = *piece_at(a.into, a, p);
+    else if (a.pieces == 1) s = load_state<WHOLE>(a.s0, a, p);
+  }
+  int turn = 0;
+  for (int64_t t = begin; t < end; t += WAVES * SETS * L, turn ^= 1) {
+    const int64_t t0 = t + slot * L;
+    Steps<T, L, WHOLE> x;
+    x.load(a, p, t0);
+    Map m = x.map();
+    if constexpr (MAPS) {
+      Map next = whole<WAVES, true>(m, maps[turn]);
+      next.after(piece);
+      piece = next;
+      continue;
+    }
+    Four h = enter<WAVES, true>(m, s, maps[turn]);
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      Pack<T, W> out;
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        h.v[k] = fmaf(x.f[i][k], h.v[k], x.v[i][k]);
+        out.v[k] = from_float<T>(t0 + i < p.len ? h.v[k] : 0.f);
+        if (x.ends >> i & 1) h.v[k] = 0.f;
+      }
+      if (t0 + i < a.T) store_piece<T, W, WHOLE>(out, row_of<T>(a.h, t0 + i, p.n), p.d, a.D);
+    }
+  }
+  if (threadIdx.x >= ROW || p.d >= a.D) return;
+  if constexpr (MAPS) {
+    *piece_at(a.gates, a, p) = *reinterpret_cast<const float4*>(&piece.a);
+    *piece_at(a.into, a, p) = *reinterpret_cast<const float4*>(&piece.b);
+    if (p.d == 0) a.cuts[(int64_t)p.piece * a.N + p.n] = piece.cut;
+  } else if (p.piece == a.pieces - 1) {
+    store_state<WHOLE>(a.s_last, a, p, s);
+  }
+}
+
+// Backward: a piece is the steps that a workgroup holds at once.  MAPS: the piece's maps of both directions (whose gates' product is the same).
+template <typename T, int L, int WAVES, bool WHOLE, bool MAPS>
+__global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(RecArgs a) {
+  __shared__ WaveMaps<WAVES> maps[2];
+  const Place p = place_of(a);
+  const int slot = threadIdx.x / ROW;
+  const int64_t t0 = (int64_t)p.piece * (WAVES * SETS * L) + slot * L;
+  Pack<T, W> px[L], pg[L], pd[L];
+#pragma unroll
+  for (int i = 0; i < L; ++i)
+    if (t0 + i < p.len) {
+      load_piece<T, W, WHOLE>(pg[i], row_of<T>(a.g, t0 + i, p.n), p.d, a.D);
+      load_piece<T, W, WHOLE>(px[i], row_of<T>(a.x, t0 + i, p.n), p.d, a.D);
+      load_piece<T, W, WHOLE>(pd[i], row_of<T>(a.dh, t0 + i, p.n), p.d, a.D);
+    }
+  uint32_t ends = 0;
+  if (a.dones)
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (t0 + i < p.len && a.dones[(t0 + i) * a.N + p.n]) ends |= 1u << i;
+  float f[L][W], rest[L][W];
+  Map m = same(), up = same();
+#pragma unroll
+  for (int i = 0; i < L; ++i)
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      gate(to_float(pg[i].v[k]), f[i][k], rest[i][k]);
+      const bool here = t0 + i < p.len;
+      if (!here) f[i][k] = 1.f;
+      const float next = here ? fmaf(f[i][k], m.b.v[k], rest[i][k] * to_float(px[i].v[k])) : m.b.v[k];
+      m.b.v[k] = ends >> i & 1 ? 0.f : next;
+      m.a.v[k] *= f[i][k];
+    }
+#pragma unroll
+  for (int i = L - 1; i >= 0; --i)
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      const float q = ends >> i & 1 ? 0.f : up.b.v[k];
+      up.b.v[k] = t0 + i < p.len ? f[i][k] * (q + to_float(pd[i].v[k])) : q;
+    }
+  up.a = m.a;
+  up.cut = m.cut = ends != 0;
+  Four s = all(0.f), q = all(0.f);
+  if (!MAPS) {
+    if (a.pieces > 1) {
+      if (p.d < a.D) {
+        *reinterpret_cast<float4*>(&s) = *piece_at(a.into, a, p);
+        *reinterpret_cast<float4*>(&q) = *piece_at(a.back, a, p);
+      }
+    } else {
+      s = load_state<WHOLE>(a.s0, a, p);
+      q = load_state<WHOLE>(a.ds_last, a, p);
+    }
+  }
+  if constexpr (MAPS) {
+    m = whole<WAVES, true>(m, maps[0]);
+    up = whole<WAVES, false>(up, maps[1]);
+    if (threadIdx.x >= ROW || p.d >= a.D) return;
+    *piece_at(a.gates, a, p) = *reinterpret_cast<const float4*>(&m.a);
+    *piece_at(a.into, a, p) = *reinterpret_cast<const float4*>(&m.b);
+    *piece_at(a.back, a, p) = *reinterpret_cast<const float4*>(&up.b);
+    if (p.d == 0) a.cuts[(int64_t)p.piece * a.N + p.n] = m.cut;
     return;
   }
-  for (int64_t t = len; t < a.T; ++t) row_of<T>(a.dx, t, n)[d] = row_of<T>(a.dg, t, n)[d] = from_float<T>(0.f);
-  float down = a.ds_last ? a.ds_last[c] : 0.f;
-  for (int64_t t = len - 1; t >= 0; --t) {
-    float f, rest;
-    gate(to_float(row_of<T>(a.g, t, n)[d]), f, rest);
-    if (a.dones && a.dones[t * a.N + n]) down = 0.f;
-    down += to_float(row_of<T>(a.dh, t, n)[d]);
-    row_of<T>(a.dx, t, n)[d] = from_float<T>(rest * down);
-    row_of<T>(a.dg, t, n)[d] = from_float<T>(f * rest * down * (a.entered[t * a.N * a.D + c] - to_float(row_of<T>(a.x, t, n)[d])));
-    down *= f;
+  Four h = enter<WAVES, true>(m, s, maps[0]), down = enter<WAVES, false>(up, q, maps[1]);
+  if (p.piece == 0 && threadIdx.x < ROW) store_state<WHOLE>(a.ds0, a, p, q);
+  float in[L][W];                           // the states that the steps start from
+#pragma unroll
+  for (int i = 0; i < L; ++i)
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      in[i][k] = h.v[k];
+      h.v[k] = ends >> i & 1 ? 0.f : t0 + i < p.len ? fmaf(f[i][k], h.v[k], rest[i][k] * to_float(px[i].v[k])) : h.v[k];
+    }
+#pragma unroll
+  for (int i = L - 1; i >= 0; --i) {
+    Pack<T, W> dx, dg;
+    const bool here = t0 + i < p.len;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      if (ends >> i & 1) down.v[k] = 0.f;
+      const float d = down.v[k] + to_float(pd[i].v[k]), by = rest[i][k] * d;
+      dx.v[k] = from_float<T>(here ? by : 0.f);
+      dg.v[k] = from_float<T>(here ? f[i][k] * by * (in[i][k] - to_float(px[i].v[k])) : 0.f);
+      if (here) down.v[k] = f[i][k] * d;
+    }
+    if (t0 + i < a.T) {
+      store_piece<T, W, WHOLE>(dx, row_of<T>(a.dx, t0 + i, p.n), p.d, a.D);
+      store_piece<T, W, WHOLE>(dg, row_of<T>(a.dg, t0 + i, p.n), p.d, a.D);
+    }
   }
-  if (a.ds0) a.ds0[c] = down;
+}
+
+// The states between the pieces, in place of the pieces' maps: the one in front of each (into), and behind each on the way back (back, blockIdx.y = 1).
+constexpr int JOIN_AHEAD = 8;
+__global__ __launch_bounds__(64) void recurrence_join_kernel(RecArgs a) {
+  const int width = (a.D + W - 1) / W * W;
+  const int64_t channels = (int64_t)a.N * width, c = (int64_t)blockIdx.x * 64 + threadIdx.x;
+  if (c >= channels) return;
+  const int64_t n = c / width;
+  const int d = (int)(c % width);
+  const bool back = blockIdx.y != 0;
+  const float* start = back ? a.ds_last : a.s0;
+  float s = start && d < a.D ? start[n * a.D + d] : 0.f;
+  float* at = back ? a.back : a.into;
+  for (int first = 0; first < a.pieces; first += JOIN_AHEAD) {
+    float scale[JOIN_AHEAD], add[JOIN_AHEAD];
+    int cut[JOIN_AHEAD];
+#pragma unroll
+    for (int i = 0; i < JOIN_AHEAD; ++i)
+      if (first + i < a.pieces) {
+        const int64_t piece = back ? a.pieces - 1 - first - i : first + i;
+        scale[i] = a.gates[piece * channels + c];
+        add[i] = at[piece * channels + c];
+        cut[i] = a.cuts[piece * a.N + n];
+      }
+#pragma unroll
+    for (int i = 0; i < JOIN_AHEAD; ++i)
+      if (first + i < a.pieces) {
+        const int64_t piece = back ? a.pieces - 1 - first - i : first + i;
+        at[piece * channels + c] = s;
+        s = cut[i] ? add[i] : fmaf(scale[i], s, add[i]);
+      }
+  }
+}
+
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(REC_THREADS) void recurrence_step_kernel(RecArgs a) {
+  const int per = (a.D + W - 1) / W;
+  const int64_t c = (int64_t)blockIdx.x * REC_THREADS + threadIdx.x;
+  if (c >= (int64_t)a.N * per) return;
+  Place p;
+  p.n = c / per;
+  p.d = (int)(c % per) * W;
+  Pack<T, W> px, pg, out;
+  load_piece<T, W, WHOLE>(pg, row_of<T>(a.g, 0, p.n), p.d, a.D);
+  load_piece<T, W, WHOLE>(px, row_of<T>(a.x, 0, p.n), p.d, a.D);
+  Four s = load_state<WHOLE>(a.dones && a.dones[p.n] ? nullptr : a.s0, a, p);
+#pragma unroll
+  for (int k = 0; k < W; ++k) {
+    float f, rest;
+    gate(to_float(pg.v[k]), f, rest);
+    s.v[k] = fmaf(f, s.v[k], rest * to_float(px.v[k]));
+    out.v[k] = from_float<T>(s.v[k]);
+  }
+  store_state<WHOLE>(a.s_last, a, p, s);
+  store_piece<T, W, WHOLE>(out, row_of<T>(a.h, 0, p.n), p.d, a.D);
+}
+
+// How the steps are shared out: wavefronts of a workgroup, steps of a lane; see plan_recurrence.
+enum RecShape { FORWARD_1 = 0, FORWARD_8, BACKWARD_1, BACKWARD_4, BACKWARD_16 };
+constexpr int LANE_STEPS[] = {4, 4, 8, 8, 4}, SHAPE_WAVES[] = {1, 8, 1, 4, 16};
+int steps_of(int shape) { return LANE_STEPS[shape] * SHAPE_WAVES[shape] * SETS; }
+
+template <typename T, bool WHOLE, bool MAPS>
+void run_shape(const RecArgs& a, hipStream_t s) {
+  const unsigned grid = (unsigned)((int64_t)a.N * ((a.D + TILE - 1) / TILE) * a.pieces);
+#define RUN(shape, kernel) \
+  case shape: hipLaunchKernelGGL((kernel<T, LANE_STEPS[shape], SHAPE_WAVES[shape], WHOLE, MAPS>), dim3(grid), dim3(SHAPE_WAVES[shape] * 64), 0, s, a); break
+  switch (a.shape) {
+    RUN(FORWARD_8, recurrence_kernel);
+    RUN(BACKWARD_16, recurrence_backward_kernel);
+    default:
+      if constexpr (!MAPS) switch (a.shape) {
+        RUN(FORWARD_1, recurrence_kernel);
+        RUN(BACKWARD_1, recurrence_backward_kernel);
+        RUN(BACKWARD_4, recurrence_backward_kernel);
+      }
+  }
+#undef RUN
+}
+
+// Whether every row of every matrix is a number of whole, aligned loads.
+bool rec_whole(const RecArgs& a, int size) {
+  auto fits = [&](const RecMatrix& m) { return !m.p || (reinterpret_cast<uintptr_t>(m.p) % (W * size) == 0 && m.step % W == 0 && m.seq % W == 0); };
+  return a.D % W == 0 && fits(a.x) && fits(a.g) && fits(a.h) && fits(a.dh) && fits(a.dx) && fits(a.dg);
 }
 
 template <typename T>
-__global__ __launch_bounds__(REC_THREADS) void recurrence_step_kernel(RecArgs a) {
-  const int64_t c = (int64_t)blockIdx.x * REC_THREADS + threadIdx.x;
-  if (c >= (int64_t)a.N * a.D) return;
-  const int n = (int)(c / a.D), d = (int)(c % a.D);
-  float f, rest;
-  gate(to_float(row_of<T>(a.g, 0, n)[d]), f, rest);
-  const float s = a.s0 && !(a.dones && a.dones[n]) ? a.s0[c] : 0.f;
-  const float h = f * s + rest * to_float(row_of<T>(a.x, 0, n)[d]);
-  a.s_last[c] = h;
-  row_of<T>(a.h, 0, n)[d] = from_float<T>(h);
+void run_type(const RecArgs& a, bool maps, hipStream_t s) {
+  const bool whole = rec_whole(a, (int)sizeof(T));
+  if (maps) whole ? run_shape<T, true, true>(a, s) : run_shape<T, false, true>(a, s);
+  else whole ? run_shape<T, true, false>(a, s) : run_shape<T, false, false>(a, s);
+}
+
+void run(const RecArgs& a, int dtype, bool maps, hipStream_t s) {
+  if (dtype == RSLX_F32) run_type<float>(a, maps, s);
+  else if (dtype == RSLX_BF16) run_type<bf16_t>(a, maps, s);
+  else run_type<__half>(a, maps, s);
 }
 
 }  // namespace
 
+// Forward, a wavefront along each sequence and 64 channels where that fills the GPU or one is enough for the steps; otherwise eight, in pieces where even
+// these are few.  Backward, the smallest workgroup that holds the sequence, the largest in pieces where none does.
 void plan_recurrence(host::Carver& c, RecArgs& a, int, bool backward) {
-  if (backward) a.entered = c.take<float>((size_t)a.T * a.N * a.D);
+  const int64_t tiles = (int64_t)a.N * ((a.D + TILE - 1) / TILE);
+  a.pieces = 1;
+  a.piece_steps = a.T;
+  if (backward) {
+    a.shape = a.T <= steps_of(BACKWARD_1) ? BACKWARD_1 : a.T <= steps_of(BACKWARD_4) ? BACKWARD_4 : BACKWARD_16;
+    a.piece_steps = steps_of(a.shape);
+  } else {
+    a.shape = a.T <= steps_of(FORWARD_1) || tiles >= 2048 ? FORWARD_1 : FORWARD_8;
+    if (a.shape == FORWARD_8 && tiles > 0) {
+      const int64_t blocks = ((int64_t)a.T + steps_of(FORWARD_8) - 1) / steps_of(FORWARD_8), want = (1023 + tiles) / tiles;
+      const int64_t each = tiles >= 256 || want < 2 ? blocks : (blocks + want - 1) / want;
+      a.piece_steps = each * steps_of(FORWARD_8);
+    }
+  }
+  if (a.piece_steps > 0 && a.piece_steps < a.T) a.pieces = (int32_t)((a.T + a.piece_steps - 1) / a.piece_steps);
+  if (a.pieces > 1) {
+    const size_t states = (size_t)a.pieces * a.N * ((a.D + W - 1) / W * W);
+    a.gates = c.take<float>(states);
+    a.into = c.take<float>(states);
+    if (backward) a.back = c.take<float>(states);
+    a.cuts = c.take<int32_t>((size_t)a.pieces * a.N);
+  }
 }
 
 hipError_t launch_recurrence(const RecArgs& a, int dtype, bool backward, hipStream_t stream) {
   const double n = (double)a.T * a.N * a.D, size = dtype == RSLX_F32 ? 4 : 2;
+  if (a.pieces > 1) {
+    {
+      TraceScope trace(stream, backward ? "recurrence_backward_maps" : "recurrence_maps", (backward ? 20 : 16) * n, (backward ? 3 : 2) * n * size);
+      run(a, dtype, true, stream);
+    }
+    const double states = (double)a.pieces * a.N * a.D;
+    TraceScope trace(stream, "recurrence_join", 2 * states, (backward ? 16 : 12) * states);
+    const int64_t channels = (int64_t)a.N * ((a.D + W - 1) / W * W);
+    hipLaunchKernelGGL(recurrence_join_kernel, dim3((unsigned)((channels + 63) / 64), backward ? 2 : 1), dim3(64), 0, stream, a);
+  }
   TraceScope trace(stream, backward ? "recurrence_backward" : "recurrence", (backward ? 25 : 10) * n, (backward ? 5 : 3) * n * size);
-  const dim3 grid((unsigned)(((int64_t)a.N * a.D + REC_THREADS - 1) / REC_THREADS)), block(REC_THREADS);
-#define RUN(T)                                                                                            \
-  do {                                                                                                    \
-    if (backward) hipLaunchKernelGGL((recurrence_kernel<T, true>), grid, block, 0, stream, a);            \
-    else hipLaunchKernelGGL((recurrence_kernel<T, false>), grid, block, 0, stream, a);                    \
-  } while (0)
-  if (dtype == RSLX_F32) RUN(float);
-  else if (dtype == RSLX_BF16) RUN(bf16_t);
-  else RUN(__half);
-#undef RUN
+  run(a, dtype, false, stream);
   return hipGetLastError();
 }
 
 hipError_t launch_recurrence_step(const RecArgs& a, int dtype, hipStream_t stream) {
   const double n = (double)a.N * a.D, size = dtype == RSLX_F32 ? 4 : 2;
   TraceScope trace(stream, "recurrence_step", 10 * n, (3 * size + 8) * n);
-  const dim3 grid((unsigned)(((int64_t)a.N * a.D + REC_THREADS - 1) / REC_THREADS)), block(REC_THREADS);
-  if (dtype == RSLX_F32) hipLaunchKernelGGL((recurrence_step_kernel<float>), grid, block, 0, stream, a);
-  else if (dtype == RSLX_BF16) hipLaunchKernelGGL((recurrence_step_kernel<bf16_t>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((recurrence_step_kernel<__half>), grid, block, 0, stream, a);
+  const dim3 grid((unsigned)(((int64_t)a.N * ((a.D + W - 1) / W) + REC_THREADS - 1) / REC_THREADS)), block(REC_THREADS);
+  const bool whole = rec_whole(a, (int)size);
+#define RUN(T)                                                                                          \
+  do {                                                                                                  \
+    if (whole) hipLaunchKernelGGL((recurrence_step_kernel<T, true>), grid, block, 0, stream, a);        \
+    else hipLaunchKernelGGL((recurrence_step_kernel<T, false>), grid, block, 0, stream, a);             \
+  } while (0)
+  if (dtype == RSLX_F32) RUN(float);
+  else if (dtype == RSLX_BF16) RUN(bf16_t);
+  else RUN(__half);
+#undef RUN
   return hipGetLastError();
 }
 

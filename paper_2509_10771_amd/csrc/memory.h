@@ -20,7 +20,11 @@ struct RecArgs {
   float* s_last;                // or null
   const float* ds_last;         // or null = 0
   float* ds0;                   // or null
-  float* entered;               // backward: the states that steps start from, [T, N, D]
+  int32_t shape;                // how the steps are shared out (gated_recurrence.hip)
+  int32_t pieces;               // of a sequence, of piece_steps steps each
+  int64_t piece_steps;
+  float *gates, *into, *back;   // more than one piece: the maps s -> gates s + into of every piece, then the states in front of them, and likewise
+  int32_t* cuts;                // (back) on the way from the end; whether an episode ends inside; [pieces, N, D rounded up to four], [pieces, N]
 };
 // Carves the workspace of a call and enters its places.
 void plan_recurrence(host::Carver& c, RecArgs& a, int dtype, bool backward);
