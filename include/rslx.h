@@ -558,7 +558,7 @@ int32_t rslx_layer_norm_backward(int32_t dtype, const void* dy, int64_t lddy, co
 /* Per sequence n and channel d, with f = sigmoid(g):
  *   h_t = f_t keep_{t-1} h_{t-1} + (1 - f_t) x_t,   h_{-1} = s0 (0 if NULL), keep_{-1} = 1
  * keep_t = 0 where dones[t, n] is set, s_last = keep_{T-1} h_{T-1}, and lengths: all as in linear attention above.  1 - f is
- * sigmoid(-g), so gates next to one keep their digits; g = +inf holds the state and -inf takes x as it is.
+ * sigmoid(-g), so gates next to one keep their digits; g = +inf holds the state, g below -87 counts as -87 (f = 1.6e-38).
  * x, g and h (and their gradients) are matrices [T, N, D]: views whose `head` is not used, under the conditions above.
  * A step's values reach no earlier step and no other episode, whatever they are; an infinite state may be a NaN some
  * steps later, where the product of the gates between is zero in fp32. */

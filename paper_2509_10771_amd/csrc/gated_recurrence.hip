@@ -22,17 +22,24 @@ constexpr int ROW = 16;                   // lanes side by side
 constexpr int TILE = W * ROW;             // channels of a workgroup
 constexpr int SETS = 64 / ROW;            // sets of lanes of a wavefront, one after another in time
 
-// sigmoid(g) and 1 - sigmoid(g), each with its own digits: one is e / (1 + e), the other 1 / (1 + e), of e = exp(-|g|) <= 1.  The exponential is that of
-// the product -|g| log2(e) in two parts: the rounded one for the instruction, what rounding left as a factor.  exp(-128) is zero in fp32.
+// f = sigmoid(g) = 1 / (1 + E) and 1 - f = E f, of E = exp(-g): each keeps its own digits.  Below -87, where f leaves fp32's normal numbers, g counts as -87.
+// For fp32 the exponential is that of the product g log2(e) in two parts, the rounded one for the instruction and what rounding left as a factor.  16-bit gates
+// do without the second: E is off by up to |g| 2^-24 more then, where the type's own half step is |g| 2^-9 or 2^-12 (and the instructions count: these
+// walks are bound by them; with the factor 8192 steps of 4 environments took 10 us more of 90).
+template <typename T>
 __device__ __forceinline__ void gate(float g, float& f, float& rest) {
   constexpr float LOG2E = 1.44269504f, LOG2E_REST = 1.92596299e-8f, LN2 = 0.693147181f;
-  const float a = fabsf(g), m = a > 128.f ? 128.f : a, p = -m * LOG2E, left = fmaf(-m, LOG2E, -p) - m * LOG2E_REST;
-  float e = __builtin_amdgcn_exp2f(p);
-  e = fmaf(e, left * LN2, e);
-  const float high = __builtin_amdgcn_rcpf(1.f + e), low = e * high;
-  f = g >= 0.f ? high : low;
-  rest = g >= 0.f ? low : high;
-  if (g != g) f = rest = g;
+  const float low = g < -87.f ? -87.f : g;
+  float e;
+  if constexpr (sizeof(T) == 4) {
+    const float m = low > 128.f ? 128.f : low, p = -m * LOG2E, left = fmaf(-m, LOG2E, -p) - m * LOG2E_REST;      // (exp(-128) is zero in fp32)
+    e = __builtin_amdgcn_exp2f(p);
+    e = fmaf(e, left * LN2, e);
+  } else {
+    e = __builtin_amdgcn_exp2f(low * -LOG2E);
+  }
+  f = __builtin_amdgcn_rcpf(1.f + e);
+  rest = e * f;
 }
 
 template <typename T> __device__ __forceinline__ T* row_of(const RecMatrix& m, int64_t t, int64_t n) {
@@ -182,56 +189,53 @@ __device__ __forceinline__ float4* piece_at(float* base, const RecArgs& a, const
   return reinterpret_cast<float4*>(base + ((int64_t)p.piece * a.N + p.n) * ((a.D + W - 1) / W * W) + p.d);
 }
 
-// A lane's steps: gates, and the part (1 - f) x of the new state.  Steps that do not exist hand the state on.
-template <typename T, int L, bool WHOLE>
-struct Steps {
-  float f[L][W], v[L][W];
-  uint32_t ends;
-  __device__ __forceinline__ void load(const RecArgs& a, const Place& p, int64_t t0) {
-    Pack<T, W> px[L], pg[L];
-#pragma unroll
-    for (int i = 0; i < L; ++i)
-      if (t0 + i < p.len) {
-        load_piece<T, W, WHOLE>(pg[i], row_of<T>(a.g, t0 + i, p.n), p.d, a.D);
-        load_piece<T, W, WHOLE>(px[i], row_of<T>(a.x, t0 + i, p.n), p.d, a.D);
-      }
-    ends = 0;
-    if (a.dones)
-#pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (t0 + i < p.len && a.dones[(t0 + i) * a.N + p.n]) ends |= 1u << i;
-#pragma unroll
-    for (int i = 0; i < L; ++i)
-#pragma unroll
-      for (int k = 0; k < W; ++k) {
-        float rest;
-        gate(to_float(pg[i].v[k]), f[i][k], rest);
-        v[i][k] = rest * to_float(px[i].v[k]);
-        if (t0 + i >= p.len) f[i][k] = 1.f, v[i][k] = 0.f;
-      }
-  }
-  __device__ __forceinline__ Map map() const {
-    Map m = same();
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      const int end = ends >> i & 1;
-#pragma unroll
-      for (int k = 0; k < W; ++k) {
-        m.b.v[k] = end ? 0.f : fmaf(f[i][k], m.b.v[k], v[i][k]);
-        m.a.v[k] *= f[i][k];
-      }
-      m.cut |= end;
+// A matrix as a lane sees it: its row of step i behind the wavefront's first.  WHOLE: rows are whole, aligned loads, and what differs between lanes fits 32 bits:
+// the address is a common one and an offset that stays, for any i; lanes beyond the last channel read the first one's.
+template <typename T, bool WHOLE>
+struct Rows {
+  char* base;
+  uint32_t offset;
+  T* mine;
+  int64_t step;
+  __device__ __forceinline__ Rows(const RecMatrix& m, const RecArgs& a, const Place& p, int64_t t, int ahead) : step(m.step) {
+    if constexpr (WHOLE) {
+      base = reinterpret_cast<char*>(static_cast<T*>(m.p) + t * m.step + p.n * m.seq);
+      offset = ((uint32_t)ahead * (uint32_t)m.step + (uint32_t)(p.d < a.D ? p.d : 0)) * (uint32_t)sizeof(T);
+    } else {
+      mine = static_cast<T*>(m.p) + (t + ahead) * m.step + p.n * m.seq;
     }
-    return m;
+  }
+  __device__ __forceinline__ void load(Pack<T, W>& v, int i, const RecArgs& a, const Place& p) const {
+    if constexpr (WHOLE) v = *reinterpret_cast<const Pack<T, W>*>(base + i * step * (int64_t)sizeof(T) + offset);
+    else load_piece<T, W, false>(v, mine + i * step, p.d, a.D);
+  }
+  __device__ __forceinline__ void store(const Pack<T, W>& v, int i, const RecArgs& a, const Place& p) const {
+    if constexpr (WHOLE) {
+      if (p.d < a.D) *reinterpret_cast<Pack<T, W>*>(base + i * step * (int64_t)sizeof(T) + offset) = v;
+    } else {
+      store_piece<T, W, false>(v, mine + i * step, p.d, a.D);
+    }
   }
 };
 
-// Forward: a workgroup goes along its piece, WAVES * SETS * L steps at a time.  MAPS: no results, the piece's map alone.
+// Which of the lane's steps from t0 on end an episode.
+template <int L>
+__device__ __forceinline__ uint32_t ends_of(const RecArgs& a, const Place& p, int64_t t0) {
+  uint32_t ends = 0;
+  if (a.dones)
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (t0 + i < p.len && a.dones[(t0 + i) * a.N + p.n]) ends |= 1u << i;
+  return ends;
+}
+
+// Forward: a workgroup goes along its piece, WAVES * SETS * L steps at a time.  MAPS: no results, the piece's map alone.  Where every step of a wavefront exists and
+// none ends an episode (`plain`), nothing is asked step by step.
 template <typename T, int L, int WAVES, bool WHOLE, bool MAPS>
 __global__ __launch_bounds__(WAVES * 64) void recurrence_kernel(RecArgs a) {
   __shared__ WaveMaps<WAVES> maps[2];
   const Place p = place_of(a);
-  const int slot = threadIdx.x / ROW;
+  const int ahead = threadIdx.x / ROW * L;
   const int64_t begin = (int64_t)p.piece * a.piece_steps, end = begin + a.piece_steps < a.T ? begin + a.piece_steps : a.T;
   Four s = all(0.f);
   Map piece = same();
@@ -241,10 +245,56 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_kernel(RecArgs a) {
   }
   int turn = 0;
   for (int64_t t = begin; t < end; t += WAVES * SETS * L, turn ^= 1) {
-    const int64_t t0 = t + slot * L;
-    Steps<T, L, WHOLE> x;
-    x.load(a, p, t0);
-    Map m = x.map();
+    const int64_t t0 = t + ahead;
+    const Rows<T, WHOLE> rx(a.x, a, p, t, ahead), rg(a.g, a, p, t, ahead);
+    Pack<T, W> px[L], pg[L];
+    const uint32_t ends = ends_of<L>(a, p, t0);
+    const bool plain = __all(ends == 0 && t0 + L <= p.len);
+    float f[L][W], v[L][W];
+    Map m = same();
+    auto gates = [&]() {
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+          float rest;
+          gate<T>(to_float(pg[i].v[k]), f[i][k], rest);
+          v[i][k] = rest * to_float(px[i].v[k]);
+        }
+    };
+    if (plain) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        rg.load(pg[i], i, a, p);
+        rx.load(px[i], i, a, p);
+      }
+      gates();
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+          m.b.v[k] = i == 0 ? v[0][k] : fmaf(f[i][k], m.b.v[k], v[i][k]);
+          m.a.v[k] = i == 0 ? f[0][k] : m.a.v[k] * f[i][k];
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (t0 + i < p.len) {
+          rg.load(pg[i], i, a, p);
+          rx.load(px[i], i, a, p);
+        }
+      gates();
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+          // steps that do not exist hand the state on
+          if (t0 + i >= p.len) f[i][k] = 1.f, v[i][k] = 0.f;
+          m.b.v[k] = ends >> i & 1 ? 0.f : fmaf(f[i][k], m.b.v[k], v[i][k]);
+          m.a.v[k] *= f[i][k];
+        }
+      m.cut = ends != 0;
+    }
     if constexpr (MAPS) {
       Map next = whole<WAVES, true>(m, maps[turn]);
       next.after(piece);
@@ -252,16 +302,30 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_kernel(RecArgs a) {
       continue;
     }
     Four h = enter<WAVES, true>(m, s, maps[turn]);
+    const Rows<T, WHOLE> rh(a.h, a, p, t, ahead);
+    if (plain) {
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      Pack<T, W> out;
+      for (int i = 0; i < L; ++i) {
+        Pack<T, W> out;
 #pragma unroll
-      for (int k = 0; k < W; ++k) {
-        h.v[k] = fmaf(x.f[i][k], h.v[k], x.v[i][k]);
-        out.v[k] = from_float<T>(t0 + i < p.len ? h.v[k] : 0.f);
-        if (x.ends >> i & 1) h.v[k] = 0.f;
+        for (int k = 0; k < W; ++k) {
+          h.v[k] = fmaf(f[i][k], h.v[k], v[i][k]);
+          out.v[k] = from_float<T>(h.v[k]);
+        }
+        rh.store(out, i, a, p);
       }
-      if (t0 + i < a.T) store_piece<T, W, WHOLE>(out, row_of<T>(a.h, t0 + i, p.n), p.d, a.D);
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        Pack<T, W> out;
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+          h.v[k] = fmaf(f[i][k], h.v[k], v[i][k]);
+          out.v[k] = from_float<T>(t0 + i < p.len ? h.v[k] : 0.f);
+          if (ends >> i & 1) h.v[k] = 0.f;
+        }
+        if (t0 + i < a.T) rh.store(out, i, a, p);
+      }
     }
   }
   if (threadIdx.x >= ROW || p.d >= a.D) return;
@@ -279,55 +343,68 @@ template <typename T, int L, int WAVES, bool WHOLE, bool MAPS>
 __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(RecArgs a) {
   __shared__ WaveMaps<WAVES> maps[2];
   const Place p = place_of(a);
-  const int slot = threadIdx.x / ROW;
-  const int64_t t0 = (int64_t)p.piece * (WAVES * SETS * L) + slot * L;
+  const int ahead = threadIdx.x / ROW * L;
+  const int64_t t = (int64_t)p.piece * (WAVES * SETS * L), t0 = t + ahead;
+  const Rows<T, WHOLE> rx(a.x, a, p, t, ahead), rg(a.g, a, p, t, ahead), rd(a.dh, a, p, t, ahead);
   Pack<T, W> px[L], pg[L], pd[L];
-#pragma unroll
-  for (int i = 0; i < L; ++i)
-    if (t0 + i < p.len) {
-      load_piece<T, W, WHOLE>(pg[i], row_of<T>(a.g, t0 + i, p.n), p.d, a.D);
-      load_piece<T, W, WHOLE>(px[i], row_of<T>(a.x, t0 + i, p.n), p.d, a.D);
-      load_piece<T, W, WHOLE>(pd[i], row_of<T>(a.dh, t0 + i, p.n), p.d, a.D);
-    }
-  uint32_t ends = 0;
-  if (a.dones)
-#pragma unroll
-    for (int i = 0; i < L; ++i)
-      if (t0 + i < p.len && a.dones[(t0 + i) * a.N + p.n]) ends |= 1u << i;
+  const uint32_t ends = ends_of<L>(a, p, t0);
+  const bool plain = __all(ends == 0 && t0 + L <= p.len);
   float f[L][W], rest[L][W];
   Map m = same(), up = same();
+  auto gates = [&]() {
 #pragma unroll
-  for (int i = 0; i < L; ++i)
+    for (int i = 0; i < L; ++i)
 #pragma unroll
-    for (int k = 0; k < W; ++k) {
-      gate(to_float(pg[i].v[k]), f[i][k], rest[i][k]);
-      const bool here = t0 + i < p.len;
-      if (!here) f[i][k] = 1.f;
-      const float next = here ? fmaf(f[i][k], m.b.v[k], rest[i][k] * to_float(px[i].v[k])) : m.b.v[k];
-      m.b.v[k] = ends >> i & 1 ? 0.f : next;
-      m.a.v[k] *= f[i][k];
+      for (int k = 0; k < W; ++k) gate<T>(to_float(pg[i].v[k]), f[i][k], rest[i][k]);
+  };
+  if (plain) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      rg.load(pg[i], i, a, p);
+      rx.load(px[i], i, a, p);
+      rd.load(pd[i], i, a, p);
     }
+    gates();
 #pragma unroll
-  for (int i = L - 1; i >= 0; --i)
+    for (int i = 0; i < L; ++i)
 #pragma unroll
-    for (int k = 0; k < W; ++k) {
-      const float q = ends >> i & 1 ? 0.f : up.b.v[k];
-      up.b.v[k] = t0 + i < p.len ? f[i][k] * (q + to_float(pd[i].v[k])) : q;
-    }
-  up.a = m.a;
-  up.cut = m.cut = ends != 0;
-  Four s = all(0.f), q = all(0.f);
-  if (!MAPS) {
-    if (a.pieces > 1) {
-      if (p.d < a.D) {
-        *reinterpret_cast<float4*>(&s) = *piece_at(a.into, a, p);
-        *reinterpret_cast<float4*>(&q) = *piece_at(a.back, a, p);
+      for (int k = 0; k < W; ++k) {
+        const float v = rest[i][k] * to_float(px[i].v[k]);
+        m.b.v[k] = i == 0 ? v : fmaf(f[i][k], m.b.v[k], v);
+        m.a.v[k] = i == 0 ? f[0][k] : m.a.v[k] * f[i][k];
       }
-    } else {
-      s = load_state<WHOLE>(a.s0, a, p);
-      q = load_state<WHOLE>(a.ds_last, a, p);
-    }
+#pragma unroll
+    for (int i = L - 1; i >= 0; --i)
+#pragma unroll
+      for (int k = 0; k < W; ++k) up.b.v[k] = f[i][k] * (i == L - 1 ? to_float(pd[i].v[k]) : up.b.v[k] + to_float(pd[i].v[k]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (t0 + i < p.len) {
+        rg.load(pg[i], i, a, p);
+        rx.load(px[i], i, a, p);
+        rd.load(pd[i], i, a, p);
+      } else {
+        // steps that do not exist hand both states on
+#pragma unroll
+        for (int k = 0; k < W; ++k) px[i].v[k] = pd[i].v[k] = pg[i].v[k] = from_float<T>(0.f);
+      }
+    gates();
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        if (t0 + i >= p.len) f[i][k] = 1.f, rest[i][k] = 0.f;
+        m.b.v[k] = ends >> i & 1 ? 0.f : fmaf(f[i][k], m.b.v[k], rest[i][k] * to_float(px[i].v[k]));
+        m.a.v[k] *= f[i][k];
+      }
+#pragma unroll
+    for (int i = L - 1; i >= 0; --i)
+#pragma unroll
+      for (int k = 0; k < W; ++k) up.b.v[k] = f[i][k] * ((ends >> i & 1 ? 0.f : up.b.v[k]) + to_float(pd[i].v[k]));
+    m.cut = up.cut = ends != 0;
   }
+  up.a = m.a;
   if constexpr (MAPS) {
     m = whole<WAVES, true>(m, maps[0]);
     up = whole<WAVES, false>(up, maps[1]);
@@ -338,31 +415,44 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(RecArgs
     if (p.d == 0) a.cuts[(int64_t)p.piece * a.N + p.n] = m.cut;
     return;
   }
+  Four s = all(0.f), q = all(0.f);
+  if (a.pieces > 1) {
+    if (p.d < a.D) {
+      *reinterpret_cast<float4*>(&s) = *piece_at(a.into, a, p);
+      *reinterpret_cast<float4*>(&q) = *piece_at(a.back, a, p);
+    }
+  } else {
+    s = load_state<WHOLE>(a.s0, a, p);
+    q = load_state<WHOLE>(a.ds_last, a, p);
+  }
   Four h = enter<WAVES, true>(m, s, maps[0]), down = enter<WAVES, false>(up, q, maps[1]);
   if (p.piece == 0 && threadIdx.x < ROW) store_state<WHOLE>(a.ds0, a, p, q);
-  float in[L][W];                           // the states that the steps start from
+  float in[L][W];                           // f (1 - f) (h - x), of the states h that the steps start from
 #pragma unroll
   for (int i = 0; i < L; ++i)
 #pragma unroll
     for (int k = 0; k < W; ++k) {
-      in[i][k] = h.v[k];
-      h.v[k] = ends >> i & 1 ? 0.f : t0 + i < p.len ? fmaf(f[i][k], h.v[k], rest[i][k] * to_float(px[i].v[k])) : h.v[k];
+      const float x = to_float(px[i].v[k]);
+      in[i][k] = f[i][k] * (h.v[k] - x);
+      h.v[k] = fmaf(f[i][k], h.v[k], rest[i][k] * x);
+      if (!plain && (ends >> i & 1)) h.v[k] = 0.f;
     }
+  const Rows<T, WHOLE> rdx(a.dx, a, p, t, ahead), rdg(a.dg, a, p, t, ahead);
 #pragma unroll
   for (int i = L - 1; i >= 0; --i) {
     Pack<T, W> dx, dg;
-    const bool here = t0 + i < p.len;
 #pragma unroll
     for (int k = 0; k < W; ++k) {
-      if (ends >> i & 1) down.v[k] = 0.f;
+      if (!plain && (ends >> i & 1)) down.v[k] = 0.f;
       const float d = down.v[k] + to_float(pd[i].v[k]), by = rest[i][k] * d;
+      const bool here = plain || t0 + i < p.len;
       dx.v[k] = from_float<T>(here ? by : 0.f);
-      dg.v[k] = from_float<T>(here ? f[i][k] * by * (in[i][k] - to_float(px[i].v[k])) : 0.f);
-      if (here) down.v[k] = f[i][k] * d;
+      dg.v[k] = from_float<T>(here ? by * in[i][k] : 0.f);
+      down.v[k] = f[i][k] * d;
     }
-    if (t0 + i < a.T) {
-      store_piece<T, W, WHOLE>(dx, row_of<T>(a.dx, t0 + i, p.n), p.d, a.D);
-      store_piece<T, W, WHOLE>(dg, row_of<T>(a.dg, t0 + i, p.n), p.d, a.D);
+    if (plain || t0 + i < a.T) {
+      rdx.store(dx, i, a, p);
+      rdg.store(dg, i, a, p);
     }
   }
 }
@@ -415,7 +505,7 @@ __global__ __launch_bounds__(REC_THREADS) void recurrence_step_kernel(RecArgs a)
 #pragma unroll
   for (int k = 0; k < W; ++k) {
     float f, rest;
-    gate(to_float(pg.v[k]), f, rest);
+    gate<T>(to_float(pg.v[k]), f, rest);
     s.v[k] = fmaf(f, s.v[k], rest * to_float(px.v[k]));
     out.v[k] = from_float<T>(s.v[k]);
   }
@@ -424,8 +514,8 @@ __global__ __launch_bounds__(REC_THREADS) void recurrence_step_kernel(RecArgs a)
 }
 
 // How the steps are shared out: wavefronts of a workgroup, steps of a lane; see plan_recurrence.
-enum RecShape { FORWARD_1 = 0, FORWARD_8, BACKWARD_1, BACKWARD_4, BACKWARD_16 };
-constexpr int LANE_STEPS[] = {4, 4, 8, 8, 4}, SHAPE_WAVES[] = {1, 8, 1, 4, 16};
+enum RecShape { FORWARD_1 = 0, FORWARD_4, BACKWARD_1, BACKWARD_4 };
+constexpr int LANE_STEPS[] = {4, 8, 8, 8}, SHAPE_WAVES[] = {1, 4, 1, 4};
 int steps_of(int shape) { return LANE_STEPS[shape] * SHAPE_WAVES[shape] * SETS; }
 
 template <typename T, bool WHOLE, bool MAPS>
@@ -434,21 +524,24 @@ void run_shape(const RecArgs& a, hipStream_t s) {
 #define RUN(shape, kernel) \
   case shape: hipLaunchKernelGGL((kernel<T, LANE_STEPS[shape], SHAPE_WAVES[shape], WHOLE, MAPS>), dim3(grid), dim3(SHAPE_WAVES[shape] * 64), 0, s, a); break
   switch (a.shape) {
-    RUN(FORWARD_8, recurrence_kernel);
-    RUN(BACKWARD_16, recurrence_backward_kernel);
+    RUN(FORWARD_4, recurrence_kernel);
+    RUN(BACKWARD_4, recurrence_backward_kernel);
     default:
       if constexpr (!MAPS) switch (a.shape) {
         RUN(FORWARD_1, recurrence_kernel);
         RUN(BACKWARD_1, recurrence_backward_kernel);
-        RUN(BACKWARD_4, recurrence_backward_kernel);
       }
   }
 #undef RUN
 }
 
-// Whether every row of every matrix is a number of whole, aligned loads.
+// Whether every row of every matrix is a number of whole, aligned loads, and the rows of a workgroup's steps lie within 2^31 bytes, upwards.
 bool rec_whole(const RecArgs& a, int size) {
-  auto fits = [&](const RecMatrix& m) { return !m.p || (reinterpret_cast<uintptr_t>(m.p) % (W * size) == 0 && m.step % W == 0 && m.seq % W == 0); };
+  const int64_t MOST = steps_of(BACKWARD_4);      // steps that a workgroup holds at once, at most
+  auto fits = [&](const RecMatrix& m) {
+    return !m.p || (reinterpret_cast<uintptr_t>(m.p) % (W * size) == 0 && m.step % W == 0 && m.seq % W == 0 && m.step >= 0 &&
+                    m.step < ((int64_t)1 << 31) / MOST / size - a.D);
+  };
   return a.D % W == 0 && fits(a.x) && fits(a.g) && fits(a.h) && fits(a.dh) && fits(a.dx) && fits(a.dg);
 }
 
@@ -474,14 +567,14 @@ void plan_recurrence(host::Carver& c, RecArgs& a, int, bool backward) {
   a.pieces = 1;
   a.piece_steps = a.T;
   if (backward) {
-    a.shape = a.T <= steps_of(BACKWARD_1) ? BACKWARD_1 : a.T <= steps_of(BACKWARD_4) ? BACKWARD_4 : BACKWARD_16;
+    a.shape = a.T <= steps_of(BACKWARD_1) ? BACKWARD_1 : BACKWARD_4;
     a.piece_steps = steps_of(a.shape);
   } else {
-    a.shape = a.T <= steps_of(FORWARD_1) || tiles >= 2048 ? FORWARD_1 : FORWARD_8;
-    if (a.shape == FORWARD_8 && tiles > 0) {
-      const int64_t blocks = ((int64_t)a.T + steps_of(FORWARD_8) - 1) / steps_of(FORWARD_8), want = (1023 + tiles) / tiles;
+    a.shape = a.T <= steps_of(FORWARD_1) || tiles >= 2048 ? FORWARD_1 : FORWARD_4;
+    if (a.shape == FORWARD_4 && tiles > 0) {
+      const int64_t blocks = ((int64_t)a.T + steps_of(FORWARD_4) - 1) / steps_of(FORWARD_4), want = (1023 + tiles) / tiles;
       const int64_t each = tiles >= 256 || want < 2 ? blocks : (blocks + want - 1) / want;
-      a.piece_steps = each * steps_of(FORWARD_8);
+      a.piece_steps = each * steps_of(FORWARD_4);
     }
   }
   if (a.piece_steps > 0 && a.piece_steps < a.T) a.pieces = (int32_t)((a.T + a.piece_steps - 1) / a.piece_steps);
