@@ -198,8 +198,8 @@ int32_t rslx_gated_recurrence(const rslx_gated_rec* a, const rslx_seq_view* x, c
   RSLX_TRY(check_apart(of_h, 1, who));
   if (s0_or_null != s_last_or_null) RSLX_TRY(check_apart(of_state, 1, who));
   RecArgs r = rec_args(*a);
-  RSLX_TRY(rec_plan(r, a->dtype, false, ws, ws_bytes, who));
   r.x = matrix(x); r.g = matrix(g); r.h = matrix(h);
+  RSLX_TRY(rec_plan(r, a->dtype, false, ws, ws_bytes, who));
   r.s0 = s0_or_null; r.s_last = s_last_or_null;
   RSLX_HIP(launch_recurrence(r, a->dtype, false, (hipStream_t)stream));
   return RSLX_OK;
@@ -230,8 +230,8 @@ int32_t rslx_gated_recurrence_backward(const rslx_gated_rec* a, const rslx_seq_v
                        {block_of(a->lengths, (int64_t)a->N * 4), "lengths"}};
   RSLX_TRY(check_apart(all, 3, who));
   RecArgs r = rec_args(*a);
-  RSLX_TRY(rec_plan(r, a->dtype, true, ws, ws_bytes, who));
   r.x = matrix(x); r.g = matrix(g); r.dh = matrix(dh); r.dx = matrix(dx); r.dg = matrix(dg);
+  RSLX_TRY(rec_plan(r, a->dtype, true, ws, ws_bytes, who));
   r.s0 = s0_or_null; r.ds_last = ds_last_or_null; r.ds0 = ds0_or_null;
   RSLX_HIP(launch_recurrence(r, a->dtype, true, (hipStream_t)stream));
   return RSLX_OK;

@@ -10,6 +10,7 @@
 // workgroup's steps hold the sequence, or channels are many enough for workgroups to go along whole sequences (forward).  Otherwise sequences
 // are cut into pieces: one launch leaves every piece's map, a second (a lane per channel) the states between the pieces, a third makes the results.
 #include "memory.h"
+#include "overlap.h"
 #include "typed.h"
 
 namespace rslx {
@@ -156,14 +157,23 @@ __device__ __forceinline__ Map whole(Map m, WaveMaps<WAVES>& maps) {
 struct Place {
   int64_t n;
   int d, len, piece;
+  bool full;                                // every lane has four channels: the same for the whole workgroup
 };
 __device__ __forceinline__ Place place_of(const RecArgs& a) {
   const int tiles = (a.D + TILE - 1) / TILE;
-  const int64_t all_tiles = (int64_t)a.N * tiles, at = blockIdx.x % all_tiles;
+  // workgroups go to the eight dies in turn.  Where neighbours share lines of memory, each die gets a row of them, so that its L2 joins what they read and
+  // write (500 steps of 300 sequences, 203 channels in bf16: 117 us, in turn 138); where they do not, in turn is better (8192 steps of 4, 1024 channels: 73 and 81)
+  uint32_t block = blockIdx.x;
+  if (a.shared_lines) {
+    const uint32_t each = gridDim.x / 8, more = gridDim.x % 8, die = block % 8;
+    block = die * each + (die < more ? die : more) + block / 8;
+  }
+  const int64_t all_tiles = (int64_t)a.N * tiles, at = block % all_tiles;
   Place p;
-  p.piece = (int)(blockIdx.x / all_tiles);
+  p.piece = (int)(block / all_tiles);
   p.n = at / tiles;
   p.d = (int)(at % tiles) * TILE + (threadIdx.x & (ROW - 1)) * W;
+  p.full = (int)(at % tiles) * TILE + TILE <= a.D;
   p.len = a.T;
   if (a.lengths) {
     const int len = a.lengths[p.n];
@@ -191,8 +201,10 @@ __device__ __forceinline__ float4* piece_at(float* base, const RecArgs& a, const
 
 // A matrix as a lane sees it: its row of step i behind the wavefront's first.  WHOLE: rows are whole, aligned loads, and what differs between lanes fits 32 bits:
 // the address is a common one and an offset that stays, for any i; lanes beyond the last channel read the first one's.
-template <typename T, bool WHOLE>
+// STREAM: how large matrices go past the caches, which keep other things then: 1, what is written; 2, what is read as well (see stream_of).
+template <typename T, bool WHOLE, int STREAM>
 struct Rows {
+  typedef uint32_t Bits __attribute__((ext_vector_type(sizeof(T) * W / 4)));
   char* base;
   uint32_t offset;
   T* mine;
@@ -206,17 +218,57 @@ struct Rows {
     }
   }
   __device__ __forceinline__ void load(Pack<T, W>& v, int i, const RecArgs& a, const Place& p) const {
-    if constexpr (WHOLE) v = *reinterpret_cast<const Pack<T, W>*>(base + i * step * (int64_t)sizeof(T) + offset);
+    if constexpr (WHOLE && STREAM == 2) {
+      const Bits bits = __builtin_nontemporal_load(reinterpret_cast<const Bits*>(base + i * step * (int64_t)sizeof(T) + offset));
+      __builtin_memcpy(&v, &bits, sizeof v);
+    } else if constexpr (WHOLE) v = *reinterpret_cast<const Pack<T, W>*>(base + i * step * (int64_t)sizeof(T) + offset);
     else load_piece<T, W, false>(v, mine + i * step, p.d, a.D);
+  }
+  // all of the lane's steps
+  template <int L>
+  __device__ __forceinline__ void load(Pack<T, W> (&v)[L], const RecArgs& a, const Place& p) const {
+    if (WHOLE || !p.full) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) load(v[i], i, a, p);
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i) __builtin_memcpy(&v[i], mine + i * step + p.d, sizeof v[i]);
+    }
+  }
+  template <int L>
+  __device__ __forceinline__ void store(const Pack<T, W> (&v)[L], const RecArgs& a, const Place& p) const {
+    if (WHOLE || !p.full) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) store(v[i], i, a, p);
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i) __builtin_memcpy(mine + i * step + p.d, &v[i], sizeof v[i]);
+    }
   }
   __device__ __forceinline__ void store(const Pack<T, W>& v, int i, const RecArgs& a, const Place& p) const {
     if constexpr (WHOLE) {
-      if (p.d < a.D) *reinterpret_cast<Pack<T, W>*>(base + i * step * (int64_t)sizeof(T) + offset) = v;
+      if (p.d >= a.D) return;
+      Bits bits;
+      __builtin_memcpy(&bits, &v, sizeof v);
+      Bits* to = reinterpret_cast<Bits*>(base + i * step * (int64_t)sizeof(T) + offset);
+      if constexpr (STREAM > 0) __builtin_nontemporal_store(bits, to);
+      else *to = bits;
     } else {
       store_piece<T, W, false>(v, mine + i * step, p.d, a.D);
     }
   }
 };
+
+// Zeros behind the last step that exists.
+template <int L, typename T, bool WHOLE, int STREAM>
+__device__ __forceinline__ void store_nothing(const Rows<T, WHOLE, STREAM>& r, int64_t t0, const RecArgs& a, const Place& p) {
+  Pack<T, W> zero;
+#pragma unroll
+  for (int k = 0; k < W; ++k) zero.v[k] = from_float<T>(0.f);
+#pragma unroll
+  for (int i = 0; i < L; ++i)
+    if (t0 + i < a.T) r.store(zero, i, a, p);
+}
 
 // Which of the lane's steps from t0 on end an episode.
 template <int L>
@@ -231,7 +283,7 @@ __device__ __forceinline__ uint32_t ends_of(const RecArgs& a, const Place& p, in
 
 // Forward: a workgroup goes along its piece, WAVES * SETS * L steps at a time.  MAPS: no results, the piece's map alone.  Where every step of a wavefront exists and
 // none ends an episode (`plain`), nothing is asked step by step.
-template <typename T, int L, int WAVES, bool WHOLE, bool MAPS>
+template <typename T, int L, int WAVES, bool WHOLE, int STREAM, bool MAPS>
 __global__ __launch_bounds__(WAVES * 64) void recurrence_kernel(RecArgs a) {
   __shared__ WaveMaps<WAVES> maps[2];
   const Place p = place_of(a);
@@ -246,10 +298,10 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_kernel(RecArgs a) {
   int turn = 0;
   for (int64_t t = begin; t < end; t += WAVES * SETS * L, turn ^= 1) {
     const int64_t t0 = t + ahead;
-    const Rows<T, WHOLE> rx(a.x, a, p, t, ahead), rg(a.g, a, p, t, ahead);
+    const Rows<T, WHOLE, STREAM> rx(a.x, a, p, t, ahead), rg(a.g, a, p, t, ahead);
     Pack<T, W> px[L], pg[L];
     const uint32_t ends = ends_of<L>(a, p, t0);
-    const bool plain = __all(ends == 0 && t0 + L <= p.len);
+    const bool plain = __all(ends == 0 && t0 + L <= p.len), none = __all(t0 >= p.len);
     float f[L][W], v[L][W];
     Map m = same();
     auto gates = [&]() {
@@ -262,12 +314,11 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_kernel(RecArgs a) {
           v[i][k] = rest * to_float(px[i].v[k]);
         }
     };
-    if (plain) {
-#pragma unroll
-      for (int i = 0; i < L; ++i) {
-        rg.load(pg[i], i, a, p);
-        rx.load(px[i], i, a, p);
-      }
+    if (none) {
+      // (the map that hands the state on)
+    } else if (plain) {
+      rg.load(pg, a, p);
+      rx.load(px, a, p);
       gates();
 #pragma unroll
       for (int i = 0; i < L; ++i)
@@ -302,18 +353,19 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_kernel(RecArgs a) {
       continue;
     }
     Four h = enter<WAVES, true>(m, s, maps[turn]);
-    const Rows<T, WHOLE> rh(a.h, a, p, t, ahead);
+    const Rows<T, WHOLE, STREAM> rh(a.h, a, p, t, ahead);
     if (plain) {
+      Pack<T, W> out[L];
 #pragma unroll
-      for (int i = 0; i < L; ++i) {
-        Pack<T, W> out;
+      for (int i = 0; i < L; ++i)
 #pragma unroll
         for (int k = 0; k < W; ++k) {
           h.v[k] = fmaf(f[i][k], h.v[k], v[i][k]);
-          out.v[k] = from_float<T>(h.v[k]);
+          out[i].v[k] = from_float<T>(h.v[k]);
         }
-        rh.store(out, i, a, p);
-      }
+      rh.store(out, a, p);
+    } else if (none) {
+      store_nothing<L>(rh, t0, a, p);
     } else {
 #pragma unroll
       for (int i = 0; i < L; ++i) {
@@ -339,16 +391,16 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_kernel(RecArgs a) {
 }
 
 // Backward: a piece is the steps that a workgroup holds at once.  MAPS: the piece's maps of both directions (whose gates' product is the same).
-template <typename T, int L, int WAVES, bool WHOLE, bool MAPS>
+template <typename T, int L, int WAVES, bool WHOLE, int STREAM, bool MAPS>
 __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(RecArgs a) {
   __shared__ WaveMaps<WAVES> maps[2];
   const Place p = place_of(a);
   const int ahead = threadIdx.x / ROW * L;
   const int64_t t = (int64_t)p.piece * (WAVES * SETS * L), t0 = t + ahead;
-  const Rows<T, WHOLE> rx(a.x, a, p, t, ahead), rg(a.g, a, p, t, ahead), rd(a.dh, a, p, t, ahead);
+  const Rows<T, WHOLE, STREAM> rx(a.x, a, p, t, ahead), rg(a.g, a, p, t, ahead), rd(a.dh, a, p, t, ahead);
   Pack<T, W> px[L], pg[L], pd[L];
   const uint32_t ends = ends_of<L>(a, p, t0);
-  const bool plain = __all(ends == 0 && t0 + L <= p.len);
+  const bool plain = __all(ends == 0 && t0 + L <= p.len), none = __all(t0 >= p.len);
   float f[L][W], rest[L][W];
   Map m = same(), up = same();
   auto gates = [&]() {
@@ -357,13 +409,12 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(RecArgs
 #pragma unroll
       for (int k = 0; k < W; ++k) gate<T>(to_float(pg[i].v[k]), f[i][k], rest[i][k]);
   };
-  if (plain) {
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      rg.load(pg[i], i, a, p);
-      rx.load(px[i], i, a, p);
-      rd.load(pd[i], i, a, p);
-    }
+  if (none) {
+    // (the maps that hand the states on)
+  } else if (plain) {
+    rg.load(pg, a, p);
+    rx.load(px, a, p);
+    rd.load(pd, a, p);
     gates();
 #pragma unroll
     for (int i = 0; i < L; ++i)
@@ -427,6 +478,12 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(RecArgs
   }
   Four h = enter<WAVES, true>(m, s, maps[0]), down = enter<WAVES, false>(up, q, maps[1]);
   if (p.piece == 0 && threadIdx.x < ROW) store_state<WHOLE>(a.ds0, a, p, q);
+  const Rows<T, WHOLE, STREAM> rdx(a.dx, a, p, t, ahead), rdg(a.dg, a, p, t, ahead);
+  if (none) {
+    store_nothing<L>(rdx, t0, a, p);
+    store_nothing<L>(rdg, t0, a, p);
+    return;
+  }
   float in[L][W];                           // f (1 - f) (h - x), of the states h that the steps start from
 #pragma unroll
   for (int i = 0; i < L; ++i)
@@ -437,7 +494,6 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(RecArgs
       h.v[k] = fmaf(f[i][k], h.v[k], rest[i][k] * x);
       if (!plain && (ends >> i & 1)) h.v[k] = 0.f;
     }
-  const Rows<T, WHOLE> rdx(a.dx, a, p, t, ahead), rdg(a.dg, a, p, t, ahead);
 #pragma unroll
   for (int i = L - 1; i >= 0; --i) {
     Pack<T, W> dx, dg;
@@ -514,18 +570,19 @@ __global__ __launch_bounds__(REC_THREADS) void recurrence_step_kernel(RecArgs a)
 }
 
 // How the steps are shared out: wavefronts of a workgroup, steps of a lane; see plan_recurrence.
-enum RecShape { FORWARD_1 = 0, FORWARD_4, BACKWARD_1, BACKWARD_4 };
-constexpr int LANE_STEPS[] = {4, 8, 8, 8}, SHAPE_WAVES[] = {1, 4, 1, 4};
+enum RecShape { FORWARD_1 = 0, FORWARD_4, BACKWARD_1, BACKWARD_4, BACKWARD_4_SHORT };
+constexpr int LANE_STEPS[] = {4, 4, 8, 8, 4}, SHAPE_WAVES[] = {1, 4, 1, 4, 4};
 int steps_of(int shape) { return LANE_STEPS[shape] * SHAPE_WAVES[shape] * SETS; }
 
-template <typename T, bool WHOLE, bool MAPS>
+template <typename T, bool WHOLE, int STREAM, bool MAPS>
 void run_shape(const RecArgs& a, hipStream_t s) {
   const unsigned grid = (unsigned)((int64_t)a.N * ((a.D + TILE - 1) / TILE) * a.pieces);
 #define RUN(shape, kernel) \
-  case shape: hipLaunchKernelGGL((kernel<T, LANE_STEPS[shape], SHAPE_WAVES[shape], WHOLE, MAPS>), dim3(grid), dim3(SHAPE_WAVES[shape] * 64), 0, s, a); break
+  case shape: hipLaunchKernelGGL((kernel<T, LANE_STEPS[shape], SHAPE_WAVES[shape], WHOLE, STREAM, MAPS>), dim3(grid), dim3(SHAPE_WAVES[shape] * 64), 0, s, a); break
   switch (a.shape) {
     RUN(FORWARD_4, recurrence_kernel);
     RUN(BACKWARD_4, recurrence_backward_kernel);
+    RUN(BACKWARD_4_SHORT, recurrence_backward_kernel);
     default:
       if constexpr (!MAPS) switch (a.shape) {
         RUN(FORWARD_1, recurrence_kernel);
@@ -545,11 +602,29 @@ bool rec_whole(const RecArgs& a, int size) {
   return a.D % W == 0 && fits(a.x) && fits(a.g) && fits(a.h) && fits(a.dh) && fits(a.dx) && fits(a.dg);
 }
 
+// Outputs of 32 MB and more are written past the caches; inputs are read past them where the call moves more than the last-level cache's 256 MB and reads them once.
+int stream_of(const RecArgs& a, int size) {
+  const double matrix = (double)a.T * a.N * a.D * size;
+  const int outputs = a.h.p ? 1 : 2, inputs = a.h.p ? 2 : 3;
+  if (outputs * matrix < 32e6) return 0;
+  return a.pieces == 1 && (outputs + inputs) * matrix > 256e6 ? 2 : 1;
+}
+
+// Whether tiles of a row meet inside a line of memory.
+bool shared_lines(const RecArgs& a, int size) {
+  auto apart = [&](const RecMatrix& m) { return !m.p || (reinterpret_cast<uintptr_t>(m.p) | (uint64_t)m.step * size | (uint64_t)m.seq * size) % 128 == 0; };
+  return (int64_t)a.D * size % 128 != 0 || !(apart(a.x) && apart(a.g) && apart(a.h) && apart(a.dh) && apart(a.dx) && apart(a.dg));
+}
+
 template <typename T>
 void run_type(const RecArgs& a, bool maps, hipStream_t s) {
   const bool whole = rec_whole(a, (int)sizeof(T));
-  if (maps) whole ? run_shape<T, true, true>(a, s) : run_shape<T, false, true>(a, s);
-  else whole ? run_shape<T, true, false>(a, s) : run_shape<T, false, false>(a, s);
+  const int stream = stream_of(a, (int)sizeof(T));
+  if (maps) whole ? run_shape<T, true, 0, true>(a, s) : run_shape<T, false, 0, true>(a, s);
+  else if (!whole) run_shape<T, false, 0, false>(a, s);
+  else if (stream == 0) run_shape<T, true, 0, false>(a, s);
+  else if (stream == 1) run_shape<T, true, 1, false>(a, s);
+  else run_shape<T, true, 2, false>(a, s);
 }
 
 void run(const RecArgs& a, int dtype, bool maps, hipStream_t s) {
@@ -562,12 +637,13 @@ void run(const RecArgs& a, int dtype, bool maps, hipStream_t s) {
 
 // Forward, a wavefront along each sequence and 64 channels where that fills the GPU or one is enough for the steps; otherwise eight, in pieces where even
 // these are few.  Backward, the smallest workgroup that holds the sequence, the largest in pieces where none does.
-void plan_recurrence(host::Carver& c, RecArgs& a, int, bool backward) {
+void plan_recurrence(host::Carver& c, RecArgs& a, int dtype, bool backward) {
   const int64_t tiles = (int64_t)a.N * ((a.D + TILE - 1) / TILE);
   a.pieces = 1;
   a.piece_steps = a.T;
   if (backward) {
-    a.shape = a.T <= steps_of(BACKWARD_1) ? BACKWARD_1 : BACKWARD_4;
+    const bool long_pieces = a.T <= steps_of(BACKWARD_4) || (a.x.p && rec_whole(a, host::type_size(dtype)) && !a.lengths);
+    a.shape = a.T <= steps_of(BACKWARD_1) ? BACKWARD_1 : a.T > steps_of(BACKWARD_4_SHORT) && long_pieces ? BACKWARD_4 : BACKWARD_4_SHORT;
     a.piece_steps = steps_of(a.shape);
   } else {
     a.shape = a.T <= steps_of(FORWARD_1) || tiles >= 2048 ? FORWARD_1 : FORWARD_4;
@@ -587,7 +663,8 @@ void plan_recurrence(host::Carver& c, RecArgs& a, int, bool backward) {
   }
 }
 
-hipError_t launch_recurrence(const RecArgs& a, int dtype, bool backward, hipStream_t stream) {
+hipError_t launch_recurrence(RecArgs& a, int dtype, bool backward, hipStream_t stream) {
+  a.shared_lines = shared_lines(a, host::type_size(dtype));
   const double n = (double)a.T * a.N * a.D, size = dtype == RSLX_F32 ? 4 : 2;
   if (a.pieces > 1) {
     {

@@ -20,6 +20,7 @@ struct RecArgs {
   float* s_last;                // or null
   const float* ds_last;         // or null = 0
   float* ds0;                   // or null
+  int32_t shared_lines;
   int32_t shape;                // how the steps are shared out (gated_recurrence.hip)
   int32_t pieces;               // of a sequence, of piece_steps steps each
   int64_t piece_steps;
@@ -28,7 +29,7 @@ struct RecArgs {
 };
 // Carves the workspace of a call and enters its places.
 void plan_recurrence(host::Carver& c, RecArgs& a, int dtype, bool backward);
-hipError_t launch_recurrence(const RecArgs& a, int dtype, bool backward, hipStream_t stream);
+hipError_t launch_recurrence(RecArgs& a, int dtype, bool backward, hipStream_t stream);
 hipError_t launch_recurrence_step(const RecArgs& a, int dtype, hipStream_t stream);
 
 // ---- root-mean-square norm --------------------------------------------------------------------------------------------
