@@ -75,7 +75,7 @@ struct MuonArgs {
   float lr, momentum, decay;
   int32_t nesterov;
 };
-constexpr int MUON_NORM_BLOCKS = 64;      // workgroups at most that sum a matrix's squares
+constexpr int MUON_NORM_BLOCKS = 512;      // workgroups at most that sum a matrix's squares
 hipError_t launch_muon(MuonArgs& a, int steps, hipStream_t stream);
 
 }  // namespace rslx
