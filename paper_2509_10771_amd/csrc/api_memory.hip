@@ -149,27 +149,15 @@ int32_t check_muon(const rslx_muon_matrix* m, int32_t count, const rslx_muon_cfg
   return RSLX_OK;
 }
 
-void plan_muon(Carver& c, const rslx_muon_matrix* m, int32_t count, const rslx_muon_cfg& cfg, MuonArgs& a) {
-  memset(&a, 0, sizeof a);
-  a.count = count;
-  a.lr = cfg.lr; a.momentum = cfg.momentum; a.decay = cfg.weight_decay;
-  a.nesterov = cfg.nesterov;
-  for (int i = 0; i < count; ++i) {
-    MuonItem& t = a.item[i];
-    t.w_in = m[i].w_in; t.w_out = m[i].w_out; t.grad = m[i].grad; t.m_in = m[i].m_in; t.m_out = m[i].m_out;
-    t.rows = m[i].rows; t.cols = m[i].cols;
-    t.p = t.rows < t.cols ? t.rows : t.cols;
-    t.q = t.rows < t.cols ? t.cols : t.rows;
-    t.scale = m[i].scale;
-    const size_t P = ((size_t)t.p + 31) / 32 * 32, Q = ((size_t)t.q + 31) / 32 * 32;
-    t.u = c.take<float>((size_t)t.rows * t.cols);
-    t.norm = c.take<double>(MUON_NORM_BLOCKS);
-    t.x = c.take<uint16_t>(2 * P * Q);
-    t.xt[0] = c.take<uint16_t>(2 * P * Q);
-    t.xt[1] = c.take<uint16_t>(2 * P * Q);
-    t.a = c.take<uint16_t>(2 * P * P);
-    t.b = c.take<uint16_t>(2 * P * P);
-  }
+// The workspace: the table, then each matrix's part.
+MuonTable* plan_muon(Carver& c, const rslx_muon_matrix* m, int32_t count, const rslx_muon_cfg& cfg, MuonTable& t) {
+  memset(&t, 0, sizeof t);
+  t.lr = cfg.lr; t.momentum = cfg.momentum; t.decay = cfg.weight_decay;
+  t.nesterov = cfg.nesterov;
+  MuonTable* table = c.take<MuonTable>(1);
+  for (int i = 0; i < count; ++i)
+    t.item[i] = {m[i].w_in, m[i].w_out, m[i].grad, m[i].m_in, m[i].m_out, c.take<char>(muon_item_bytes(m[i].rows, m[i].cols)), m[i].rows, m[i].cols, m[i].scale};
+  return table;
 }
 
 }  // namespace
@@ -320,8 +308,8 @@ int32_t rslx_rms_norm_backward(int32_t dtype, const void* dy, int64_t lddy, cons
 size_t rslx_muon_step_workspace_bytes(const rslx_muon_matrix* matrices, int32_t count, const rslx_muon_cfg* cfg) {
   if (check_muon(matrices, count, cfg, "rslx_muon_step_workspace_bytes") != RSLX_OK) return 0;
   Carver c(nullptr);
-  MuonArgs a;
-  plan_muon(c, matrices, count, *cfg, a);
+  MuonTable t;
+  plan_muon(c, matrices, count, *cfg, t);
   return c.off > 256 ? c.off : 256;
 }
 
@@ -355,11 +343,11 @@ int32_t rslx_muon_step(const rslx_muon_matrix* matrices, int32_t count, const rs
     if (r.written && (!far_written || r.hi > far_written->hi)) far_written = &r;
   }
   Carver c(ws);
-  MuonArgs a;
-  plan_muon(c, matrices, count, *cfg, a);
+  MuonTable t;
+  MuonTable* table = plan_muon(c, matrices, count, *cfg, t);
   if (!ws || ws_bytes < c.off) return fail(RSLX_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", who, ws_bytes, c.off);
   if (!aligned16(ws)) return fail(RSLX_ERR_INVALID_ARG, "%s: workspace not 16-byte aligned", who);
-  RSLX_HIP(launch_muon(a, cfg->steps, (hipStream_t)stream));
+  RSLX_HIP(launch_muon(t, count, table, cfg->steps, (hipStream_t)stream));
   return RSLX_OK;
 }
 

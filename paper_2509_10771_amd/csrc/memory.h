@@ -56,26 +56,27 @@ hipError_t launch_rms_norm_backward(const RmsArgs& a, int dtype, hipStream_t str
 
 // ---- Muon step --------------------------------------------------------------------------------------------------------
 // p <= q are a matrix's sides, X [p, q] (the transposed update where the matrix is tall), in 32 x 16 blocks of 64 lanes: see muon.hip.
-struct MuonItem {
+struct alignas(16) MuonItem {
   const float* w_in;
   float* w_out;
   const float* grad;
   const float* m_in;
   float* m_out;
-  float* u;                     // the update before it is made orthogonal, [rows, cols]
-  double* norm;                 // partial sums of its squares
-  uint16_t *x, *xt[2], *a, *b;  // X; X transposed, two in turn; A = X X^T; a I + b A + c A^2
-  int32_t rows, cols, p, q;
+  char* base;                   // the matrix's part of the workspace (muon_item_bytes)
+  int32_t rows, cols;
   float scale;
-  int32_t first;                // of the launch's workgroups
 };
-struct MuonArgs {
+// What every launch reads: the first one, which has it as an argument, leaves it at the start of the workspace for the others (an argument of that size
+// is read from memory of the host, several times in a row).
+enum MuonGrid { MUON_MOMENTUM_GRID, MUON_PACK_GRID, MUON_SYMMETRIC_GRID, MUON_APPLY_GRID, MUON_GRIDS };
+struct MuonTable {
   MuonItem item[RSLX_MUON_MAX_MATRICES];
-  int32_t count;
+  int32_t first[MUON_GRIDS][RSLX_MUON_MAX_MATRICES];     // workgroup of a launch that a matrix begins with; INT32_MAX behind the last one
   float lr, momentum, decay;
   int32_t nesterov;
 };
-constexpr int MUON_NORM_BLOCKS = 512;      // workgroups at most that sum a matrix's squares
-hipError_t launch_muon(MuonArgs& a, int steps, hipStream_t stream);
+constexpr int MUON_NORM_BLOCKS = 512;     // workgroups at most that sum a matrix's squares
+size_t muon_item_bytes(int32_t rows, int32_t cols);
+hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int steps, hipStream_t stream);
 
 }  // namespace rslx

@@ -28,12 +28,53 @@ constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float HOLD = 4096.f, UNHOLD = 0x1p-12f, UNHOLD2 = 0x1p-24f;
 constexpr int BLOCK = 1024;               // fp16 values of a block: 512 of hi, 512 of lo
 
-__device__ __forceinline__ int pad32(int n) { return (n + 31) & ~31; }
+__host__ __device__ inline int pad32(int n) { return (n + 31) & ~31; }
 
-__device__ __forceinline__ const MuonItem& item_of(const MuonArgs& a, int block) {
-  int i = 0;
-  while (i + 1 < a.count && a.item[i + 1].first <= block) ++i;
-  return a.item[i];
+// A matrix as the kernels see it.  p <= q are its sides, X is [p, q] (the transposed update where the matrix is tall), P and Q blocks of 32 rows.
+struct Matrix {
+  MuonItem m;
+  int p, q, P, Q, block;                  // block: the workgroup's among the matrix's
+  bool tall;
+  float* u;                               // the update before it is made orthogonal, [rows, cols]
+  double* norm;                           // partial sums of its squares
+  uint16_t *x, *xt0, *xt1, *a, *b;           // X; X transposed, two in turn; A = X X^T; B = a I + b A + c A^2
+};
+__host__ __device__ inline size_t values_bytes(int rows, int cols) { return ((size_t)rows * cols * sizeof(float) + 255) / 256 * 256; }
+
+// The matrix that the workgroup belongs to.  Every lane asks for one matrix's entry at once with where they begin, so that the table is read in one go.
+__device__ __forceinline__ Matrix matrix_of(const MuonTable& t, MuonGrid grid) {
+  constexpr int WORDS = sizeof(MuonItem) / 4;
+  static_assert(sizeof(MuonItem) == 64 && RSLX_MUON_MAX_MATRICES <= 64, "an entry is four loads of 16 bytes, a lane has one");
+  const int lane = (threadIdx.x & 63) % RSLX_MUON_MAX_MATRICES;
+  const int begins = (threadIdx.x & 63) < RSLX_MUON_MAX_MATRICES ? t.first[grid][lane] : INT32_MAX;
+  uint32_t entry[WORDS];
+  __builtin_memcpy(entry, &t.item[lane], sizeof entry);
+  // workgroups go to the eight dies in turn: each die gets a row of neighbours, which share operands in its L2
+  const uint32_t each = gridDim.x / 8, more = gridDim.x % 8, die = blockIdx.x % 8;
+  const int block = (int)(die * each + (die < more ? die : more) + blockIdx.x / 8);
+  const int i = __popcll(__ballot(begins <= block)) - 1;
+#pragma unroll
+  for (int w = 0; w < WORDS; ++w) entry[w] = __builtin_amdgcn_readlane(entry[w], i);
+  Matrix r;
+  __builtin_memcpy(&r.m, entry, sizeof entry);
+  r.block = block - __builtin_amdgcn_readlane(begins, i);
+  r.tall = r.m.rows > r.m.cols;
+  r.p = r.tall ? r.m.cols : r.m.rows;
+  r.q = r.tall ? r.m.rows : r.m.cols;
+  r.P = pad32(r.p) / 32;
+  r.Q = pad32(r.q) / 32;
+  char* at = r.m.base;
+  r.u = reinterpret_cast<float*>(at);
+  at += values_bytes(r.m.rows, r.m.cols);
+  r.norm = reinterpret_cast<double*>(at);
+  at += MUON_NORM_BLOCKS * sizeof(double);
+  r.x = reinterpret_cast<uint16_t*>(at);
+  const int64_t plane = (int64_t)r.P * r.Q * 2 * BLOCK, square = (int64_t)r.P * r.P * 2 * BLOCK;
+  r.xt0 = r.x + plane;
+  r.xt1 = r.xt0 + plane;
+  r.a = r.xt1 + plane;
+  r.b = r.a + square;
+  return r;
 }
 
 // hi and lo of a value that is held times 2^12.
@@ -44,8 +85,8 @@ __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
 
 constexpr int ELEMENT_THREADS = 256;
 
-__host__ __device__ inline int norm_blocks(const MuonItem& m) {
-  const int64_t n = ((int64_t)m.rows * m.cols + 4 * ELEMENT_THREADS - 1) / (4 * ELEMENT_THREADS);
+__host__ __device__ inline int norm_blocks(int rows, int cols) {
+  const int64_t n = ((int64_t)rows * cols + 4 * ELEMENT_THREADS - 1) / (4 * ELEMENT_THREADS);
   return n < MUON_NORM_BLOCKS ? (int)n : MUON_NORM_BLOCKS;
 }
 
@@ -62,12 +103,14 @@ __device__ __forceinline__ double group_sum(double v) {
 }
 
 // Squares are summed in 64 bits, where no fp32 value's vanishes or overflows.
-__global__ __launch_bounds__(ELEMENT_THREADS) void muon_momentum_kernel(MuonArgs a) {
-  const MuonItem& m = item_of(a, blockIdx.x);
-  const int block = blockIdx.x - m.first;
-  const int64_t n = (int64_t)m.rows * m.cols, stride = (int64_t)norm_blocks(m) * ELEMENT_THREADS;
+__global__ __launch_bounds__(ELEMENT_THREADS) void muon_momentum_kernel(MuonTable t, MuonTable* in_workspace) {
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < (int)(sizeof t / 4); i += ELEMENT_THREADS) reinterpret_cast<uint32_t*>(in_workspace)[i] = reinterpret_cast<const uint32_t*>(&t)[i];
+  const Matrix x = matrix_of(t, MUON_MOMENTUM_GRID);
+  const MuonItem& m = x.m;
+  const int64_t n = (int64_t)m.rows * m.cols, stride = (int64_t)norm_blocks(m.rows, m.cols) * ELEMENT_THREADS;
   double sum = 0.0;
-  for (int64_t i = (int64_t)block * ELEMENT_THREADS + threadIdx.x; i < n; i += 4 * stride) {
+  for (int64_t i = (int64_t)x.block * ELEMENT_THREADS + threadIdx.x; i < n; i += 4 * stride) {
     float g[4], before[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
@@ -78,37 +121,41 @@ __global__ __launch_bounds__(ELEMENT_THREADS) void muon_momentum_kernel(MuonArgs
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (i + k * stride < n) {
-        const float now = fmaf(a.momentum, before[k], g[k]), u = a.nesterov ? fmaf(a.momentum, now, g[k]) : now;
+        const float now = fmaf(t.momentum, before[k], g[k]), u = t.nesterov ? fmaf(t.momentum, now, g[k]) : now;
         if (m.m_out) m.m_out[i + k * stride] = now;
-        m.u[i + k * stride] = u;
+        x.u[i + k * stride] = u;
         sum += (double)u * u;
       }
   }
   sum = group_sum(sum);
-  if (threadIdx.x == 0) m.norm[block] = sum;
+  if (threadIdx.x == 0) x.norm[x.block] = sum;
 }
 
 // X and X transposed from u: a wavefront makes 32 x 32 values of X.
-__global__ __launch_bounds__(ELEMENT_THREADS) void muon_pack_kernel(MuonArgs a) {
+__global__ __launch_bounds__(ELEMENT_THREADS) void muon_pack_kernel(const MuonTable* t) {
   __shared__ float tile[ELEMENT_THREADS / 64][32][33];
-  const MuonItem& m = item_of(a, blockIdx.x);
+  const Matrix m = matrix_of(*t, MUON_PACK_GRID);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int at = m.block * (ELEMENT_THREADS / 64) + wave;
+  const bool here = at < m.P * m.Q;
+  const int p0 = here ? at / m.Q * 32 : 0, q0 = here ? at % m.Q * 32 : 0;
+  float u[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int row = (m.tall ? q0 : p0) + i * 2 + (lane >> 5), col = (m.tall ? p0 : q0) + (lane & 31);
+    u[i] = row < m.m.rows && col < m.m.cols ? m.u[(int64_t)row * m.m.cols + col] : 0.f;
+  }
   double sum = 0.0;
-  for (int i = threadIdx.x; i < norm_blocks(m); i += ELEMENT_THREADS) sum += m.norm[i];
+  for (int i = threadIdx.x; i < norm_blocks(m.m.rows, m.m.cols); i += ELEMENT_THREADS) sum += m.norm[i];
   sum = group_sum(sum);
   const double inv = sum == 0.0 ? 0.0 : (double)HOLD / sqrt(sum);
-  const int P = pad32(m.p) / 32, Q = pad32(m.q) / 32;
-  const int at = (blockIdx.x - m.first) * (ELEMENT_THREADS / 64) + wave;
-  const bool here = at < P * Q, tall = m.rows > m.cols;
-  const int p0 = here ? at / Q * 32 : 0, q0 = here ? at % Q * 32 : 0;
-  if (here)
-    for (int i = lane; i < 1024; i += 64) {
-      const int slow = i >> 5, fast = i & 31;            // of u: rows and columns
-      const int row = (tall ? q0 : p0) + slow, col = (tall ? p0 : q0) + fast;
-      const float v = row < m.rows && col < m.cols ? (float)(m.u[(int64_t)row * m.cols + col] * inv) : 0.f;
-      if (tall) tile[wave][fast][slow] = v;
-      else tile[wave][slow][fast] = v;
-    }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int slow = i * 2 + (lane >> 5), fast = lane & 31;            // of u: rows and columns
+    const float v = (float)(u[i] * inv);
+    if (m.tall) tile[wave][fast][slow] = v;
+    else tile[wave][slow][fast] = v;
+  }
   __syncthreads();
   if (!here) return;
   const int r = lane & 31, k8 = (lane >> 5) * 8;
@@ -121,7 +168,7 @@ __global__ __launch_bounds__(ELEMENT_THREADS) void muon_pack_kernel(MuonArgs a) 
       hi[e] = h;
       lo[e] = l;
     }
-    uint16_t* to = m.x + ((int64_t)(p0 >> 5) * (Q * 2) + (q0 >> 4) + half) * BLOCK + lane * 8;
+    uint16_t* to = m.x + ((int64_t)(p0 >> 5) * (m.Q * 2) + (q0 >> 4) + half) * BLOCK + lane * 8;
     *reinterpret_cast<half8*>(to) = hi;
     *reinterpret_cast<half8*>(to + 512) = lo;
 #pragma unroll
@@ -131,7 +178,7 @@ __global__ __launch_bounds__(ELEMENT_THREADS) void muon_pack_kernel(MuonArgs a) 
       hi[e] = h;
       lo[e] = l;
     }
-    to = m.xt[0] + ((int64_t)(q0 >> 5) * (P * 2) + (p0 >> 4) + half) * BLOCK + lane * 8;
+    to = m.xt0 + ((int64_t)(q0 >> 5) * (m.P * 2) + (p0 >> 4) + half) * BLOCK + lane * 8;
     *reinterpret_cast<half8*>(to) = hi;
     *reinterpret_cast<half8*>(to + 512) = lo;
   }
@@ -139,12 +186,33 @@ __global__ __launch_bounds__(ELEMENT_THREADS) void muon_pack_kernel(MuonArgs a) 
 
 enum MuonProduct { MUON_GRAM, MUON_SQUARE, MUON_APPLY, MUON_LAST };
 
+// Neighbouring workgroups make tiles of the same rows and columns: tiles are numbered in strips of eight rows (of eight columns where only those on
+// and above the diagonal count), across the strip first.
+constexpr int STRIP = 8;
+
 // Tile `t` of the upper triangle, column by column: (0,0), (0,1), (1,1), (0,2), ..
 __device__ __forceinline__ void triangle(int t, int& i, int& j) {
   j = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
   while ((int64_t)j * (j + 1) / 2 > t) --j;
   while ((int64_t)(j + 1) * (j + 2) / 2 <= t) ++j;
   i = t - (int)((int64_t)j * (j + 1) / 2);
+}
+
+// The same in strips, of n columns: strip g has the 8 g rows above its own triangle.
+__device__ __forceinline__ void triangle_in_strips(int t, int n, int& i, int& j) {
+  auto before = [](int64_t g) { return STRIP * STRIP * g * (g - 1) / 2 + STRIP * (STRIP + 1) / 2 * g; };
+  int g = (int)sqrtf(t * (2.f / (STRIP * STRIP)));
+  while (before(g) > t) --g;
+  while (before(g + 1) <= t) ++g;
+  const int wide = n - g * STRIP < STRIP ? n - g * STRIP : STRIP, in = t - (int)before(g), above = g * STRIP * wide;
+  if (in < above) {
+    i = in / wide;
+    j = g * STRIP + in % wide;
+  } else {
+    triangle(in - above, i, j);
+    i += g * STRIP;
+    j += g * STRIP;
+  }
 }
 
 // A wavefront's operands for 16 contraction indices: BM blocks of rows of the left matrix, BN of the right one.
@@ -183,20 +251,20 @@ typedef float Tile[32][33];
 
 // What becomes of 32 x 32 values of a product (times 2^24, in the wavefront's tile): block (rb, cb).
 template <MuonProduct KIND>
-__device__ __forceinline__ void finish(const MuonArgs& a, const MuonItem& m, int turn, int rb, int cb, const Tile& tile) {
+__device__ __forceinline__ void finish(const MuonTable& t, const Matrix& m, int turn, int rb, int cb, const Tile& tile) {
   constexpr bool SYMMETRIC = KIND == MUON_GRAM || KIND == MUON_SQUARE;
   const int lane = threadIdx.x & 63, r = lane & 31, k8 = (lane >> 5) * 8;
-  const int P = pad32(m.p) / 32, Q = pad32(m.q) / 32;
   if constexpr (KIND == MUON_LAST) {
-    const float keep = 1.f - a.lr * a.decay, by = a.lr * m.scale * UNHOLD2;
-    const bool tall = m.rows > m.cols;
-#pragma unroll 4
+    const float keep = 1.f - t.lr * t.decay, by = t.lr * m.m.scale * UNHOLD2;
+    const int row = (m.tall ? cb : rb) * 32 + (lane >> 5), col = (m.tall ? rb : cb) * 32 + r;
+    const int64_t at = (int64_t)row * m.m.cols + col;
+    float w[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i] = m.m.w_in && row + i * 2 < m.m.rows && col < m.m.cols ? m.m.w_in[at + (int64_t)i * 2 * m.m.cols] : 0.f;
+#pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int slow = i * 2 + (lane >> 5), row = (tall ? cb : rb) * 32 + slow, col = (tall ? rb : cb) * 32 + r;
-      if (row < m.rows && col < m.cols) {
-        const int64_t at = (int64_t)row * m.cols + col;
-        m.w_out[at] = (m.w_in ? keep * m.w_in[at] : 0.f) - by * (tall ? tile[r][slow] : tile[slow][r]);
-      }
+      const int slow = i * 2 + (lane >> 5);
+      if (row + i * 2 < m.m.rows && col < m.m.cols) m.m.w_out[at + (int64_t)i * 2 * m.m.cols] = keep * w[i] - by * (m.tall ? tile[r][slow] : tile[slow][r]);
     }
     return;
   }
@@ -206,7 +274,7 @@ __device__ __forceinline__ void finish(const MuonArgs& a, const MuonItem& m, int
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int k = half * 16 + k8;
-      const int64_t block = way == 0 ? (int64_t)rb * (SYMMETRIC ? P : Q) * 2 + cb * 2 + half : (int64_t)cb * P * 2 + rb * 2 + half;
+      const int64_t block = way == 0 ? (int64_t)rb * (SYMMETRIC ? m.P : m.Q) * 2 + cb * 2 + half : (int64_t)cb * m.P * 2 + rb * 2 + half;
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = (way == 0 ? tile[r][k + e] : tile[k + e][r]) * UNHOLD;
@@ -223,7 +291,7 @@ __device__ __forceinline__ void finish(const MuonArgs& a, const MuonItem& m, int
         hi[e] = h;
         lo[e] = l;
       }
-      uint16_t* to = (KIND == MUON_GRAM ? m.a : KIND == MUON_SQUARE ? m.b : way == 0 ? m.x : m.xt[turn ^ 1]) + block * BLOCK + lane * 8;
+      uint16_t* to = (KIND == MUON_GRAM ? m.a : KIND == MUON_SQUARE ? m.b : way == 0 ? m.x : (turn ? m.xt0 : m.xt1)) + block * BLOCK + lane * 8;
       *reinterpret_cast<half8*>(to) = hi;
       *reinterpret_cast<half8*>(to + 512) = lo;
     }
@@ -233,30 +301,31 @@ __device__ __forceinline__ void finish(const MuonArgs& a, const MuonItem& m, int
 // One product; a workgroup makes B x B blocks, its four wavefronts a quarter of the contraction each, straight from memory's own layout into registers, DEPTH steps
 // of 16 ahead.  A and B are symmetric: of each pair of blocks one is computed and both are stored.
 template <MuonProduct KIND, int B, int DEPTH>
-__global__ __launch_bounds__(256) void muon_product_kernel(MuonArgs a, int turn) {
+__global__ __launch_bounds__(256) void muon_product_kernel(const MuonTable* t, int turn) {
   constexpr bool SYMMETRIC = KIND == MUON_GRAM || KIND == MUON_SQUARE;
+  // a block's parts: those of the wavefronts behind the one that adds them up
   __shared__ union {
-    float4 part[4][B * B][4][64];                        // wavefront, block, four of its sixteen registers
+    float4 part[B * B][3][4][64];                        // block, wavefront, four of its sixteen registers
     Tile tile[4];
   } lds;
-  const MuonItem& m = item_of(a, blockIdx.x);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int P = pad32(m.p) / 32, Q = pad32(m.q) / 32, columns = SYMMETRIC ? P : Q;
+  const Matrix m = matrix_of(*t, SYMMETRIC ? MUON_SYMMETRIC_GRID : MUON_APPLY_GRID);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, columns = SYMMETRIC ? m.P : m.Q;
   int ti, tj;
   if (SYMMETRIC) {
-    triangle(blockIdx.x - m.first, ti, tj);
+    triangle_in_strips(m.block, (m.P + B - 1) / B, ti, tj);
   } else {
-    const int tiles = (Q + B - 1) / B;
-    ti = (blockIdx.x - m.first) / tiles;
-    tj = (blockIdx.x - m.first) % tiles;
+    const int rows = (m.P + B - 1) / B, tiles = STRIP * ((m.Q + B - 1) / B), strip = m.block / tiles, in = m.block % tiles;
+    const int high = rows - strip * STRIP < STRIP ? rows - strip * STRIP : STRIP;
+    ti = strip * STRIP + in % high;
+    tj = in / high;
   }
-  const int kb = KIND == MUON_GRAM ? Q * 2 : P * 2, each = (kb + 3) / 4, k0 = wave * each, k1 = k0 + each < kb ? k0 + each : kb;
+  const int kb = (KIND == MUON_GRAM ? m.Q : m.P) * 2, each = (kb + 3) / 4, k0 = wave * each, k1 = k0 + each < kb ? k0 + each : kb;
   const uint16_t* l0 = (KIND == MUON_GRAM ? m.x : KIND == MUON_SQUARE ? m.a : m.b) + lane * 8;
-  const uint16_t* r0 = (KIND == MUON_GRAM ? m.x : KIND == MUON_SQUARE ? m.a : m.xt[turn]) + lane * 8;
+  const uint16_t* r0 = (KIND == MUON_GRAM ? m.x : KIND == MUON_SQUARE ? m.a : (turn ? m.xt1 : m.xt0)) + lane * 8;
   const uint16_t *left[B], *right[B];
 #pragma unroll
   for (int i = 0; i < B; ++i) {                          // (blocks beyond the edge: the last one again, and nothing is stored)
-    const int rb = ti * B + i < P ? ti * B + i : P - 1, cb = tj * B + i < columns ? tj * B + i : columns - 1;
+    const int rb = ti * B + i < m.P ? ti * B + i : m.P - 1, cb = tj * B + i < columns ? tj * B + i : columns - 1;
     left[i] = l0 + (int64_t)rb * kb * BLOCK;
     right[i] = r0 + (int64_t)cb * kb * BLOCK;
   }
@@ -268,35 +337,44 @@ __global__ __launch_bounds__(256) void muon_product_kernel(MuonArgs a, int turn)
   if (k0 < k1) {
     Operands<B, B> o[DEPTH];
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) o[d].load(left, right, k0 + d < k1 ? k0 + d : k1 - 1);
+    for (int d = 0; d < DEPTH; ++d)
+      if (k0 + d < k1) o[d].load(left, right, k0 + d);
     for (int k = k0; k < k1; k += DEPTH)
 #pragma unroll
       for (int d = 0; d < DEPTH; ++d) {
         if (k + d < k1) o[d].multiply(acc);
-        o[d].load(left, right, k + d + DEPTH < k1 ? k + d + DEPTH : k1 - 1);
+        if (k + d + DEPTH < k1) o[d].load(left, right, k + d + DEPTH);
       }
   }
-  // the wavefronts' parts, in their order: a wavefront adds up a quarter of the blocks (B = 2), or the first one all of one block
+  // a block's parts are added up by the wavefront of its number: its own, then those of the ones behind it, around
+#pragma unroll
+  for (int i = 0; i < B; ++i)
+#pragma unroll
+    for (int j = 0; j < B; ++j) {
+      const int behind = (wave - (i * B + j) + 4) & 3;
+      if (behind > 0)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          lds.part[i * B + j][behind - 1][q][lane] = float4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+    }
+  __syncthreads();
+  const int rb = ti * B + wave / B, cb = tj * B + wave % B;
+  const bool mine = wave < B * B && rb < m.P && cb < columns && (!SYMMETRIC || rb <= cb);
+  float4 sum[4];
 #pragma unroll
   for (int i = 0; i < B; ++i)
 #pragma unroll
     for (int j = 0; j < B; ++j)
+      if (mine && wave == i * B + j)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) lds.part[wave][i * B + j][q][lane] = float4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
-  __syncthreads();
-  const int rb = ti * B + wave / B, cb = tj * B + wave % B;
-  const bool mine = wave < B * B && rb < P && cb < columns && (!SYMMETRIC || rb <= cb);
-  float4 sum[4];
-  if (mine)
+        for (int q = 0; q < 4; ++q) {
+          sum[q] = float4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      sum[q] = lds.part[0][wave][q][lane];
-#pragma unroll
-      for (int w = 1; w < 4; ++w) {
-        const float4 p = lds.part[w][wave][q][lane];
-        sum[q] = float4{sum[q].x + p.x, sum[q].y + p.y, sum[q].z + p.z, sum[q].w + p.w};
-      }
-    }
+          for (int w = 0; w < 3; ++w) {
+            const float4 p = lds.part[i * B + j][w][q][lane];
+            sum[q] = float4{sum[q].x + p.x, sum[q].y + p.y, sum[q].z + p.z, sum[q].w + p.w};
+          }
+        }
   __syncthreads();
   if (!mine) return;
   // a lane has one column and four times four rows one after another
@@ -311,25 +389,31 @@ __global__ __launch_bounds__(256) void muon_product_kernel(MuonArgs a, int turn)
   }
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  finish<KIND>(a, m, turn, rb, cb, tile);
+  finish<KIND>(*t, m, turn, rb, cb, tile);
 }
 
+// Workgroups of a launch, matrix by matrix.
 template <typename Count>
-unsigned place_items(MuonArgs& a, Count count) {
+unsigned place_items(MuonTable& t, int count, MuonGrid grid, Count of) {
   int64_t n = 0;
-  for (int i = 0; i < a.count; ++i) {
-    a.item[i].first = (int32_t)n;
-    n += count(a.item[i]);
+  for (int i = 0; i < RSLX_MUON_MAX_MATRICES; ++i) {
+    t.first[grid][i] = i < count ? (int32_t)n : INT32_MAX;
+    if (i < count) n += of(t.item[i].rows, t.item[i].cols);
   }
   return (unsigned)n;
 }
 
 }  // namespace
 
-hipError_t launch_muon(MuonArgs& a, int steps, hipStream_t stream) {
+size_t muon_item_bytes(int32_t rows, int32_t cols) {
+  const size_t P = pad32(rows < cols ? rows : cols), Q = pad32(rows < cols ? cols : rows);
+  return values_bytes(rows, cols) + MUON_NORM_BLOCKS * sizeof(double) + sizeof(uint16_t) * 2 * (3 * P * Q + 2 * P * P);
+}
+
+hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int steps, hipStream_t stream) {
   double values = 0, gram = 0, square = 0, apply = 0, planes = 0, symmetric = 0;
-  for (int i = 0; i < a.count; ++i) {
-    const double p = a.item[i].p, q = a.item[i].q;
+  for (int i = 0; i < count; ++i) {
+    const double rows = t.item[i].rows, cols = t.item[i].cols, p = rows < cols ? rows : cols, q = rows < cols ? cols : rows;
     values += p * q;
     gram += p * p * q;
     square += p * p * p;
@@ -337,30 +421,36 @@ hipError_t launch_muon(MuonArgs& a, int steps, hipStream_t stream) {
     planes += 4 * p * q;
     symmetric += 4 * p * p;
   }
-  const auto blocks32 = [](int n) { return (int64_t)(n + 31) / 32; };
-  unsigned grid = place_items(a, [](const MuonItem& m) { return (int64_t)norm_blocks(m); });
+  // tiles of b x b blocks
+  const auto symmetric_tiles = [](int b) {
+    return [=](int rows, int cols) {
+      const int64_t n = (pad32(rows < cols ? rows : cols) / 32 + b - 1) / b;
+      return n * (n + 1) / 2;
+    };
+  };
+  const auto apply_tiles = [](int b) { return [=](int rows, int cols) { return (int64_t)((pad32(rows) / 32 + b - 1) / b) * ((pad32(cols) / 32 + b - 1) / b); }; };
+  // blocks of 64 x 64 where they are as many as the GPU has compute units, of 32 x 32 otherwise
+  unsigned on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(2)), on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(2));
+  const bool large_symmetric = on_symmetric >= 256, large_apply = on_apply >= 256;
+  if (!large_symmetric) on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(1));
+  if (!large_apply) on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(1));
+  const unsigned on_pack = place_items(t, count, MUON_PACK_GRID, [](int rows, int cols) { return ((int64_t)(pad32(rows) / 32) * (pad32(cols) / 32) + 3) / 4; });
+  const unsigned on_momentum = place_items(t, count, MUON_MOMENTUM_GRID, [](int rows, int cols) { return (int64_t)norm_blocks(rows, cols); });
   {
     TraceScope trace(stream, "muon_momentum", 6 * values, 16 * values);
-    hipLaunchKernelGGL(muon_momentum_kernel, dim3(grid), dim3(ELEMENT_THREADS), 0, stream, a);
+    hipLaunchKernelGGL(muon_momentum_kernel, dim3(on_momentum), dim3(ELEMENT_THREADS), 0, stream, t, in_workspace);
   }
-  grid = place_items(a, [&](const MuonItem& m) { return (blocks32(m.p) * blocks32(m.q) + 3) / 4; });
   {
     TraceScope trace(stream, "muon_pack", values, 4 * values + 2 * planes);
-    hipLaunchKernelGGL(muon_pack_kernel, dim3(grid), dim3(ELEMENT_THREADS), 0, stream, a);
+    hipLaunchKernelGGL(muon_pack_kernel, dim3(on_pack), dim3(ELEMENT_THREADS), 0, stream, in_workspace);
   }
-  // blocks of 64 x 64 where they are as many as the GPU has compute units, of 32 x 32 otherwise
   auto product = [&](auto kind, const char* name, double flops, double bytes, int turn) {
     constexpr MuonProduct KIND = decltype(kind)::value;
-    auto tiles = [&](int b) {
-      return [=](const MuonItem& m) {
-        const int64_t rows = (blocks32(m.p) + b - 1) / b, cols = (blocks32(m.q) + b - 1) / b;
-        return KIND == MUON_GRAM || KIND == MUON_SQUARE ? rows * (rows + 1) / 2 : rows * cols;
-      };
-    };
+    constexpr bool SYMMETRIC = KIND == MUON_GRAM || KIND == MUON_SQUARE;
     TraceScope trace(stream, name, flops, bytes);
-    const unsigned grid = place_items(a, tiles(2));
-    if (grid >= 256) hipLaunchKernelGGL((muon_product_kernel<KIND, 2, 2>), dim3(grid), dim3(256), 0, stream, a, turn);
-    else hipLaunchKernelGGL((muon_product_kernel<KIND, 1, 4>), dim3(place_items(a, tiles(1))), dim3(256), 0, stream, a, turn);
+    const dim3 grid(SYMMETRIC ? on_symmetric : on_apply);
+    if (SYMMETRIC ? large_symmetric : large_apply) hipLaunchKernelGGL((muon_product_kernel<KIND, 2, 3>), grid, dim3(256), 0, stream, in_workspace, turn);
+    else hipLaunchKernelGGL((muon_product_kernel<KIND, 1, 4>), grid, dim3(256), 0, stream, in_workspace, turn);
   };
   for (int s = 0; s < steps; ++s) {
     product(std::integral_constant<MuonProduct, MUON_GRAM>(), "muon_gram", gram, planes + symmetric, s & 1);
