@@ -133,17 +133,20 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_kernel(RmsArgs a) {
 }
 
 // A lane's columns stay the same from row to row, and their gradients of the weight add up in its registers; what the workgroup holds in the end is one
-// row of partial sums, which norm_fold_kernel adds up in a fixed order.  Long rows (1024 lanes have 128 registers each) are not loaded ahead.
+// row of partial sums, which norm_fold_kernel adds up in a fixed order.  1024 lanes have 128 registers each: with 16 values a lane the sums lie in
+// LDS, where nobody else reads or writes a lane's, a row is not loaded ahead, and what is made of it is made twice (nothing is left on the stack that way).
 template <typename T, int W, int ITEMS, int TPR, bool WHOLE>
 __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_backward_kernel(RmsArgs a) {
   constexpr int ROWS = THREADS_OF<TPR> / TPR;
-  constexpr bool AHEAD = TPR < 1024 || ITEMS * W <= 8;
+  constexpr bool LONG = TPR == 1024 && ITEMS * W > 8;
   __shared__ float lds[2][TPR > 64 ? TPR / 64 : 1];
   __shared__ float join[ROWS > 1 ? (ROWS - 1) * TPR * ITEMS * W : 1];
+  __shared__ __attribute__((aligned(16))) float sums[LONG ? ITEMS * W * TPR : 4];
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   const float inv = 1.f / (float)a.cols;
   const int64_t stride = (int64_t)gridDim.x * ROWS;
   int64_t row = (int64_t)blockIdx.x * ROWS + sub;
+  auto sum_at = [&](int x) -> float4& { return *reinterpret_cast<float4*>(sums + (x / 4 * TPR + lane) * 4); };
   Pack<T, W> px[ITEMS], pd[ITEMS], pt[ITEMS];
   float rstd = 0.f;
   auto load = [&](int64_t r) {
@@ -152,54 +155,66 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_backward_kernel(RmsA
       for (int i = 0; i < ITEMS; ++i) {
         load_piece<T, W, WHOLE>(px[i], static_cast<const T*>(a.x) + r * a.ldx, (i * TPR + lane) * W, a.cols);
         load_piece<T, W, WHOLE>(pd[i], static_cast<const T*>(a.dy) + r * a.lddy, (i * TPR + lane) * W, a.cols);
-        if (a.y && a.residual) load_piece<T, W, WHOLE>(pt[i], static_cast<const T*>(a.residual) + r * a.ldr, (i * TPR + lane) * W, a.cols);
+        if (!LONG && a.y && a.residual) load_piece<T, W, WHOLE>(pt[i], static_cast<const T*>(a.residual) + r * a.ldr, (i * TPR + lane) * W, a.cols);
       }
       rstd = a.rstd[r];
     }
   };
-  if (AHEAD) load(row);
+  if (!LONG) load(row);
   Pack<float, W> w[ITEMS];
-  float dw[ITEMS * W];
+  float dw[LONG ? 4 : ITEMS * W];
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
 #pragma unroll
     for (int k = 0; k < W; ++k) {
       w[i].v[k] = 1.f;
-      dw[i * W + k] = 0.f;
+      if constexpr (!LONG) dw[i * W + k] = 0.f;
+      else if (k % 4 == 0) sum_at(i * W + k) = float4{0.f, 0.f, 0.f, 0.f};
     }
     if (a.weight) load_piece<float, W, WHOLE>(w[i], a.weight, (i * TPR + lane) * W, a.cols);
   }
   for (int turn = 0; row < a.rows; row += stride, turn ^= 1) {
-    if (!AHEAD) load(row);
-    float s[1] = {0.f}, h[ITEMS * W], g[ITEMS * W];
+    if (LONG) load(row);
+    float s[1] = {0.f}, h[LONG ? 1 : ITEMS * W], g[LONG ? 1 : ITEMS * W];
     const float scale = rstd;
-    Pack<T, W> t[ITEMS];
+    Pack<T, W> t[LONG ? 1 : ITEMS];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      t[i] = pt[i];
+      if constexpr (!LONG) t[i] = pt[i];
 #pragma unroll
       for (int k = 0; k < W; ++k) {
         const int x = i * W + k;
         const bool here = in_row<W, WHOLE>((i * TPR + lane) * W, k, a.cols);
-        const float d = here ? to_float(pd[i].v[k]) : 0.f;
-        h[x] = here ? to_float(px[i].v[k]) * scale : 0.f;
-        g[x] = here ? d * w[i].v[k] : 0.f;
-        dw[x] += d * h[x];
-        s[0] += g[x] * h[x];
+        const float d = here ? to_float(pd[i].v[k]) : 0.f, hx = here ? to_float(px[i].v[k]) * scale : 0.f, gx = here ? d * w[i].v[k] : 0.f;
+        s[0] += gx * hx;
+        if constexpr (!LONG) {
+          h[x] = hx;
+          g[x] = gx;
+          dw[x] += d * hx;
+        } else {
+          dw[x % 4] = d * hx;
+          if (x % 4 == 3) {
+            float4& to = sum_at(x);
+            to = float4{to.x + dw[0], to.y + dw[1], to.z + dw[2], to.w + dw[3]};
+          }
+        }
       }
     }
-    if (AHEAD) load(row + stride);
+    if (!LONG) load(row + stride);
     if (a.y) {
       row_sum<TPR, 1>(s, lds[turn]);
       const float mean = s[0] * inv;
       T* dx = static_cast<T*>(a.y) + row * a.ldy;
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
-        Pack<T, W> out;
+        Pack<T, W> out, late;
+        if (LONG && a.residual) load_piece<T, W, WHOLE>(late, static_cast<const T*>(a.residual) + row * a.ldr, (i * TPR + lane) * W, a.cols);
 #pragma unroll
         for (int k = 0; k < W; ++k) {
-          float v = scale * (g[i * W + k] - h[i * W + k] * mean);
-          if (a.residual) v += to_float(t[i].v[k]);
+          float v;
+          if constexpr (!LONG) v = scale * (g[i * W + k] - h[i * W + k] * mean);
+          else v = scale * (to_float(pd[i].v[k]) * w[i].v[k] - to_float(px[i].v[k]) * scale * mean);
+          if (a.residual) v += to_float(LONG ? late.v[k] : t[LONG ? 0 : i].v[k]);
           out.v[k] = from_float<T>(v);
         }
         store_piece<T, W, WHOLE>(out, dx, (i * TPR + lane) * W, a.cols);
@@ -223,7 +238,19 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_backward_kernel(RmsA
     for (int i = 0; i < ITEMS; ++i) {
       Pack<float, W> out;
 #pragma unroll
-      for (int k = 0; k < W; ++k) out.v[k] = dw[i * W + k];
+      for (int k = 0; k < W; ++k) {
+        if constexpr (LONG) {
+          if (k % 4 == 0) {
+            const float4 f = sum_at(i * W + k);
+            out.v[k] = f.x;
+            out.v[k + 1] = f.y;
+            out.v[k + 2] = f.z;
+            out.v[k + 3] = f.w;
+          }
+        } else {
+          out.v[k] = dw[i * W + k];
+        }
+      }
       store_piece<float, W, WHOLE>(out, to, (i * TPR + lane) * W, a.cols);
     }
   }
