@@ -602,11 +602,12 @@ bool rec_whole(const RecArgs& a, int size) {
   return a.D % W == 0 && fits(a.x) && fits(a.g) && fits(a.h) && fits(a.dh) && fits(a.dx) && fits(a.dg);
 }
 
-// Outputs of 32 MB and more are written past the caches; inputs are read past them where the call moves more than the last-level cache's 256 MB and reads them once.
+// Outputs of 16 MB and more, which the dies' L2 could not keep beside the inputs, are written past the caches (gradients of a minibatch's roll-out: 28 us, through
+// them 41); inputs are read past them where the call moves more than the last-level cache's 256 MB and reads them once (a roll-out: 65 us, through them 73).
 int stream_of(const RecArgs& a, int size) {
   const double matrix = (double)a.T * a.N * a.D * size;
   const int outputs = a.h.p ? 1 : 2, inputs = a.h.p ? 2 : 3;
-  if (outputs * matrix < 32e6) return 0;
+  if (outputs * matrix < (double)(16 << 20)) return 0;
   return a.pieces == 1 && (outputs + inputs) * matrix > 256e6 ? 2 : 1;
 }
 

@@ -49,6 +49,7 @@ struct RmsArgs {
   float* rstd;                            // forward: or null
   float* partials;                        // backward: [blocks][cols], or null where dweight is not asked for
   float* dweight;
+  int32_t past;                           // outputs go past the caches
 };
 int rms_backward_blocks(int64_t rows, int cols);
 hipError_t launch_rms_norm(const RmsArgs& a, int dtype, bool e4m3, hipStream_t stream);

@@ -53,4 +53,18 @@ __device__ __forceinline__ void store_piece(const Pack<T, W>& p, T* row, int c, 
   }
 }
 
+// As store_piece; `past`: past the caches, which keep what they hold (for outputs larger than they are; the same for all lanes).
+template <typename T, int W, bool WHOLE>
+__device__ __forceinline__ void store_piece(const Pack<T, W>& p, T* row, int c, int cols, bool past) {
+  constexpr int WORDS = sizeof(T) * W / 4;
+  typedef uint32_t Words __attribute__((ext_vector_type(WORDS), aligned(1)));
+  if (past && (WHOLE ? c < cols : c + W <= cols)) {
+    Words bits;
+    __builtin_memcpy(&bits, &p, sizeof p);
+    __builtin_nontemporal_store(bits, reinterpret_cast<Words*>(row + c));
+  } else {
+    store_piece<T, W, WHOLE>(p, row, c, cols);
+  }
+}
+
 }  // namespace rslx
