@@ -562,10 +562,11 @@ int32_t rslx_layer_norm_backward(int32_t dtype, const void* dy, int64_t lddy, co
  * x, g and h (and their gradients) are matrices [T, N, D]: views whose `head` is not used, under the conditions above.
  * A step's values reach no earlier step and no other episode, whatever they are; an infinite state may be a NaN some
  * steps later, where the product of the gates between is zero in fp32. */
-#define RSLX_REC_MAX_CHANNELS (1 << 30)
+#define RSLX_REC_MAX_TILES 16777215 /* 2^24 - 1 */
 typedef struct rslx_gated_rec {
   int32_t dtype;                 /* RSLX_F32, RSLX_BF16, RSLX_F16: x, g, h and their gradients; states are fp32 */
-  int32_t T, N, D;               /* T: 0..RSLX_ATTN_MAX_STEPS; N: 0 or more; D: 1 or more; N * D: to RSLX_REC_MAX_CHANNELS */
+  int32_t T, N, D;               /* T: 0..RSLX_ATTN_MAX_STEPS; N: 0 or more; D: 1 or more; N ceil(D / 64), in whole calls times the pieces
+                                    of 64 steps or more that long sequences are cut into: to RSLX_REC_MAX_TILES */
   const uint8_t* dones;          /* device [T, N] or NULL */
   const int32_t* lengths;        /* device [N] or NULL */
 } rslx_gated_rec;

@@ -9,14 +9,15 @@ using namespace rslx::host;
 namespace {
 
 RowSet block_of(const void* p, int64_t bytes) { return {p, bytes, {}, {p && bytes > 0 ? 1 : 0, 1, 1}}; }
+RowSet floats_of(const void* p, int64_t n) { return p ? host::rows_of(p, 1, n, 1, 4) : block_of(nullptr, 0); }
 
 // ---- gated linear recurrence ----------------------------------------------------------------------------------------
 int32_t check_rec(const rslx_gated_rec* a, const char* who, bool step) {
   if (!a) return fail(RSLX_ERR_INVALID_ARG, "%s: null description", who);
   RSLX_TRY(check_dtype(a->dtype, who));
   if (a->T < 0 || a->T > RSLX_ATTN_MAX_STEPS || a->N < 0 || a->D < 1) return fail(RSLX_ERR_SHAPE, "%s: T = %d, N = %d, D = %d", who, a->T, a->N, a->D);
-  if ((int64_t)a->N * a->D > RSLX_REC_MAX_CHANNELS)
-    return fail(RSLX_ERR_SHAPE, "%s: N * D = %lld exceeds %d", who, (long long)a->N * a->D, RSLX_REC_MAX_CHANNELS);
+  const int64_t tiles = (a->N > 0 ? (int64_t)a->N : 1) * (((int64_t)a->D + 63) / 64);
+  if (tiles > RSLX_REC_MAX_TILES) return fail(RSLX_ERR_SHAPE, "%s: N * ceil(D / 64) = %lld exceeds %d", who, (long long)tiles, RSLX_REC_MAX_TILES);
   if (step && (a->T != 1 || a->dones || a->lengths))
     return fail(RSLX_ERR_INVALID_ARG, "%s: one step has T = 1 and neither dones nor lengths", who);
   return RSLX_OK;
@@ -54,17 +55,26 @@ RecArgs rec_args(const rslx_gated_rec& a) {
   return r;
 }
 
+// A launch has fewer than 2^32 lanes.
+int32_t check_grid(const RecArgs& r, const char* who) {
+  if ((int64_t)r.N * ((r.D + 63) / 64) * r.pieces >= (int64_t)1 << 24)
+    return fail(RSLX_ERR_SHAPE, "%s: %d pieces of %d sequences of %d channels are too many", who, r.pieces, r.N, r.D);
+  return RSLX_OK;
+}
+
 size_t rec_workspace(const rslx_gated_rec* a, bool backward, const char* who) {
   if (check_rec(a, who, false) != RSLX_OK) return 0;
   Carver c(nullptr);
   RecArgs r = rec_args(*a);
   plan_recurrence(c, r, a->dtype, backward);
+  if (check_grid(r, who) != RSLX_OK) return 0;
   return c.off > 256 ? c.off : 256;
 }
 
 int32_t rec_plan(RecArgs& r, int dtype, bool backward, void* ws, size_t ws_bytes, const char* who) {
   Carver c(ws);
   plan_recurrence(c, r, dtype, backward);
+  RSLX_TRY(check_grid(r, who));
   if (c.off > 0 && (!ws || ws_bytes < c.off)) return fail(RSLX_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", who, ws_bytes, c.off);
   if (c.off > 0 && !aligned16(ws)) return fail(RSLX_ERR_INVALID_ARG, "%s: workspace not 16-byte aligned", who);
   return RSLX_OK;
@@ -121,8 +131,8 @@ int32_t rms_norm(int32_t dtype, bool e4m3, const void* x, int64_t ldx, const voi
   for (int i = 0; i < 2; ++i)
     for (int j = 0; j < 2; ++j)
       if (i == 1 || !e4m3) RSLX_TRY(check_in_place(out[i], in[j], rows, cols, who));
-  const Named all[] = {{out[0].rows(rows, cols), "y"}, {out[1].rows(rows, cols), "total"}, {block_of(scales, rows * 4), "scales"},
-                       {block_of(rstd, rows * 4), "rstd"}, {block_of(weight, (int64_t)cols * 4), "weight"}};
+  const Named all[] = {{out[0].rows(rows, cols), "y"}, {out[1].rows(rows, cols), "total"}, {floats_of(scales, rows), "scales"},
+                       {floats_of(rstd, rows), "rstd"}, {floats_of(weight, cols), "weight"}};
   RSLX_TRY(check_apart(all, 4, who));
   const Named statistics[] = {all[2], all[3], {in[0].rows(rows, cols), "x"}, {in[1].rows(rows, cols), "residual"}};
   RSLX_TRY(check_apart(statistics, 2, who));
@@ -284,8 +294,8 @@ int32_t rslx_rms_norm_backward(int32_t dtype, const void* dy, int64_t lddy, cons
   RSLX_TRY(check_written(out, rows, cols, who));
   if (!aligned16(weight_or_null)) return fail(RSLX_ERR_INVALID_ARG, "%s: weight not 16-byte aligned", who);
   for (const NormMatrix& m : in) RSLX_TRY(check_in_place(out, m, rows, cols, who));
-  const Named written[] = {{out.rows(rows, cols), "dx"}, {block_of(dweight_or_null, (int64_t)cols * 4), "dweight"},
-                           {block_of(weight_or_null, (int64_t)cols * 4), "weight"}, {block_of(rstd, rows * 4), "rstd"}};
+  const Named written[] = {{out.rows(rows, cols), "dx"}, {floats_of(dweight_or_null, cols), "dweight"},
+                           {floats_of(weight_or_null, cols), "weight"}, {floats_of(rstd, rows), "rstd"}};
   RSLX_TRY(check_apart(written, 2, who));
   const Named sums[] = {written[1], {in[0].rows(rows, cols), "dy"}, {in[1].rows(rows, cols), "total"}, {in[2].rows(rows, cols), "dtotal"}};
   RSLX_TRY(check_apart(sums, 1, who));

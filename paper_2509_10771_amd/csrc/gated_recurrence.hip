@@ -639,7 +639,7 @@ void run(const RecArgs& a, int dtype, bool maps, hipStream_t s) {
 // Forward, a wavefront along each sequence and 64 channels where that fills the GPU or one is enough for the steps; otherwise eight, in pieces where even
 // these are few.  Backward, the smallest workgroup that holds the sequence, the largest in pieces where none does.
 void plan_recurrence(host::Carver& c, RecArgs& a, int dtype, bool backward) {
-  const int64_t tiles = (int64_t)a.N * ((a.D + TILE - 1) / TILE);
+  const int64_t tiles = (int64_t)a.N * (((int64_t)a.D + TILE - 1) / TILE);
   a.pieces = 1;
   a.piece_steps = a.T;
   if (backward) {

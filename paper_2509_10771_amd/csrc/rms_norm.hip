@@ -297,10 +297,10 @@ void run_type(const RmsArgs& a, RmsKind kind, int blocks, hipStream_t s) {
 
 // Outputs of 16 MB and more, which the dies' L2 could not keep beside the inputs, go past the caches: 98304 rows of 512 in bf16 74.6 us, through them 78.8;
 // gradients of 24576 rows of 235 in fp32 23.9 and 27.7.
-constexpr int64_t PAST_BYTES = 16 << 20;
+constexpr double PAST_BYTES = 16 << 20;
 
 hipError_t run(RmsArgs a, int dtype, RmsKind kind, int blocks, hipStream_t s) {
-  const int64_t size = dtype == RSLX_F32 ? 4 : 2, n = a.rows * a.cols;
+  const double size = dtype == RSLX_F32 ? 4 : 2, n = (double)a.rows * a.cols;
   a.past = (a.total ? n * size : 0) + (a.y ? n * (kind == RMS_FORWARD_E4M3 ? 1 : size) : 0) >= PAST_BYTES;
   if (dtype == RSLX_F32) run_type<float>(a, kind, blocks, s);
   else if (dtype == RSLX_BF16) run_type<bf16_t>(a, kind, blocks, s);

@@ -37,6 +37,8 @@ def test_recurrence_shapes_and_types():
         rx.rslx_gated_recurrence_workspace_bytes(_rec(D=0))
     with pytest.raises(rx.RslxError, match="exceeds"):
         rx.rslx_gated_recurrence_workspace_bytes(_rec(N=1 << 16, D=1 << 15))
+    with pytest.raises(rx.RslxError, match="too many"):
+        rx.rslx_gated_recurrence_backward_workspace_bytes(_rec(T=1 << 20, N=1 << 16, D=1))
     with pytest.raises(rx.RslxError, match="more than 32 bits"):
         _rec(T=1 << 32)
     with pytest.raises(rx.RslxError, match="x is"):
@@ -132,7 +134,7 @@ def test_recurrence_workspace():
         _backward(_rec(T=8192, N=4, D=1024, dtype=BF16))
     n = rx.rslx_gated_recurrence_backward_workspace_bytes(_rec(T=8192, N=1, D=8))
     with pytest.raises(rx.RslxError, match="workspace"):
-        _backward(_rec(T=8192, N=1, D=8), ws=Z(n - 1, dtype=torch.uint8))
+        _backward(_rec(T=8192, N=1, D=8), ws=Z(n // 4, dtype=torch.uint8))       # (aligned rows are cut into half as many pieces as the query has to expect)
     with pytest.raises(rx.RslxError, match="workspace not 16-byte"):
         _backward(_rec(T=8192, N=1, D=8), ws=Z(n + 8, dtype=torch.uint8)[8:])
 
