@@ -77,6 +77,13 @@ __device__ __forceinline__ Matrix matrix_of(const MuonTable& t, MuonGrid grid) {
   return r;
 }
 
+// Loads and stores of global memory: pointers that come from the table would be accessed as any kind of memory, and those accesses are waited for
+// with every access of LDS.
+template <typename T> __device__ __forceinline__ T get(const T* p) { return *(const __attribute__((address_space(1))) T*)p; }
+template <typename T> __device__ __forceinline__ void set(T* p, T v) { *(__attribute__((address_space(1))) T*)p = v; }
+__device__ __forceinline__ half8 get8(const uint16_t* p) { return get(reinterpret_cast<const half8*>(p)); }
+__device__ __forceinline__ void set8(uint16_t* p, half8 v) { set(reinterpret_cast<half8*>(p), v); }
+
 // hi and lo of a value that is held times 2^12.
 __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
   hi = (_Float16)v;
@@ -115,20 +122,20 @@ __global__ __launch_bounds__(ELEMENT_THREADS) void muon_momentum_kernel(MuonTabl
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (i + k * stride < n) {
-        g[k] = m.grad[i + k * stride];
-        before[k] = m.m_in ? m.m_in[i + k * stride] : 0.f;
+        g[k] = get(m.grad + i + k * stride);
+        before[k] = m.m_in ? get(m.m_in + i + k * stride) : 0.f;
       }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (i + k * stride < n) {
         const float now = fmaf(t.momentum, before[k], g[k]), u = t.nesterov ? fmaf(t.momentum, now, g[k]) : now;
-        if (m.m_out) m.m_out[i + k * stride] = now;
-        x.u[i + k * stride] = u;
+        if (m.m_out) set(m.m_out + i + k * stride, now);
+        set(x.u + i + k * stride, u);
         sum += (double)u * u;
       }
   }
   sum = group_sum(sum);
-  if (threadIdx.x == 0) x.norm[x.block] = sum;
+  if (threadIdx.x == 0) set(x.norm + x.block, sum);
 }
 
 // X and X transposed from u: a wavefront makes 32 x 32 values of X.
@@ -143,10 +150,10 @@ __global__ __launch_bounds__(ELEMENT_THREADS) void muon_pack_kernel(const MuonTa
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int row = (m.tall ? q0 : p0) + i * 2 + (lane >> 5), col = (m.tall ? p0 : q0) + (lane & 31);
-    u[i] = row < m.m.rows && col < m.m.cols ? m.u[(int64_t)row * m.m.cols + col] : 0.f;
+    u[i] = row < m.m.rows && col < m.m.cols ? get(m.u + (int64_t)row * m.m.cols + col) : 0.f;
   }
   double sum = 0.0;
-  for (int i = threadIdx.x; i < norm_blocks(m.m.rows, m.m.cols); i += ELEMENT_THREADS) sum += m.norm[i];
+  for (int i = threadIdx.x; i < norm_blocks(m.m.rows, m.m.cols); i += ELEMENT_THREADS) sum += get(m.norm + i);
   sum = group_sum(sum);
   const double inv = sum == 0.0 ? 0.0 : (double)HOLD / sqrt(sum);
 #pragma unroll
@@ -169,8 +176,8 @@ __global__ __launch_bounds__(ELEMENT_THREADS) void muon_pack_kernel(const MuonTa
       lo[e] = l;
     }
     uint16_t* to = m.x + ((int64_t)(p0 >> 5) * (m.Q * 2) + (q0 >> 4) + half) * BLOCK + lane * 8;
-    *reinterpret_cast<half8*>(to) = hi;
-    *reinterpret_cast<half8*>(to + 512) = lo;
+    set8(to, hi);
+    set8(to + 512, lo);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       _Float16 h, l;
@@ -179,8 +186,8 @@ __global__ __launch_bounds__(ELEMENT_THREADS) void muon_pack_kernel(const MuonTa
       lo[e] = l;
     }
     to = m.xt0 + ((int64_t)(q0 >> 5) * (m.P * 2) + (p0 >> 4) + half) * BLOCK + lane * 8;
-    *reinterpret_cast<half8*>(to) = hi;
-    *reinterpret_cast<half8*>(to + 512) = lo;
+    set8(to, hi);
+    set8(to + 512, lo);
   }
 }
 
@@ -189,6 +196,13 @@ enum MuonProduct { MUON_GRAM, MUON_SQUARE, MUON_APPLY, MUON_LAST };
 // Neighbouring workgroups make tiles of the same rows and columns: tiles are numbered in strips of eight rows (of eight columns where only those on
 // and above the diagonal count), across the strip first.
 constexpr int STRIP = 8;
+
+// Tile `t` of rows x cols.
+__device__ __forceinline__ void tile_in_strips(int t, int rows, int cols, int& i, int& j) {
+  const int strip = t / (STRIP * cols), in = t % (STRIP * cols), high = rows - strip * STRIP < STRIP ? rows - strip * STRIP : STRIP;
+  i = strip * STRIP + in % high;
+  j = in / high;
+}
 
 // Tile `t` of the upper triangle, column by column: (0,0), (0,1), (1,1), (0,2), ..
 __device__ __forceinline__ void triangle(int t, int& i, int& j) {
@@ -222,13 +236,13 @@ struct Operands {
   __device__ __forceinline__ void load(const uint16_t* const (&left)[BM], const uint16_t* const (&right)[BN], int k) {
 #pragma unroll
     for (int i = 0; i < BM; ++i) {
-      lh[i] = *reinterpret_cast<const half8*>(left[i] + (int64_t)k * BLOCK);
-      ll[i] = *reinterpret_cast<const half8*>(left[i] + (int64_t)k * BLOCK + 512);
+      lh[i] = get8(left[i] + (int64_t)k * BLOCK);
+      ll[i] = get8(left[i] + (int64_t)k * BLOCK + 512);
     }
 #pragma unroll
     for (int j = 0; j < BN; ++j) {
-      rh[j] = *reinterpret_cast<const half8*>(right[j] + (int64_t)k * BLOCK);
-      rl[j] = *reinterpret_cast<const half8*>(right[j] + (int64_t)k * BLOCK + 512);
+      rh[j] = get8(right[j] + (int64_t)k * BLOCK);
+      rl[j] = get8(right[j] + (int64_t)k * BLOCK + 512);
     }
   }
   __device__ __forceinline__ void multiply(float16v (&acc)[BM][BN]) const {
@@ -260,11 +274,11 @@ __device__ __forceinline__ void finish(const MuonTable& t, const Matrix& m, int 
     const int64_t at = (int64_t)row * m.m.cols + col;
     float w[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) w[i] = m.m.w_in && row + i * 2 < m.m.rows && col < m.m.cols ? m.m.w_in[at + (int64_t)i * 2 * m.m.cols] : 0.f;
+    for (int i = 0; i < 16; ++i) w[i] = m.m.w_in && row + i * 2 < m.m.rows && col < m.m.cols ? get(m.m.w_in + at + (int64_t)i * 2 * m.m.cols) : 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int slow = i * 2 + (lane >> 5);
-      if (row + i * 2 < m.m.rows && col < m.m.cols) m.m.w_out[at + (int64_t)i * 2 * m.m.cols] = keep * w[i] - by * (m.tall ? tile[r][slow] : tile[slow][r]);
+      if (row + i * 2 < m.m.rows && col < m.m.cols) set(m.m.w_out + at + (int64_t)i * 2 * m.m.cols, keep * w[i] - by * (m.tall ? tile[r][slow] : tile[slow][r]));
     }
     return;
   }
@@ -279,7 +293,7 @@ __device__ __forceinline__ void finish(const MuonTable& t, const Matrix& m, int 
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = (way == 0 ? tile[r][k + e] : tile[k + e][r]) * UNHOLD;
       if constexpr (KIND == MUON_SQUARE) {
-        const half8 h = *reinterpret_cast<const half8*>(m.a + block * BLOCK + lane * 8), l = *reinterpret_cast<const half8*>(m.a + block * BLOCK + 512 + lane * 8);
+        const half8 h = get8(m.a + block * BLOCK + lane * 8), l = get8(m.a + block * BLOCK + 512 + lane * 8);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = NS_C * v[e] + NS_B * ((float)h[e] + (float)l[e]) + (rb == cb && r == k + e ? NS_A * HOLD : 0.f);
       }
@@ -292,8 +306,8 @@ __device__ __forceinline__ void finish(const MuonTable& t, const Matrix& m, int 
         lo[e] = l;
       }
       uint16_t* to = (KIND == MUON_GRAM ? m.a : KIND == MUON_SQUARE ? m.b : way == 0 ? m.x : (turn ? m.xt0 : m.xt1)) + block * BLOCK + lane * 8;
-      *reinterpret_cast<half8*>(to) = hi;
-      *reinterpret_cast<half8*>(to + 512) = lo;
+      set8(to, hi);
+      set8(to + 512, lo);
     }
   }
 }
@@ -314,10 +328,7 @@ __global__ __launch_bounds__(256) void muon_product_kernel(const MuonTable* t, i
   if (SYMMETRIC) {
     triangle_in_strips(m.block, (m.P + B - 1) / B, ti, tj);
   } else {
-    const int rows = (m.P + B - 1) / B, tiles = STRIP * ((m.Q + B - 1) / B), strip = m.block / tiles, in = m.block % tiles;
-    const int high = rows - strip * STRIP < STRIP ? rows - strip * STRIP : STRIP;
-    ti = strip * STRIP + in % high;
-    tj = in / high;
+    tile_in_strips(m.block, (m.P + B - 1) / B, (m.Q + B - 1) / B, ti, tj);
   }
   const int kb = (KIND == MUON_GRAM ? m.Q : m.P) * 2, each = (kb + 3) / 4, k0 = wave * each, k1 = k0 + each < kb ? k0 + each : kb;
   const uint16_t* l0 = (KIND == MUON_GRAM ? m.x : KIND == MUON_SQUARE ? m.a : m.b) + lane * 8;
@@ -392,6 +403,106 @@ __global__ __launch_bounds__(256) void muon_product_kernel(const MuonTable* t, i
   finish<KIND>(*t, m, turn, rb, cb, tile);
 }
 
+// The same product with tiles of 4 RW x 4 blocks, for matrices whose tiles fill the GPU: the kernel above reads 8 KB for every 12 matrix instructions, and is bound
+// by what the L2 delivers (16 TB/s, the matrix cores 39 % busy).  Here a wavefront has RW rows of blocks to itself, straight from memory, and the four columns
+// that all of them need come through LDS, two steps of 16 at a time, the next ones on their way in registers.
+template <MuonProduct KIND, int RW>
+__global__ __launch_bounds__(256) void muon_large_kernel(const MuonTable* t, int turn) {
+  constexpr int CW = 4, UNITS = 256;                     // columns of blocks; units of 16 bytes that two steps of a column are
+  __shared__ union {
+    half8 right[2][CW][2][2][64];                        // turn, column, step, hi and lo
+    Tile tile[4];
+  } lds;
+  const Matrix m = matrix_of(*t, MUON_APPLY_GRID);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int ti, tj;
+  tile_in_strips(m.block, (m.P + 4 * RW - 1) / (4 * RW), (m.Q + CW - 1) / CW, ti, tj);
+  const int kb = m.P * 2, stages = m.P;
+  const uint16_t *left[RW], *right[CW];
+  const int row0 = (ti * 4 + wave) * RW, col0 = tj * CW;
+#pragma unroll
+  for (int i = 0; i < RW; ++i) left[i] = m.b + lane * 8 + (int64_t)(row0 + i < m.P ? row0 + i : m.P - 1) * kb * BLOCK;
+#pragma unroll
+  for (int j = 0; j < CW; ++j) right[j] = (turn ? m.xt1 : m.xt0) + threadIdx.x * 8 + (int64_t)(col0 + j < m.Q ? col0 + j : m.Q - 1) * kb * BLOCK;
+  float16v acc[RW][CW];
+#pragma unroll
+  for (int i = 0; i < RW; ++i)
+#pragma unroll
+    for (int j = 0; j < CW; ++j) acc[i][j] = float16v{};
+  half8 ahead[CW], lh[2][RW], ll[2][RW];
+  auto ask = [&](int s) {
+#pragma unroll
+    for (int j = 0; j < CW; ++j) ahead[j] = get8(right[j] + (int64_t)s * 2 * BLOCK);
+  };
+  auto put = [&](int s) {
+#pragma unroll
+    for (int j = 0; j < CW; ++j) (&lds.right[s & 1][j][0][0][0])[threadIdx.x] = ahead[j];
+  };
+  auto ask_left = [&](int h, int k) {
+#pragma unroll
+    for (int i = 0; i < RW; ++i) {
+      lh[h][i] = get8(left[i] + (int64_t)k * BLOCK);
+      ll[h][i] = get8(left[i] + (int64_t)k * BLOCK + 512);
+    }
+  };
+  static_assert(sizeof lds.right[0][0] == UNITS * 16, "a thread has one unit of a column");
+  ask(0);
+  ask_left(0, 0);
+  ask_left(1, 1);
+  put(0);
+  if (stages > 1) ask(1);
+  __syncthreads();
+  for (int s = 0; s < stages; ++s) {
+    if (s + 1 < stages) {
+      put(s + 1);                                        // (read last in front of the barrier behind stage s - 1)
+      if (s + 2 < stages) ask(s + 2);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < CW; j += 2) {
+        half8 rh[2], rl[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          rh[c] = lds.right[s & 1][j + c][h][0][lane];
+          rl[c] = lds.right[s & 1][j + c][h][1][lane];
+        }
+#pragma unroll
+        for (int i = 0; i < RW; ++i)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) acc[i][j + c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[h][i], rl[c], acc[i][j + c], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < RW; ++i)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) acc[i][j + c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ll[h][i], rh[c], acc[i][j + c], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < RW; ++i)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) acc[i][j + c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[h][i], rh[c], acc[i][j + c], 0, 0, 0);
+      }
+      if (s + 1 < stages) ask_left(h, s * 2 + 2 + h);
+    }
+    __syncthreads();
+  }
+  Tile& tile = lds.tile[wave];
+#pragma unroll
+  for (int i = 0; i < RW; ++i)
+#pragma unroll
+    for (int j = 0; j < CW; ++j) {
+      const int rb = row0 + i, cb = col0 + j;
+      if (rb >= m.P || cb >= m.Q) continue;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) tile[(q >> 2) * 8 + (lane >> 5) * 4 + (q & 3)][lane & 31] = acc[i][j][q];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      finish<KIND>(*t, m, turn, rb, cb, tile);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+}
+
+enum MuonShape { SMALL, MEDIUM, LARGE };                 // tiles of 32 x 32, 64 x 64, 256 x 128
+
 // Workgroups of a launch, matrix by matrix.
 template <typename Count>
 unsigned place_items(MuonTable& t, int count, MuonGrid grid, Count of) {
@@ -428,12 +539,23 @@ hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int ste
       return n * (n + 1) / 2;
     };
   };
-  const auto apply_tiles = [](int b) { return [=](int rows, int cols) { return (int64_t)((pad32(rows) / 32 + b - 1) / b) * ((pad32(cols) / 32 + b - 1) / b); }; };
-  // blocks of 64 x 64 where they are as many as the GPU has compute units, of 32 x 32 otherwise
-  unsigned on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(2)), on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(2));
-  const bool large_symmetric = on_symmetric >= 256, large_apply = on_apply >= 256;
-  if (!large_symmetric) on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(1));
-  if (!large_apply) on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(1));
+  const auto apply_tiles = [](int high, int wide) {
+    return [=](int rows, int cols) {
+      const int p = rows < cols ? rows : cols, q = rows < cols ? cols : rows;
+      return (int64_t)((pad32(p) / 32 + high - 1) / high) * ((pad32(q) / 32 + wide - 1) / wide);
+    };
+  };
+  // the largest tiles that are as many as the GPU has compute units, the smallest where none are
+  bool medium_symmetric = true;
+  MuonShape apply_shape = SMALL;
+  unsigned on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(2)), on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(8, 4));
+  if (on_symmetric < 256) {
+    medium_symmetric = false;
+    on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(1));
+  }
+  if (on_apply >= 256) apply_shape = LARGE;
+  else if ((on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(2, 2))) >= 256) apply_shape = MEDIUM;
+  else on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(1, 1));
   const unsigned on_pack = place_items(t, count, MUON_PACK_GRID, [](int rows, int cols) { return ((int64_t)(pad32(rows) / 32) * (pad32(cols) / 32) + 3) / 4; });
   const unsigned on_momentum = place_items(t, count, MUON_MOMENTUM_GRID, [](int rows, int cols) { return (int64_t)norm_blocks(rows, cols); });
   {
@@ -449,8 +571,10 @@ hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int ste
     constexpr bool SYMMETRIC = KIND == MUON_GRAM || KIND == MUON_SQUARE;
     TraceScope trace(stream, name, flops, bytes);
     const dim3 grid(SYMMETRIC ? on_symmetric : on_apply);
-    if (SYMMETRIC ? large_symmetric : large_apply) hipLaunchKernelGGL((muon_product_kernel<KIND, 2, 3>), grid, dim3(256), 0, stream, in_workspace, turn);
-    else hipLaunchKernelGGL((muon_product_kernel<KIND, 1, 4>), grid, dim3(256), 0, stream, in_workspace, turn);
+    const MuonShape shape = !SYMMETRIC ? apply_shape : medium_symmetric ? MEDIUM : SMALL;
+    if (shape == SMALL) hipLaunchKernelGGL((muon_product_kernel<KIND, 1, 4>), grid, dim3(256), 0, stream, in_workspace, turn);
+    else if (shape == MEDIUM) hipLaunchKernelGGL((muon_product_kernel<KIND, 2, 3>), grid, dim3(256), 0, stream, in_workspace, turn);
+    else if constexpr (!SYMMETRIC) hipLaunchKernelGGL((muon_large_kernel<KIND, 2>), grid, dim3(256), 0, stream, in_workspace, turn);
   };
   for (int s = 0; s < steps; ++s) {
     product(std::integral_constant<MuonProduct, MUON_GRAM>(), "muon_gram", gram, planes + symmetric, s & 1);
