@@ -447,40 +447,44 @@ __global__ __launch_bounds__(256) void muon_large_kernel(const MuonTable* t, int
   };
   static_assert(sizeof lds.right[0][0] == UNITS * 16, "a thread has one unit of a column");
   ask(0);
+  put(0);
+  ask(stages > 1 ? 1 : 0);                               // (in the order of the loop below, which waits for the columns alone that way)
+  __builtin_amdgcn_sched_barrier(0);
   ask_left(0, 0);
   ask_left(1, 1);
-  put(0);
-  if (stages > 1) ask(1);
   __syncthreads();
-  for (int s = 0; s < stages; ++s) {
-    if (s + 1 < stages) {
-      put(s + 1);                                        // (read last in front of the barrier behind stage s - 1)
-      if (s + 2 < stages) ask(s + 2);
+  // Behind the last stage its columns and rows are asked for and put again, and not used: a branch between a load and its use would have the compiler wait for
+  // whatever the other way leaves.  The columns of a pair are read while the pair before it is multiplied.
+  half8 rh[2][2], rl[2][2];
+  auto read = [&](int s, int pair) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      rh[pair & 1][c] = lds.right[s & 1][(pair & 1) * 2 + c][pair >> 1][0][lane];
+      rl[pair & 1][c] = lds.right[s & 1][(pair & 1) * 2 + c][pair >> 1][1][lane];
     }
+  };
+  for (int s = 0; s < stages; ++s) {
+    read(s, 0);
+    put(s + 1);                                          // (read last in front of the barrier behind stage s - 1)
+    ask(s + 2 < stages ? s + 2 : stages - 1);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int pair = 0; pair < 4; ++pair) {
+      const int h = pair >> 1, j = (pair & 1) * 2, now = pair & 1;
+      if (pair < 3) read(s, pair + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int j = 0; j < CW; j += 2) {
-        half8 rh[2], rl[2];
+      for (int i = 0; i < RW; ++i)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          rh[c] = lds.right[s & 1][j + c][h][0][lane];
-          rl[c] = lds.right[s & 1][j + c][h][1][lane];
-        }
+        for (int c = 0; c < 2; ++c) acc[i][j + c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[h][i], rl[now][c], acc[i][j + c], 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < RW; ++i)
+      for (int i = 0; i < RW; ++i)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) acc[i][j + c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[h][i], rl[c], acc[i][j + c], 0, 0, 0);
+        for (int c = 0; c < 2; ++c) acc[i][j + c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ll[h][i], rh[now][c], acc[i][j + c], 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < RW; ++i)
+      for (int i = 0; i < RW; ++i)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) acc[i][j + c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ll[h][i], rh[c], acc[i][j + c], 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < RW; ++i)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) acc[i][j + c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[h][i], rh[c], acc[i][j + c], 0, 0, 0);
-      }
-      if (s + 1 < stages) ask_left(h, s * 2 + 2 + h);
+        for (int c = 0; c < 2; ++c) acc[i][j + c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[h][i], rh[now][c], acc[i][j + c], 0, 0, 0);
+      if (pair & 1) ask_left(h, s + 1 < stages ? s * 2 + 2 + h : s * 2 + h);
     }
     __syncthreads();
   }
