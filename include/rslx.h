@@ -609,8 +609,8 @@ int32_t rslx_rms_norm(int32_t dtype, const void* x, int64_t ldx, const void* res
                       int64_t ldy, float* rstd_or_null, void* stream);
 
 /* The same with y in a byte a value: e4m3 (4 bits of exponent, 3 of fraction, largest value 448; OCP's, without infinities),
- * y = scales[row] * y8, scales[row] = max |y| / 448 of the row (at least 2^-126: a row of zeros has zeros).  y8 is rounded to nearest, ties to
- * even; it overlaps nothing.  A row that holds a NaN is NaN, its scale too. */
+ * y = scales[row] * y8, scales[row] = max |y| / 448 of the row (at least 2^-126: with eps > 0 a row of zeros has zeros).  y8 is rounded to nearest,
+ * ties to even; it overlaps nothing.  A row that holds a NaN is NaN, its scale too. */
 int32_t rslx_rms_norm_e4m3(int32_t dtype, const void* x, int64_t ldx, const void* residual_or_null, int64_t ldr, int64_t rows,
                            int32_t cols, const float* weight_or_null, float eps, void* total_or_null, int64_t ldt, void* y8,
                            int64_t ldy, float* scales, float* rstd_or_null, void* stream);
@@ -635,7 +635,8 @@ int32_t rslx_rms_norm_backward(int32_t dtype, const void* dy, int64_t lddy, cons
  * operands are held as pairs of fp16 values (22 significant bits), sums in fp32.  u = 0 leaves X = 0; a matrix whose u
  * holds a value that is not finite gets NaN, the others of the call nothing of it.
  * w_in NULL: 0; m_in NULL: 0; m_out NULL: not kept (w_in = m_in = m_out = NULL, lr = -1: X itself).  w_out may be w_in and m_out
- * may be m_in; nothing else that is written may overlap what is read or written.  Pointers are aligned to 4 bytes; the descriptions are host memory. */
+ * may be m_in; nothing else that is written may overlap what is read or written.  Pointers are aligned to 4 bytes; the descriptions are host memory,
+ * read before the call returns (a captured call keeps them, lr among them). */
 #define RSLX_MUON_MAX_MATRICES 32
 #define RSLX_MUON_MAX_DIM 65536
 #define RSLX_MUON_MAX_STEPS 32

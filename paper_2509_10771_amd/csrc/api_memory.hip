@@ -107,12 +107,12 @@ int32_t check_written(const NormMatrix& m, int64_t rows, int32_t cols, const cha
   return RSLX_OK;
 }
 
-// An output may be one of the inputs, row by row in place.
+// An output may be one of the inputs, row by row in place; it must not overlap it otherwise (rows are loaded before earlier ones are stored).
 int32_t check_in_place(const NormMatrix& out, const NormMatrix& in, int64_t rows, int32_t cols, const char* who) {
-  if (!out.p || !in.p) return RSLX_OK;
-  char names[64];
-  snprintf(names, sizeof names, "%s and %s", out.name, in.name);
-  return host::check_in_place(out.rows(rows, cols), in.rows(rows, cols), who, names);
+  if (!out.p || !in.p || (out.p == in.p && (rows == 1 || out.ld == in.ld))) return RSLX_OK;
+  if (share_memory(out.rows(rows, cols), in.rows(rows, cols)))
+    return fail(RSLX_ERR_INVALID_ARG, "%s: %s and %s overlap and are not the same matrix", who, out.name, in.name);
+  return RSLX_OK;
 }
 
 int32_t rms_norm(int32_t dtype, bool e4m3, const void* x, int64_t ldx, const void* residual, int64_t ldr, int64_t rows, int32_t cols, const float* weight,
@@ -167,6 +167,7 @@ MuonTable* plan_muon(Carver& c, const rslx_muon_matrix* m, int32_t count, const 
   MuonTable* table = c.take<MuonTable>(1);
   for (int i = 0; i < count; ++i)
     t.item[i] = {m[i].w_in, m[i].w_out, m[i].grad, m[i].m_in, m[i].m_out, c.take<char>(muon_item_bytes(m[i].rows, m[i].cols)), m[i].rows, m[i].cols, m[i].scale};
+  t.parts = c.take<float>(plan_muon_parts(t, count));
   return table;
 }
 

@@ -22,6 +22,7 @@ namespace rslx {
 namespace {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
@@ -33,7 +34,7 @@ __host__ __device__ inline int pad32(int n) { return (n + 31) & ~31; }
 // A matrix as the kernels see it.  p <= q are its sides, X is [p, q] (the transposed update where the matrix is tall), P and Q blocks of 32 rows.
 struct Matrix {
   MuonItem m;
-  int p, q, P, Q, block;                  // block: the workgroup's among the matrix's
+  int p, q, P, Q, block, place, index;    // block: the workgroup's among the matrix's, place: among all; index: the matrix's
   bool tall;
   float* u;                               // the update before it is made orthogonal, [rows, cols]
   double* norm;                           // partial sums of its squares
@@ -58,6 +59,8 @@ __device__ __forceinline__ Matrix matrix_of(const MuonTable& t, MuonGrid grid) {
   Matrix r;
   __builtin_memcpy(&r.m, entry, sizeof entry);
   r.block = block - __builtin_amdgcn_readlane(begins, i);
+  r.place = block;
+  r.index = i;
   r.tall = r.m.rows > r.m.cols;
   r.p = r.tall ? r.m.cols : r.m.rows;
   r.q = r.tall ? r.m.rows : r.m.cols;
@@ -227,6 +230,20 @@ __device__ __forceinline__ void triangle_in_strips(int t, int n, int& i, int& j)
     i += g * STRIP;
     j += g * STRIP;
   }
+}
+
+// Tile `t` of 8 x 4 blocks among those that reach on or above the diagonal, row by row: row i has cols - 2 i.
+__device__ __forceinline__ void wide_triangle(int t, int cols, int& i, int& j) {
+  auto before = [&](int i) { return i * cols - i * (i - 1); };
+  const float b = cols + 1.f, under = b * b - 4.f * t;
+  i = (int)((b - sqrtf(under > 0.f ? under : 0.f)) * 0.5f);
+  while (i > 0 && before(i) > t) --i;
+  while (before(i + 1) <= t) ++i;
+  j = 2 * i + t - before(i);
+}
+__host__ __device__ inline int wide_triangle_tiles(int P) {
+  const int rows = (P + 7) / 8, cols = (P + 3) / 4;
+  return rows * cols - rows * (rows - 1);
 }
 
 // A wavefront's operands for 16 contraction indices: BM blocks of rows of the left matrix, BN of the right one.
@@ -403,27 +420,40 @@ __global__ __launch_bounds__(256) void muon_product_kernel(const MuonTable* t, i
   finish<KIND>(*t, m, turn, rb, cb, tile);
 }
 
-// The same product with tiles of 4 RW x 4 blocks, for matrices whose tiles fill the GPU: the kernel above reads 8 KB for every 12 matrix instructions, and is bound
-// by what the L2 delivers (16 TB/s, the matrix cores 39 % busy).  Here a wavefront has RW rows of blocks to itself, straight from memory, and the four columns
+// The same product with tiles of 8 x 4 blocks, for matrices whose tiles fill the GPU: the kernel above reads 8 KB for every 12 matrix instructions, and is bound
+// by what the L2 delivers (16 TB/s, the matrix cores 39 % busy).  Here a wavefront has two rows of blocks to itself, straight from memory, and the four columns
 // that all of them need come through LDS, two steps of 16 at a time, the next ones on their way in registers.
-template <MuonProduct KIND, int RW>
+// Symmetric products have too few such tiles: they are cut into pieces of the contraction as well, whose sums go to memory and are added up, in their order,
+// by muon_fold_kernel.
+constexpr int PART = 32 * 1024;                          // sums of a tile's 32 blocks: block, four of its sixteen registers, lane
+template <MuonProduct KIND>
 __global__ __launch_bounds__(256) void muon_large_kernel(const MuonTable* t, int turn) {
-  constexpr int CW = 4, UNITS = 256;                     // columns of blocks; units of 16 bytes that two steps of a column are
+  constexpr bool SYMMETRIC = KIND == MUON_GRAM || KIND == MUON_SQUARE;
+  constexpr int RW = 2, CW = 4, UNITS = 256;             // rows and columns of blocks; units of 16 bytes that two steps of a column are
   __shared__ union {
     half8 right[2][CW][2][2][64];                        // turn, column, step, hi and lo
     Tile tile[4];
   } lds;
-  const Matrix m = matrix_of(*t, MUON_APPLY_GRID);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int ti, tj;
-  tile_in_strips(m.block, (m.P + 4 * RW - 1) / (4 * RW), (m.Q + CW - 1) / CW, ti, tj);
-  const int kb = m.P * 2, stages = m.P;
+  const Matrix m = matrix_of(*t, SYMMETRIC ? MUON_SYMMETRIC_GRID : MUON_APPLY_GRID);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), columns = SYMMETRIC ? m.P : m.Q;
+  const int kb = (KIND == MUON_GRAM ? m.Q : m.P) * 2;
+  int ti, tj, first = 0, stages = kb / 2;
+  if constexpr (SYMMETRIC) {
+    const int tiles = wide_triangle_tiles(m.P), each = (stages + t->pieces - 1) / t->pieces;
+    first = m.block / tiles * each;
+    stages = stages - first < each ? stages - first : each;      // (may be none)
+    wide_triangle(m.block % tiles, (m.P + CW - 1) / CW, ti, tj);
+  } else {
+    tile_in_strips(m.block, (m.P + 4 * RW - 1) / (4 * RW), (m.Q + CW - 1) / CW, ti, tj);
+  }
+  const uint16_t* l0 = (KIND == MUON_GRAM ? m.x : KIND == MUON_SQUARE ? m.a : m.b) + (int64_t)first * 2 * BLOCK + lane * 8;
+  const uint16_t* r0 = (KIND == MUON_GRAM ? m.x : KIND == MUON_SQUARE ? m.a : (turn ? m.xt1 : m.xt0)) + (int64_t)first * 2 * BLOCK + threadIdx.x * 8;
   const uint16_t *left[RW], *right[CW];
   const int row0 = (ti * 4 + wave) * RW, col0 = tj * CW;
 #pragma unroll
-  for (int i = 0; i < RW; ++i) left[i] = m.b + lane * 8 + (int64_t)(row0 + i < m.P ? row0 + i : m.P - 1) * kb * BLOCK;
+  for (int i = 0; i < RW; ++i) left[i] = l0 + (int64_t)(row0 + i < m.P ? row0 + i : m.P - 1) * kb * BLOCK;
 #pragma unroll
-  for (int j = 0; j < CW; ++j) right[j] = (turn ? m.xt1 : m.xt0) + threadIdx.x * 8 + (int64_t)(col0 + j < m.Q ? col0 + j : m.Q - 1) * kb * BLOCK;
+  for (int j = 0; j < CW; ++j) right[j] = r0 + (int64_t)(col0 + j < columns ? col0 + j : columns - 1) * kb * BLOCK;
   float16v acc[RW][CW];
 #pragma unroll
   for (int i = 0; i < RW; ++i)
@@ -446,12 +476,14 @@ __global__ __launch_bounds__(256) void muon_large_kernel(const MuonTable* t, int
     }
   };
   static_assert(sizeof lds.right[0][0] == UNITS * 16, "a thread has one unit of a column");
-  ask(0);
+  if (stages > 0) ask(0);
   put(0);
-  ask(stages > 1 ? 1 : 0);                               // (in the order of the loop below, which waits for the columns alone that way)
+  if (stages > 0) ask(stages > 1 ? 1 : 0);               // (in the order of the loop below, which waits for the columns alone that way)
   __builtin_amdgcn_sched_barrier(0);
-  ask_left(0, 0);
-  ask_left(1, 1);
+  if (stages > 0) {
+    ask_left(0, 0);
+    ask_left(1, 1);
+  }
   __syncthreads();
   // Behind the last stage its columns and rows are asked for and put again, and not used: a branch between a load and its use would have the compiler wait for
   // whatever the other way leaves.  The columns of a pair are read while the pair before it is multiplied.
@@ -488,6 +520,18 @@ __global__ __launch_bounds__(256) void muon_large_kernel(const MuonTable* t, int
     }
     __syncthreads();
   }
+  if constexpr (SYMMETRIC) {
+    float4v* part = reinterpret_cast<float4v*>(t->parts + (int64_t)m.place * PART) + lane;
+#pragma unroll
+    for (int i = 0; i < RW; ++i)
+#pragma unroll
+      for (int j = 0; j < CW; ++j)
+        if (row0 + i <= col0 + j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            set(part + (((wave * RW + i) * CW + j) * 4 + q) * 64, float4v{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]});
+    return;
+  }
   Tile& tile = lds.tile[wave];
 #pragma unroll
   for (int i = 0; i < RW; ++i)
@@ -503,6 +547,40 @@ __global__ __launch_bounds__(256) void muon_large_kernel(const MuonTable* t, int
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
+}
+
+// A wavefront adds up the pieces of a block; eight workgroups have a tile.
+template <MuonProduct KIND>
+__global__ __launch_bounds__(256) void muon_fold_kernel(const MuonTable* t, int turn) {
+  __shared__ Tile tiles[4];
+  const Matrix m = matrix_of(*t, MUON_FOLD_GRID);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), block = m.block % 8 * 4 + wave;
+  const int count = wide_triangle_tiles(m.P), at = m.block / 8;
+  int ti, tj;
+  wide_triangle(at, (m.P + 3) / 4, ti, tj);
+  const int rb = ti * 8 + block / 4, cb = tj * 4 + block % 4;
+  if (rb > cb || cb >= m.P) return;
+  const float4v* part = reinterpret_cast<const float4v*>(t->parts + (int64_t)(t->first[MUON_SYMMETRIC_GRID][m.index] + at) * PART) + block * 256 + lane;
+  float4v sum[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) sum[q] = get(part + q * 64);
+  for (int piece = 1; piece < t->pieces; ++piece) {
+    part += (int64_t)count * (PART / 4);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum[q] += get(part + q * 64);
+  }
+  Tile& tile = tiles[wave];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int row = q * 8 + (lane >> 5) * 4, col = lane & 31;
+    tile[row][col] = sum[q].x;
+    tile[row + 1][col] = sum[q].y;
+    tile[row + 2][col] = sum[q].z;
+    tile[row + 3][col] = sum[q].w;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  finish<KIND>(*t, m, turn, rb, cb, tile);
 }
 
 enum MuonShape { SMALL, MEDIUM, LARGE };                 // tiles of 32 x 32, 64 x 64, 256 x 128
@@ -523,6 +601,21 @@ unsigned place_items(MuonTable& t, int count, MuonGrid grid, Count of) {
 size_t muon_item_bytes(int32_t rows, int32_t cols) {
   const size_t P = pad32(rows < cols ? rows : cols), Q = pad32(rows < cols ? cols : rows);
   return values_bytes(rows, cols) + MUON_NORM_BLOCKS * sizeof(double) + sizeof(uint16_t) * 2 * (3 * P * Q + 2 * P * P);
+}
+
+// Symmetric products go through the large tiles where these, in at most as many pieces as there are compute units for, fill the GPU, and a piece is 16 stages of 32
+// contraction indices or more.
+size_t plan_muon_parts(MuonTable& t, int count) {
+  int64_t tiles = 0, longest = INT32_MAX;
+  for (int i = 0; i < count; ++i) {
+    const int P = pad32(t.item[i].rows < t.item[i].cols ? t.item[i].rows : t.item[i].cols) / 32;
+    tiles += wide_triangle_tiles(P);
+    longest = P / 16 < longest ? P / 16 : longest;
+  }
+  int64_t pieces = tiles > 0 && tiles < 256 ? 256 / tiles : 1;
+  if (pieces > longest) pieces = longest;
+  t.pieces = tiles * pieces >= 200 ? (int32_t)pieces : 0;
+  return t.pieces > 0 ? (size_t)tiles * pieces * PART : 0;
 }
 
 hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int steps, hipStream_t stream) {
@@ -550,11 +643,16 @@ hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int ste
     };
   };
   // the largest tiles that are as many as the GPU has compute units, the smallest where none are
-  bool medium_symmetric = true;
-  MuonShape apply_shape = SMALL;
-  unsigned on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(2)), on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(8, 4));
-  if (on_symmetric < 256) {
-    medium_symmetric = false;
+  MuonShape symmetric_shape = SMALL, apply_shape = SMALL;
+  unsigned on_symmetric, on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(8, 4)), on_fold = 0;
+  if (t.pieces > 0) {
+    symmetric_shape = LARGE;
+    const auto tiles = [](int rows, int cols) { return (int64_t)wide_triangle_tiles(pad32(rows < cols ? rows : cols) / 32); };
+    on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, [&](int rows, int cols) { return tiles(rows, cols) * t.pieces; });
+    on_fold = place_items(t, count, MUON_FOLD_GRID, [&](int rows, int cols) { return tiles(rows, cols) * 8; });
+  } else if ((on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(2))) >= 256) {
+    symmetric_shape = MEDIUM;
+  } else {
     on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(1));
   }
   if (on_apply >= 256) apply_shape = LARGE;
@@ -573,12 +671,19 @@ hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int ste
   auto product = [&](auto kind, const char* name, double flops, double bytes, int turn) {
     constexpr MuonProduct KIND = decltype(kind)::value;
     constexpr bool SYMMETRIC = KIND == MUON_GRAM || KIND == MUON_SQUARE;
-    TraceScope trace(stream, name, flops, bytes);
     const dim3 grid(SYMMETRIC ? on_symmetric : on_apply);
-    const MuonShape shape = !SYMMETRIC ? apply_shape : medium_symmetric ? MEDIUM : SMALL;
-    if (shape == SMALL) hipLaunchKernelGGL((muon_product_kernel<KIND, 1, 4>), grid, dim3(256), 0, stream, in_workspace, turn);
-    else if (shape == MEDIUM) hipLaunchKernelGGL((muon_product_kernel<KIND, 2, 3>), grid, dim3(256), 0, stream, in_workspace, turn);
-    else if constexpr (!SYMMETRIC) hipLaunchKernelGGL((muon_large_kernel<KIND, 2>), grid, dim3(256), 0, stream, in_workspace, turn);
+    const MuonShape shape = SYMMETRIC ? symmetric_shape : apply_shape;
+    {
+      TraceScope trace(stream, name, flops, bytes);
+      if (shape == SMALL) hipLaunchKernelGGL((muon_product_kernel<KIND, 1, 4>), grid, dim3(256), 0, stream, in_workspace, turn);
+      else if (shape == MEDIUM) hipLaunchKernelGGL((muon_product_kernel<KIND, 2, 3>), grid, dim3(256), 0, stream, in_workspace, turn);
+      else hipLaunchKernelGGL((muon_large_kernel<KIND>), grid, dim3(256), 0, stream, in_workspace, turn);
+    }
+    if constexpr (SYMMETRIC)
+      if (shape == LARGE) {
+        TraceScope trace(stream, "muon_fold", 0, 0);
+        hipLaunchKernelGGL((muon_fold_kernel<KIND>), dim3(on_fold), dim3(256), 0, stream, in_workspace, turn);
+      }
   };
   for (int s = 0; s < steps; ++s) {
     product(std::integral_constant<MuonProduct, MUON_GRAM>(), "muon_gram", gram, planes + symmetric, s & 1);
