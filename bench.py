@@ -20,11 +20,12 @@ if ROOT not in sys.path:
 FP32_MFMA_PEAK_TFLOPS = 157.3        # the recurrent step kernels
 SPLIT_MFMA_PEAK_TFLOPS = 2516.6 / 6  # dense layers: six bf16 products (dense bf16 peak) for every fp32 product
 HBM_PEAK_GBS = 8000.0
-SEQUENCE_SOURCES = ("api_sequence.hip", "layer_norm.hip", "linear_attention.hip", "sequence.h", "typed.h")
+SEQUENCE_SOURCES = ("api_memory.hip", "api_sequence.hip", "gated_recurrence.hip", "layer_norm.hip", "linear_attention.hip", "memory.h", "muon.hip",
+                    "norm_rows.h", "overlap.h", "rms_norm.hip", "sequence.h", "typed.h")
 
 
 def kernel_sources_hash():
-    """sha256/16 of the HIP sources, the stamp the counter summaries under profiles/ carry.  The sequence operators' own files, which no
+    """sha256/16 of the HIP sources, the stamp the counter summaries under profiles/ carry.  The sequence operators' and the gated memory's own files, which no
     workload here launches anything of, are not part of it."""
     import glob
     import hashlib

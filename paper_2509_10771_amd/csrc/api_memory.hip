@@ -330,7 +330,8 @@ int32_t rslx_muon_step(const rslx_muon_matrix* matrices, int32_t count, const rs
   if (count == 0) return RSLX_OK;
   // everything that is written, then everything that is read, by matrix
   struct Range { uintptr_t lo, hi; int matrix; bool written; const char* name; };
-  std::vector<Range> ranges;
+  Range ranges[5 * RSLX_MUON_MAX_MATRICES];
+  int n = 0;
   for (int i = 0; i < count; ++i) {
     const rslx_muon_matrix& m = matrices[i];
     if (!m.w_out || !m.grad) return fail(RSLX_ERR_INVALID_ARG, "%s: matrix %d: null w_out or grad", who, i);
@@ -340,13 +341,14 @@ int32_t rslx_muon_step(const rslx_muon_matrix* matrices, int32_t count, const rs
     for (const auto& x : all) {
       const uintptr_t at = reinterpret_cast<uintptr_t>(x.p);
       if (at % sizeof(float)) return fail(RSLX_ERR_INVALID_ARG, "%s: matrix %d: %s not aligned to its type", who, i, x.name);
-      if (x.p) ranges.push_back({at, at + (uintptr_t)m.rows * m.cols * sizeof(float), i, x.written, x.name});
+      if (x.p) ranges[n++] = {at, at + (uintptr_t)m.rows * m.cols * sizeof(float), i, x.written, x.name};
     }
   }
   // by their starts: a range meets an earlier one where it starts before the furthest end of those that are written, or, written itself, of all
-  std::sort(ranges.begin(), ranges.end(), [](const Range& x, const Range& y) { return x.lo < y.lo; });
+  std::sort(ranges, ranges + n, [](const Range& x, const Range& y) { return x.lo < y.lo; });
   const Range *far = nullptr, *far_written = nullptr;
-  for (const Range& r : ranges) {
+  for (int i = 0; i < n; ++i) {
+    const Range& r = ranges[i];
     const Range* meets = r.written && far && r.lo < far->hi ? far : far_written && r.lo < far_written->hi ? far_written : nullptr;
     if (meets)
       return fail(RSLX_ERR_INVALID_ARG, "%s: %s of matrix %d overlaps %s of matrix %d", who, r.name, r.matrix, meets->name, meets->matrix);
