@@ -24,9 +24,9 @@ constexpr int TILE = W * ROW;             // channels of a workgroup
 constexpr int SETS = 64 / ROW;            // sets of lanes of a wavefront, one after another in time
 
 // f = sigmoid(g) = 1 / (1 + E) and 1 - f = E f, of E = exp(-g): each keeps its own digits.  Below -87, where f leaves fp32's normal numbers, g counts as -87.
-// For fp32 the exponential is that of the product g log2(e) in two parts, the rounded one for the instruction and what rounding left as a factor.  16-bit gates
-// do without the second: E is off by up to |g| 2^-24 more then, where the type's own half step is |g| 2^-9 or 2^-12 (and the instructions count: these
-// walks are bound by them; with the factor 8192 steps of 4 environments took 10 us more of 90).
+// For fp32 the exponential is that of the product g log2(e) in two parts, the rounded one for the instruction and what rounding left as a factor.  Gates of 16
+// bits do without the second: E is off by up to |g| 2^-24 more then, where the type's own half step is |g| 2^-9 or 2^-12 (8192 steps of
+// 4 environments, 1024 channels, in bf16: 71 us, with the factor 76).
 template <typename T>
 __device__ __forceinline__ void gate(float g, float& f, float& rest) {
   constexpr float LOG2E = 1.44269504f, LOG2E_REST = 1.92596299e-8f, LN2 = 0.693147181f;
@@ -636,15 +636,20 @@ void run(const RecArgs& a, int dtype, bool maps, hipStream_t s) {
 
 }  // namespace
 
-// Forward, a wavefront along each sequence and 64 channels where that fills the GPU or one is enough for the steps; otherwise eight, in pieces where even
-// these are few.  Backward, the smallest workgroup that holds the sequence, the largest in pieces where none does.
+// Forward, a wavefront along each sequence and 64 channels where these fill the GPU with eight wavefronts for each compute unit, or where 16 steps are all;
+// otherwise four, 64 steps at a time, in about 1024 pieces where these are few (100 steps of 300 sequences of 256 channels in bf16: 14.1 us, with one
+// 16.7; 777 steps of 37 of 200 in fp32: 32, in 512 pieces 37, in 2048 31; 8192 steps of 4 of 1024 in bf16: 72, in 512 pieces 81).
+// Backward, the smallest workgroup that holds the sequence: 32, 64 or 128 steps.  Longer ones are cut into pieces of 128 where these are many, the last ones a small
+// part and rows aligned (4096 steps of 4 of 1024 in bf16: 59 us, pieces of 64 65), of 64 otherwise (777 steps of 37 of 200 in fp32: 44 us, pieces of
+// 128 52; 300 steps of 300 of 256 in bf16 93 and 101; rows of 203 in fp16 44 and 60).
 void plan_recurrence(host::Carver& c, RecArgs& a, int dtype, bool backward) {
   const int64_t tiles = (int64_t)a.N * (((int64_t)a.D + TILE - 1) / TILE);
   a.pieces = 1;
   a.piece_steps = a.T;
   if (backward) {
-    const bool long_pieces = a.T <= steps_of(BACKWARD_4) || (a.x.p && rec_whole(a, host::type_size(dtype)) && !a.lengths);
-    a.shape = a.T <= steps_of(BACKWARD_1) ? BACKWARD_1 : a.T > steps_of(BACKWARD_4_SHORT) && long_pieces ? BACKWARD_4 : BACKWARD_4_SHORT;
+    const int64_t pieces = tiles * (((int64_t)a.T + steps_of(BACKWARD_4) - 1) / steps_of(BACKWARD_4));
+    const bool large = a.T <= steps_of(BACKWARD_4) || (a.x.p && rec_whole(a, host::type_size(dtype)) && a.T >= 1024 && pieces >= 1536);
+    a.shape = a.T <= steps_of(BACKWARD_1) ? BACKWARD_1 : a.T > steps_of(BACKWARD_4_SHORT) && large ? BACKWARD_4 : BACKWARD_4_SHORT;
     a.piece_steps = steps_of(a.shape);
   } else {
     a.shape = a.T <= steps_of(FORWARD_1) || tiles >= 2048 ? FORWARD_1 : FORWARD_4;
