@@ -158,11 +158,14 @@ __global__ __launch_bounds__(ELEMENT_THREADS) void muon_pack_kernel(const MuonTa
   double sum = 0.0;
   for (int i = threadIdx.x; i < norm_blocks(m.m.rows, m.m.cols); i += ELEMENT_THREADS) sum += get(m.norm + i);
   sum = group_sum(sum);
-  const double inv = sum == 0.0 ? 0.0 : (double)HOLD / sqrt(sum);
+  // 2^12 / |u|_F as a power of two and a factor: neither the values nor the factor leave fp32's range (multiplied in 64 bits the small nets' launch took 9.9 us
+  // instead of 5.1)
+  int power;
+  const float factor = (float)frexp(sum == 0.0 ? 0.0 : (double)HOLD / sqrt(sum), &power);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int slow = i * 2 + (lane >> 5), fast = lane & 31;            // of u: rows and columns
-    const float v = (float)(u[i] * inv);
+    const float v = ldexpf(u[i], power) * factor;
     if (m.tall) tile[wave][fast][slow] = v;
     else tile[wave][slow][fast] = v;
   }
