@@ -283,53 +283,73 @@ struct Operands {
 
 typedef float Tile[32][33];
 
-// What becomes of 32 x 32 values of a product (times 2^24, in the wavefront's tile): block (rb, cb).
+// What becomes of 32 x 32 values of a product (times 2^24, in a tile in LDS): block (rb, cb), in four quarters, which one wavefront makes after another or four
+// side by side.  A quarter of a stored result is half of the block's 16-byte units, as it is (0, 1) or transposed (2, 3); of the weights, eight rows.
 template <MuonProduct KIND>
-__device__ __forceinline__ void finish(const MuonTable& t, const Matrix& m, int turn, int rb, int cb, const Tile& tile) {
-  constexpr bool SYMMETRIC = KIND == MUON_GRAM || KIND == MUON_SQUARE;
-  const int lane = threadIdx.x & 63, r = lane & 31, k8 = (lane >> 5) * 8;
-  if constexpr (KIND == MUON_LAST) {
-    const float keep = 1.f - t.lr * t.decay, by = t.lr * m.m.scale * UNHOLD2;
-    const int row = (m.tall ? cb : rb) * 32 + (lane >> 5), col = (m.tall ? rb : cb) * 32 + r;
-    const int64_t at = (int64_t)row * m.m.cols + col;
-    float w[16];
+struct Quarter {
+  static constexpr bool SYMMETRIC = KIND == MUON_GRAM || KIND == MUON_SQUARE;
+  bool here;
+  int64_t at;                                            // its place in the result (in A where that is read as well), or in the weights
+  half8 h, l;                                            // MUON_SQUARE: A there
+  float w[4];                                            // MUON_LAST: the weights
+  // Where it goes, and what has to be read there.
+  __device__ __forceinline__ void ask(const Matrix& m, int quarter, int rb, int cb) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (KIND == MUON_LAST) {
+      const int row = (m.tall ? cb : rb) * 32 + quarter * 8 + (lane >> 5), col = (m.tall ? rb : cb) * 32 + (lane & 31);
+      at = (int64_t)row * m.m.cols + col;
+      here = col < m.m.cols;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) w[i] = m.m.w_in && row + i * 2 < m.m.rows && col < m.m.cols ? get(m.m.w_in + at + (int64_t)i * 2 * m.m.cols) : 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int slow = i * 2 + (lane >> 5);
-      if (row + i * 2 < m.m.rows && col < m.m.cols) set(m.m.w_out + at + (int64_t)i * 2 * m.m.cols, keep * w[i] - by * (m.tall ? tile[r][slow] : tile[slow][r]));
+      for (int i = 0; i < 4; ++i) w[i] = m.m.w_in && here && row + i * 2 < m.m.rows ? get(m.m.w_in + at + (int64_t)i * 2 * m.m.cols) : 0.f;
+    } else {
+      const bool turned = quarter >= 2;
+      here = !(SYMMETRIC && turned && rb == cb);
+      at = ((turned ? (int64_t)cb * m.P * 2 + rb * 2 : (int64_t)rb * (SYMMETRIC ? m.P : m.Q) * 2 + cb * 2) + (quarter & 1)) * BLOCK + lane * 8;
+      if constexpr (KIND == MUON_SQUARE)
+        if (here) {
+          h = get8(m.a + at);
+          l = get8(m.a + at + 512);
+        }
     }
-    return;
   }
+  __device__ __forceinline__ void make(const MuonTable& t, const Matrix& m, int turn, int quarter, int rb, int cb, const Tile& tile) const {
+    const int lane = threadIdx.x & 63, r = lane & 31;
+    if (!here) return;
+    if constexpr (KIND == MUON_LAST) {
+      const float keep = 1.f - t.lr * t.decay, by = t.lr * m.m.scale * UNHOLD2;
+      const int slow = quarter * 8 + (lane >> 5), row = (m.tall ? cb : rb) * 32 + slow;
 #pragma unroll
-  for (int way = 0; way < 2; ++way) {                    // as it is, and transposed
-    if (SYMMETRIC && way == 1 && rb == cb) break;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int k = half * 16 + k8;
-      const int64_t block = way == 0 ? (int64_t)rb * (SYMMETRIC ? m.P : m.Q) * 2 + cb * 2 + half : (int64_t)cb * m.P * 2 + rb * 2 + half;
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (way == 0 ? tile[r][k + e] : tile[k + e][r]) * UNHOLD;
-      if constexpr (KIND == MUON_SQUARE) {
-        const half8 h = get8(m.a + block * BLOCK + lane * 8), l = get8(m.a + block * BLOCK + 512 + lane * 8);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = NS_C * v[e] + NS_B * ((float)h[e] + (float)l[e]) + (rb == cb && r == k + e ? NS_A * HOLD : 0.f);
-      }
+      for (int i = 0; i < 4; ++i)
+        if (row + i * 2 < m.m.rows)
+          set(m.m.w_out + at + (int64_t)i * 2 * m.m.cols, keep * w[i] - by * (m.tall ? tile[r][slow + i * 2] : tile[slow + i * 2][r]));
+    } else {
+      const bool turned = quarter >= 2;
+      const int k = (quarter & 1) * 16 + (lane >> 5) * 8;
       half8 hi, lo;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        _Float16 h, l;
-        split(v[e], h, l);
-        hi[e] = h;
-        lo[e] = l;
+        float v = (turned ? tile[k + e][r] : tile[r][k + e]) * UNHOLD;
+        if constexpr (KIND == MUON_SQUARE) v = NS_C * v + NS_B * ((float)h[e] + (float)l[e]) + (rb == cb && r == k + e ? NS_A * HOLD : 0.f);
+        _Float16 high, low;
+        split(v, high, low);
+        hi[e] = high;
+        lo[e] = low;
       }
-      uint16_t* to = (KIND == MUON_GRAM ? m.a : KIND == MUON_SQUARE ? m.b : way == 0 ? m.x : (turn ? m.xt0 : m.xt1)) + block * BLOCK + lane * 8;
+      uint16_t *const x = m.x, *const xt0 = m.xt0, *const xt1 = m.xt1;       // (values, not places to choose from: those would lie on the stack)
+      uint16_t* const next = turn ? xt0 : xt1;
+      uint16_t* const to = (KIND == MUON_GRAM ? m.a : KIND == MUON_SQUARE ? m.b : turned ? next : x) + at;
       set8(to, hi);
       set8(to + 512, lo);
     }
   }
+};
+template <MuonProduct KIND>
+__device__ __forceinline__ void finish(const MuonTable& t, const Matrix& m, int turn, int rb, int cb, const Tile& tile) {
+  Quarter<KIND> q[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i].ask(m, i, rb, cb);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i].make(t, m, turn, i, rb, cb, tile);
 }
 
 // One product; a workgroup makes B x B blocks, its four wavefronts a quarter of the contraction each, straight from memory's own layout into registers, DEPTH steps
@@ -337,13 +357,13 @@ __device__ __forceinline__ void finish(const MuonTable& t, const Matrix& m, int 
 template <MuonProduct KIND, int B, int DEPTH>
 __global__ __launch_bounds__(256) void muon_product_kernel(const MuonTable* t, int turn) {
   constexpr bool SYMMETRIC = KIND == MUON_GRAM || KIND == MUON_SQUARE;
-  // a block's parts: those of the wavefronts behind the one that adds them up
+  // a block's parts (B = 2: those of the wavefronts behind the one that adds them up)
   __shared__ union {
-    float4 part[B * B][3][4][64];                        // block, wavefront, four of its sixteen registers
-    Tile tile[4];
+    float4 part[B == 1 ? 4 : B * B][B == 1 ? 4 : 3][B == 1 ? 1 : 4][64];      // block, wavefront, four of its sixteen registers; B = 1: registers, wavefront
+    Tile tile[B == 1 ? 1 : 4];
   } lds;
   const Matrix m = matrix_of(*t, SYMMETRIC ? MUON_SYMMETRIC_GRID : MUON_APPLY_GRID);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, columns = SYMMETRIC ? m.P : m.Q;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), columns = SYMMETRIC ? m.P : m.Q;
   int ti, tj;
   if (SYMMETRIC) {
     triangle_in_strips(m.block, (m.P + B - 1) / B, ti, tj);
@@ -360,6 +380,8 @@ __global__ __launch_bounds__(256) void muon_product_kernel(const MuonTable* t, i
     left[i] = l0 + (int64_t)rb * kb * BLOCK;
     right[i] = r0 + (int64_t)cb * kb * BLOCK;
   }
+  Quarter<KIND> quarter;
+  if constexpr (B == 1) quarter.ask(m, wave, ti, tj);
   float16v acc[B][B];
 #pragma unroll
   for (int i = 0; i < B; ++i)
@@ -377,6 +399,28 @@ __global__ __launch_bounds__(256) void muon_product_kernel(const MuonTable* t, i
         if (k + d + DEPTH < k1) o[d].load(left, right, k + d + DEPTH);
       }
   }
+  if constexpr (B == 1) {
+    // every wavefront adds up a quarter of the registers, and makes a quarter of the result
+#pragma unroll
+    for (int q = 0; q < 4; ++q) lds.part[q][wave][0][lane] = float4{acc[0][0][q * 4], acc[0][0][q * 4 + 1], acc[0][0][q * 4 + 2], acc[0][0][q * 4 + 3]};
+    __syncthreads();
+    float4 sum = lds.part[wave][0][0][lane];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+      const float4 p = lds.part[wave][w][0][lane];
+      sum = float4{sum.x + p.x, sum.y + p.y, sum.z + p.z, sum.w + p.w};
+    }
+    __syncthreads();
+    Tile& tile = lds.tile[0];
+    const int row = wave * 8 + (lane >> 5) * 4, col = lane & 31;
+    tile[row][col] = sum.x;
+    tile[row + 1][col] = sum.y;
+    tile[row + 2][col] = sum.z;
+    tile[row + 3][col] = sum.w;
+    __syncthreads();
+    quarter.make(*t, m, turn, wave, ti, tj, tile);
+    return;
+  } else {
   // a block's parts are added up by the wavefront of its number: its own, then those of the ones behind it, around
 #pragma unroll
   for (int i = 0; i < B; ++i)
@@ -421,6 +465,7 @@ __global__ __launch_bounds__(256) void muon_product_kernel(const MuonTable* t, i
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   finish<KIND>(*t, m, turn, rb, cb, tile);
+  }
 }
 
 // The same product with tiles of 8 x 4 blocks, for matrices whose tiles fill the GPU: the kernel above reads 8 KB for every 12 matrix instructions, and is bound
