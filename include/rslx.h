@@ -566,7 +566,8 @@ int32_t rslx_layer_norm_backward(int32_t dtype, const void* dy, int64_t lddy, co
 typedef struct rslx_gated_rec {
   int32_t dtype;                 /* RSLX_F32, RSLX_BF16, RSLX_F16: x, g, h and their gradients; states are fp32 */
   int32_t T, N, D;               /* T: 0..RSLX_ATTN_MAX_STEPS; N: 0 or more; D: 1 or more; N ceil(D / 64), in whole calls times the pieces
-                                    of 64 steps or more that long sequences are cut into: to RSLX_REC_MAX_TILES */
+                                    of 64 steps or more that long sequences are cut into: to RSLX_REC_MAX_TILES (cut ones
+                                    have less than 2^28 channels N * D, D rounded up to four) */
   const uint8_t* dones;          /* device [T, N] or NULL */
   const int32_t* lengths;        /* device [N] or NULL */
 } rslx_gated_rec;

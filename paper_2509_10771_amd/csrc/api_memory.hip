@@ -57,7 +57,7 @@ RecArgs rec_args(const rslx_gated_rec& a) {
 
 // A launch has fewer than 2^32 lanes.
 int32_t check_grid(const RecArgs& r, const char* who) {
-  if ((int64_t)r.N * ((r.D + 63) / 64) * r.pieces >= (int64_t)1 << 24)
+  if ((int64_t)r.N * ((r.D + 63) / 64) * r.pieces >= (int64_t)1 << 24 || (r.pieces > 1 && (int64_t)r.N * ((r.D + 3) / 4) >= (int64_t)1 << 26))
     return fail(RSLX_ERR_SHAPE, "%s: %d pieces of %d sequences of %d channels are too many", who, r.pieces, r.N, r.D);
   return RSLX_OK;
 }

@@ -39,6 +39,8 @@ def test_recurrence_shapes_and_types():
         rx.rslx_gated_recurrence_workspace_bytes(_rec(N=1 << 16, D=1 << 15))
     with pytest.raises(rx.RslxError, match="too many"):
         rx.rslx_gated_recurrence_backward_workspace_bytes(_rec(T=1 << 20, N=1 << 16, D=1))
+    with pytest.raises(rx.RslxError, match="too many"):
+        rx.rslx_gated_recurrence_backward_workspace_bytes(_rec(T=129, N=1 << 16, D=1 << 12))
     with pytest.raises(rx.RslxError, match="more than 32 bits"):
         _rec(T=1 << 32)
     with pytest.raises(rx.RslxError, match="x is"):
