@@ -8,7 +8,13 @@
 // read 64 channels, 128 to 256 bytes of a row; the wavefront's four sets of lanes and the workgroup's wavefronts compose theirs through shuffles and
 // LDS; then every lane walks its steps again from the state that enters them.  Every value is read once and every result written once, as long as a
 // workgroup's steps hold the sequence, or channels are many enough for workgroups to go along whole sequences (forward).  Otherwise sequences
-// are cut into pieces: one launch leaves every piece's map, a second (a lane per channel) the states between the pieces, a third makes the results.
+// are cut into pieces: one launch leaves every piece's map, a second the states between the pieces, a third makes the results.
+//
+// Bound by memory where values are read once: a roll-out of 24 steps of 4096 environments of 256 in fp32 61 us = 5.1 TB/s, the gradients of a quarter of
+// it 27 us = 4.9 TB/s.  In pieces inputs are read twice, the second time from the last-level cache where they fit: 8192 steps of 4 environments of 1024 in
+// bf16 71 us (maps 31 us, 4.4 TB/s; join 5; results 34), gradients of 4096 steps 57 us.  Gates cost 16-bit walks as much as memory does, so that what stands
+// beside them counts: addresses are common to a wavefront where offsets fit 32 bits, steps are not asked one by one where all exist and none ends an episode
+// (40 -> 17 vector instructions a value; 90 -> 76 us and 92 -> 63 for these two).
 #include "memory.h"
 #include "overlap.h"
 #include "typed.h"
