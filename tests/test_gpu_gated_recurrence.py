@@ -331,3 +331,37 @@ def test_the_same_inputs_give_the_same_bits(rx):
         first = run(rx)
         for _ in range(3):
             assert all(torch.equal(a, b) for a, b in zip(first, run(rx)))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [7, 90, 300])
+def test_rows_shared_by_sequences_or_steps(rx, T, dtype):
+    """Inputs whose rows are the same memory for every sequence, or for every step: the gradients come for each."""
+    c = Case(T, T, 5, 36, dtype, done_p=0.05)
+    c.x, c.g, c.dh = c.x[:, :1].expand(T, 5, 36), c.g[:1].expand(T, 5, 36), c.dh[:1, :1].expand(T, 5, 36)
+
+    def place(*xs):
+        if all(0 in x.stride() for x in xs):
+            return [x[tuple(slice(None) if s else slice(1) for s in x.stride())].contiguous().cuda().expand(x.shape) for x in xs]
+        return [x.contiguous().cuda() for x in xs]
+    c.place = place
+    assert 0 in c.place(c.x)[0].stride()
+    c.check_forward(*c.forward(rx))
+    c.check_backward(*c.backward(rx))
+
+
+def test_two_streams_at_once(rx):
+    """Calls on two streams, each with its own workspace and outputs, give what they give alone."""
+    cases = [Case(20, 1500, 3, 64, "bf16", done_p=0.01), Case(21, 900, 5, 100, "fp32", done_p=0.01)]
+    alone = [(c.forward(rx), c.backward(rx)) for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(3):
+        got = []
+        for c, s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                got.append((c.forward(rx), c.backward(rx)))
+        torch.cuda.synchronize()
+        for a, b in zip(alone, got):
+            for x, y in zip(a, b):
+                assert all(torch.equal(p, q) for p, q in zip(x, y))
