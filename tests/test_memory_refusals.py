@@ -88,6 +88,16 @@ def test_recurrence_pointers():
         rx.rslx_gated_recurrence_step(_rec(T=1, dones=Z(1, 2, dtype=torch.uint8)), Z(1, 2, 8), Z(1, 2, 8), None, None, Z(2, 8), Z(1, 2, 8))
     with pytest.raises(rx.RslxError, match="reset"):
         rx.rslx_gated_recurrence_step(_rec(T=1), Z(1, 2, 8), Z(1, 2, 8), Z(2), None, Z(2, 8), Z(1, 2, 8))
+    wrong = ((Z(2, 8), "needed"), (Z(1, 2, 4), "needed"), (Z(1, 2, 8, dtype=torch.float16), "needed"), (Z(1, 2, 16)[..., ::2], "side by side"))
+    for name in ("x", "g", "h"):                              # the views of a step, each wrong in turn
+        for t, word in wrong:
+            rows = dict({n: Z(1, 2, 8) for n in ("x", "g", "h")}, **{name: t})
+            with pytest.raises(rx.RslxError, match="^%s.* %s" % (name, word)):
+                rx.rslx_gated_recurrence_step(_rec(T=1), rows["x"], rows["g"], None, None, Z(2, 8), rows["h"])
+    for n, s in ((17, Z(17)), (16, Z(16, dtype=torch.float16))):
+        for states in ((s, Z(2, 8)), (None, s)):
+            with pytest.raises(rx.RslxError, match="s_(in|out) has %d values" % n):
+                rx.rslx_gated_recurrence_step(_rec(T=1), Z(1, 2, 8), Z(1, 2, 8), None, *states, Z(1, 2, 8))
 
 
 def test_recurrence_outputs_that_overlap():
