@@ -164,6 +164,7 @@ struct Place {
   int64_t n;
   int d, len, piece;
   bool full;                                // every lane has four channels: the same for the whole workgroup
+  int from, shift;                          // the last four channels that a lane may read from, and how far behind them its own are (D >= W)
 };
 // `last_first`: in the other order on each die, for a launch that reads what the one before it read: what that read last lies in the caches still (gradients of
 // 2048 steps of 32 sequences, 1024 channels in bf16: 227 us, in the same order 250; 777 steps of 37 of 200 in fp32 46 and 48).  Forward pieces run all at once, and
@@ -182,6 +183,8 @@ __device__ __forceinline__ Place place_of(const RecArgs& a, bool last_first = fa
   p.n = at / tiles;
   p.d = (int)(at % tiles) * TILE + (threadIdx.x & (ROW - 1)) * W;
   p.full = (int)(at % tiles) * TILE + TILE <= a.D;
+  p.from = p.d <= a.D - W ? p.d : a.D - W;
+  p.shift = (p.d - p.from) & (W - 1);
   p.len = a.T;
   if (a.lengths) {
     const int len = a.lengths[p.n];
@@ -213,6 +216,7 @@ __device__ __forceinline__ float4* piece_at(float* base, const RecArgs& a, const
 template <typename T, bool WHOLE, int STREAM>
 struct Rows {
   typedef uint32_t Bits __attribute__((ext_vector_type(sizeof(T) * W / 4)));
+  static constexpr bool EDGE = !WHOLE && sizeof(T) == 2;
   char* base;
   uint32_t offset;
   T* mine;
@@ -232,15 +236,27 @@ struct Rows {
     } else if constexpr (WHOLE) v = *reinterpret_cast<const Pack<T, W>*>(base + i * step * (int64_t)sizeof(T) + offset);
     else load_piece<T, W, false>(v, mine + i * step, p.d, a.D);
   }
-  // all of the lane's steps
+  // EDGE: 16-bit values of rows that start anywhere.  Those of a row's last channels, which four need not be, come in one load as well, and rows are loaded without
+  // asking which steps exist: what is loaded in parts, or under a condition, is put together in a register, and waited for there and then (500 steps of 300 sequences,
+  // 203 channels in bf16: 78 us, in parts 130; their gradients 158 and 244).  Values of 32 bits have registers of their own: in fp32 106 in parts, 135 in this way.
+  __device__ __forceinline__ void load_edge(Pack<T, W>& v, int i, const Place& p) const {
+    uint64_t bits;
+    __builtin_memcpy(&bits, mine + i * step + p.from, sizeof bits);
+    bits >>= p.shift * 16;
+    __builtin_memcpy(&v, &bits, sizeof bits);
+  }
+  // all of the lane's steps; EDGE: the step `last` in place of those behind it
   template <int L>
-  __device__ __forceinline__ void load(Pack<T, W> (&v)[L], const RecArgs& a, const Place& p) const {
-    if (WHOLE || !p.full) {
+  __device__ __forceinline__ void load(Pack<T, W> (&v)[L], const RecArgs& a, const Place& p, int64_t last = L) const {
+    if (!WHOLE && p.full) {
 #pragma unroll
-      for (int i = 0; i < L; ++i) load(v[i], i, a, p);
+      for (int i = 0; i < L; ++i) __builtin_memcpy(&v[i], mine + (!EDGE || i < last ? i : last) * step + p.d, sizeof v[i]);
+    } else if (!EDGE || a.D < W) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) load(v[i], !EDGE || i < last ? i : (int)last, a, p);
     } else {
 #pragma unroll
-      for (int i = 0; i < L; ++i) __builtin_memcpy(&v[i], mine + i * step + p.d, sizeof v[i]);
+      for (int i = 0; i < L; ++i) load_edge(v[i], i < last ? i : (int)last, p);
     }
   }
   template <int L>
@@ -293,6 +309,7 @@ __device__ __forceinline__ uint32_t ends_of(const RecArgs& a, const Place& p, in
 // none ends an episode (`plain`), nothing is asked step by step.
 template <typename T, int L, int WAVES, bool WHOLE, int STREAM, bool MAPS>
 __global__ __launch_bounds__(WAVES * 64) void recurrence_kernel(RecArgs a) {
+  constexpr bool EDGE = Rows<T, WHOLE, STREAM>::EDGE;
   __shared__ WaveMaps<WAVES> maps[2];
   const Place p = place_of(a);
   const int ahead = threadIdx.x / ROW * L;
@@ -336,12 +353,17 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_kernel(RecArgs a) {
           m.a.v[k] = i == 0 ? f[0][k] : m.a.v[k] * f[i][k];
         }
     } else {
+      if (EDGE) {
+        rg.load(pg, a, p, p.len - 1 - t0);
+        rx.load(px, a, p, p.len - 1 - t0);
+      } else {
 #pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (t0 + i < p.len) {
-          rg.load(pg[i], i, a, p);
-          rx.load(px[i], i, a, p);
-        }
+        for (int i = 0; i < L; ++i)
+          if (t0 + i < p.len) {
+            rg.load(pg[i], i, a, p);
+            rx.load(px[i], i, a, p);
+          }
+      }
       gates();
 #pragma unroll
       for (int i = 0; i < L; ++i)
@@ -401,6 +423,7 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_kernel(RecArgs a) {
 // Backward: a piece is the steps that a workgroup holds at once.  MAPS: the piece's maps of both directions (whose gates' product is the same).
 template <typename T, int L, int WAVES, bool WHOLE, int STREAM, bool MAPS>
 __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(RecArgs a) {
+  constexpr bool EDGE = Rows<T, WHOLE, STREAM>::EDGE;
   __shared__ WaveMaps<WAVES> maps[2];
   const Place p = place_of(a, !MAPS && a.pieces > 1);
   const int ahead = threadIdx.x / ROW * L;
@@ -437,12 +460,19 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(RecArgs
 #pragma unroll
       for (int k = 0; k < W; ++k) up.b.v[k] = f[i][k] * (i == L - 1 ? to_float(pd[i].v[k]) : up.b.v[k] + to_float(pd[i].v[k]));
   } else {
+    if (EDGE) {
+      rg.load(pg, a, p, p.len - 1 - t0);
+      rx.load(px, a, p, p.len - 1 - t0);
+      rd.load(pd, a, p, p.len - 1 - t0);
+    }
 #pragma unroll
     for (int i = 0; i < L; ++i)
       if (t0 + i < p.len) {
-        rg.load(pg[i], i, a, p);
-        rx.load(px[i], i, a, p);
-        rd.load(pd[i], i, a, p);
+        if (!EDGE) {
+          rg.load(pg[i], i, a, p);
+          rx.load(px[i], i, a, p);
+          rd.load(pd[i], i, a, p);
+        }
       } else {
         // steps that do not exist hand both states on
 #pragma unroll

@@ -131,6 +131,16 @@ def test_forward_and_backward(rx, T, N, D, dtype):
     c.check_backward(*c.backward(rx))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("D", [2, 3, 5, 6, 7, 66, 69, 129, 131])
+def test_last_channels(rx, dtype, D):
+    """Rows whose last piece is one, two or three values, with NaN on both sides of the row; episodes that end, sequences that are shorter."""
+    for ragged in (False, True):
+        c = Case(D, 75, 6, D, dtype, done_p=0.05, ragged=ragged, layout="odd")
+        c.check_forward(*c.forward(rx))
+        c.check_backward(*c.backward(rx))
+
+
 @pytest.mark.parametrize("layout", ["side", "dense", "batch_first", "odd"])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("T", [6, 100, 700])
