@@ -172,7 +172,7 @@ struct Place {
 __device__ __forceinline__ Place place_of(const RecArgs& a, bool last_first = false) {
   const int tiles = (a.D + TILE - 1) / TILE;
   // workgroups go to the eight dies in turn.  Where neighbours share lines of memory, each die gets a row of them, so that its L2 joins what they read and
-  // write (500 steps of 300 sequences, 203 channels in bf16: 117 us, in turn 138); where they do not, in turn is better (8192 steps of 4, 1024 channels: 73 and 81)
+  // write (500 steps of 300 sequences, 203 channels in bf16: 77 us, in turn 86); where they do not, in turn is better (8192 steps of 4, 1024 channels: 73 and 81)
   const uint32_t each = gridDim.x / 8, more = gridDim.x % 8, die = blockIdx.x % 8;
   uint32_t turn = blockIdx.x / 8;
   if (last_first) turn = each + (die < more ? 1 : 0) - 1 - turn;
@@ -632,8 +632,8 @@ __global__ __launch_bounds__(REC_THREADS) void recurrence_step_kernel(RecArgs a)
 }
 
 // How the steps are shared out: wavefronts of a workgroup, steps of a lane; see plan_recurrence.
-enum RecShape { FORWARD_1 = 0, FORWARD_4, BACKWARD_1, BACKWARD_4, BACKWARD_4_SHORT };
-constexpr int LANE_STEPS[] = {4, 4, 8, 8, 4}, SHAPE_WAVES[] = {1, 4, 1, 4, 4};
+enum RecShape { FORWARD_1 = 0, FORWARD_4, BACKWARD_1, BACKWARD_4, BACKWARD_4_SHORT, BACKWARD_2_SHORT };
+constexpr int LANE_STEPS[] = {4, 4, 8, 8, 4, 4}, SHAPE_WAVES[] = {1, 4, 1, 4, 4, 2};
 int steps_of(int shape) { return LANE_STEPS[shape] * SHAPE_WAVES[shape] * SETS; }
 
 template <typename T, bool WHOLE, int STREAM, bool MAPS>
@@ -645,6 +645,7 @@ void run_shape(const RecArgs& a, hipStream_t s) {
     RUN(FORWARD_4, recurrence_kernel);
     RUN(BACKWARD_4, recurrence_backward_kernel);
     RUN(BACKWARD_4_SHORT, recurrence_backward_kernel);
+    RUN(BACKWARD_2_SHORT, recurrence_backward_kernel);
     default:
       if constexpr (!MAPS) switch (a.shape) {
         RUN(FORWARD_1, recurrence_kernel);
@@ -701,17 +702,22 @@ void run(const RecArgs& a, int dtype, bool maps, hipStream_t s) {
 // Forward, a wavefront along each sequence and 64 channels where these fill the GPU with eight wavefronts for each compute unit, or where 16 steps are all;
 // otherwise four, 64 steps at a time, in about 1024 pieces where these are few (100 steps of 300 sequences of 256 channels in bf16: 14.1 us, with one
 // 16.7; 777 steps of 37 of 200 in fp32: 32, in 512 pieces 37, in 2048 31; 8192 steps of 4 of 1024 in bf16: 72, in 512 pieces 81).
-// Backward, the smallest workgroup that holds the sequence: 32, 64 or 128 steps.  Longer ones are cut into pieces of 128 where these are many, the last ones a small
-// part and rows aligned (4096 steps of 4 of 1024 in bf16: 59 us, pieces of 64 65), of 64 otherwise (777 steps of 37 of 200 in fp32: 44 us, pieces of
-// 128 52; 300 steps of 300 of 256 in bf16 93 and 101; rows of 203 in fp16 44 and 60).
+// Backward, the smallest workgroup that holds the sequence: 32, 64 or 128 steps.  Longer ones are cut into pieces: of 32 up to 2048 steps (777 steps of 37 of 203 in
+// fp16, ragged: 37.5 us, pieces of 64 41.5; 200 steps of 500 of 203 in bf16 129 and 149; 1024 steps of 300 of 256 in bf16 277, pieces of 128 284), where the
+// join has few; beyond, of 128 where these are many and rows aligned (4096 steps of 4 of 1024 in bf16: 58 us, pieces of 64 61), of 64 otherwise (8192
+// steps of 4 of 256 in fp32: 53 us, pieces of 128 55, of 32 58).
 void plan_recurrence(host::Carver& c, RecArgs& a, int dtype, bool backward) {
   const int64_t tiles = (int64_t)a.N * (((int64_t)a.D + TILE - 1) / TILE);
   a.pieces = 1;
   a.piece_steps = a.T;
   if (backward) {
-    const int64_t pieces = tiles * (((int64_t)a.T + steps_of(BACKWARD_4) - 1) / steps_of(BACKWARD_4));
-    const bool large = a.T <= steps_of(BACKWARD_4) || (a.x.p && rec_whole(a, host::type_size(dtype)) && a.T >= 1024 && pieces >= 1536);
-    a.shape = a.T <= steps_of(BACKWARD_1) ? BACKWARD_1 : a.T > steps_of(BACKWARD_4_SHORT) && large ? BACKWARD_4 : BACKWARD_4_SHORT;
+    const auto pieces = [&](int shape) { return tiles * (((int64_t)a.T + steps_of(shape) - 1) / steps_of(shape)); };
+    if (a.T <= steps_of(BACKWARD_1)) a.shape = BACKWARD_1;
+    else if (a.T <= steps_of(BACKWARD_4_SHORT)) a.shape = BACKWARD_4_SHORT;
+    else if (a.T <= steps_of(BACKWARD_4)) a.shape = BACKWARD_4;
+    else if (a.T <= 2048 && pieces(BACKWARD_2_SHORT) < (int64_t)1 << 24) a.shape = BACKWARD_2_SHORT;      // (as many as a launch has)
+    else if (a.T > 2048 && a.x.p && rec_whole(a, host::type_size(dtype)) && pieces(BACKWARD_4) >= 1536) a.shape = BACKWARD_4;
+    else a.shape = BACKWARD_4_SHORT;
     a.piece_steps = steps_of(a.shape);
   } else {
     a.shape = a.T <= steps_of(FORWARD_1) || tiles >= 2048 ? FORWARD_1 : FORWARD_4;
