@@ -5,7 +5,7 @@
 //
 // Bound by memory, and built like layer norm: a row is read once into the registers of the TPR lanes that share it, the next one is on its way while
 // this one is reduced, results are written once.  Squares and products are summed in fp32: a lane's values in order, then a fixed tree.  98304 rows of 512 in bf16
-// into bytes 66 us = 5.3 TB/s; gradients of 24576 rows of 235 in fp32, which start anywhere, 21 us = 4.4 TB/s and 4 for the fold of the weight's.
+// into bytes 66 us = 5.3 TB/s; gradients of 24576 rows of 235 in fp32, which start anywhere, 18 us = 5.1 TB/s and 4 for the fold of the weight's.
 #include "memory.h"
 #include "norm_rows.h"
 
@@ -41,9 +41,45 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, p, true);
 }
 
+// A lane's piece i of a row, W values from `at` on, of which those from `first` to `end` are its own.  Rows that start anywhere end with a piece that begins
+// earlier, so that it is one load too: 16-bit values that come one by one (IN_PARTS) are each put together in a register, and waited for, with the next row on
+// its way (98304 rows of 511 in bf16, to bytes: 80 us, in parts 95; their gradients 92 and 127; of 24576 of 999 in fp32 73 and 135).  The first half of a lane's
+// pieces is inside the row (see norm_shape).
+template <int W, int ITEMS, int TPR, bool WHOLE, bool IN_PARTS = false>
+struct Span {
+  int at, first, end;
+  __device__ __forceinline__ Span(int i, int cols) : at((i * TPR + (int)threadIdx.x % TPR) * W), first(0), end(W) {
+    if (i < ITEMS / 2) return;
+    end = cols - at < W ? cols - at : W;
+    if (!WHOLE && !IN_PARTS && cols >= W && end < W) {
+      const int c = at;
+      at = cols - W;
+      first = c - at;
+      end = W;
+    }
+  }
+  __device__ __forceinline__ bool has(int k) const { return WHOLE ? end > 0 : k >= first && k < end; }
+  template <typename T>
+  __device__ __forceinline__ void load(Pack<T, W>& p, const T* row, int cols) const {
+    if (WHOLE || IN_PARTS || cols < W) load_piece<T, W, WHOLE>(p, row, at, cols);
+    else __builtin_memcpy(&p, row + at, sizeof p);
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(const Pack<T, W>& p, T* row, int cols, bool past) const {
+    if (WHOLE || IN_PARTS || first == 0) {
+      store_piece<T, W, WHOLE>(p, row, at, cols, past);
+    } else {
+#pragma unroll
+      for (int k = 1; k < W; ++k)
+        if (k >= first) row[at + k] = p.v[k];
+    }
+  }
+};
+
 template <typename T, int W, int ITEMS, int TPR, bool WHOLE, bool E4M3>
 __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_kernel(RmsArgs a) {
   constexpr int ROWS = THREADS_OF<TPR> / TPR;
+  typedef Span<W, ITEMS, TPR, WHOLE> Piece;
   __shared__ float lds[2][TPR > 64 ? TPR / 64 : 1];
   __shared__ uint32_t lds_max[TPR > 64 ? TPR / 64 : 1];
   const int lane = threadIdx.x % TPR;
@@ -55,8 +91,8 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_kernel(RmsArgs a) {
     if (r < a.rows)
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
-        load_piece<T, W, WHOLE>(px[i], static_cast<const T*>(a.x) + r * a.ldx, (i * TPR + lane) * W, a.cols);
-        if (a.residual) load_piece<T, W, WHOLE>(pr[i], static_cast<const T*>(a.residual) + r * a.ldr, (i * TPR + lane) * W, a.cols);
+        Piece(i, a.cols).load(px[i], static_cast<const T*>(a.x) + r * a.ldx, a.cols);
+        if (a.residual) Piece(i, a.cols).load(pr[i], static_cast<const T*>(a.residual) + r * a.ldr, a.cols);
       }
   };
   load(row);
@@ -65,7 +101,7 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_kernel(RmsArgs a) {
   for (int i = 0; i < ITEMS; ++i) {
 #pragma unroll
     for (int k = 0; k < W; ++k) w[i].v[k] = 1.f;
-    if (a.weight) load_piece<float, W, WHOLE>(w[i], a.weight, (i * TPR + lane) * W, a.cols);
+    if (a.weight) Piece(i, a.cols).load(w[i], a.weight, a.cols);
   }
   // (TPR <= 64: lanes leave the loop in whole rows, and the shuffles stay inside a row; above, the workgroup has one row)
   for (int turn = 0; row < a.rows; row += stride, turn ^= 1) {
@@ -76,7 +112,7 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_kernel(RmsArgs a) {
       for (int k = 0; k < W; ++k) {
         float z = to_float(px[i].v[k]);
         if (a.residual) z += to_float(pr[i].v[k]);
-        f[i * W + k] = in_row<W, WHOLE>((i * TPR + lane) * W, k, a.cols) ? z : 0.f;
+        f[i * W + k] = Piece(i, a.cols).has(k) ? z : 0.f;
         s[0] += f[i * W + k] * f[i * W + k];
       }
     load(row + stride);
@@ -87,7 +123,7 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_kernel(RmsArgs a) {
         Pack<T, W> out;
 #pragma unroll
         for (int k = 0; k < W; ++k) out.v[k] = from_float<T>(f[i * W + k]);
-        store_piece<T, W, WHOLE>(out, to, (i * TPR + lane) * W, a.cols, a.past);
+        Piece(i, a.cols).store(out, to, a.cols, a.past);
       }
     }
     row_sum<TPR, 1>(s, lds[turn]);
@@ -99,7 +135,7 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_kernel(RmsArgs a) {
         Pack<T, W> out;
 #pragma unroll
         for (int k = 0; k < W; ++k) out.v[k] = from_float<T>(f[i * W + k] * rstd * w[i].v[k]);
-        store_piece<T, W, WHOLE>(out, y, (i * TPR + lane) * W, a.cols, a.past);
+        Piece(i, a.cols).store(out, y, a.cols, a.past);
       }
     } else {
       uint32_t most = 0;
@@ -107,7 +143,7 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_kernel(RmsArgs a) {
       for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
         for (int k = 0; k < W; ++k) {
-          f[i * W + k] = in_row<W, WHOLE>((i * TPR + lane) * W, k, a.cols) ? f[i * W + k] * rstd * w[i].v[k] : 0.f;
+          f[i * W + k] = Piece(i, a.cols).has(k) ? f[i * W + k] * rstd * w[i].v[k] : 0.f;
           const uint32_t bits = __float_as_uint(f[i * W + k]) & 0x7fffffffu;
           most = bits > most ? bits : most;
         }
@@ -125,7 +161,7 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_kernel(RmsArgs a) {
           const uint32_t four = pack_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
           __builtin_memcpy(out.v + k, &four, 4);
         }
-        store_piece<uint8_t, W, WHOLE>(out, y, (i * TPR + lane) * W, a.cols, a.past);
+        Piece(i, a.cols).store(out, y, a.cols, a.past);
       }
       if (lane == 0) a.scales[row] = scale;
     }
@@ -140,6 +176,8 @@ template <typename T, int W, int ITEMS, int TPR, bool WHOLE>
 __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_backward_kernel(RmsArgs a) {
   constexpr int ROWS = THREADS_OF<TPR> / TPR;
   constexpr bool LONG = TPR == 1024 && ITEMS * W > 8;
+  // (LONG: no registers for more; fp32 rows of several pieces a lane: 98304 rows of 511 157 us, as one load 167)
+  typedef Span<W, ITEMS, TPR, WHOLE, LONG || (sizeof(T) == 4 && ITEMS > 1)> Piece;
   __shared__ float lds[2][TPR > 64 ? TPR / 64 : 1];
   __shared__ float join[ROWS > 1 ? (ROWS - 1) * TPR * ITEMS * W : 1];
   __shared__ __attribute__((aligned(16))) float sums[LONG ? ITEMS * W * TPR : 4];
@@ -154,9 +192,9 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_backward_kernel(RmsA
     if (r < a.rows) {
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
-        load_piece<T, W, WHOLE>(px[i], static_cast<const T*>(a.x) + r * a.ldx, (i * TPR + lane) * W, a.cols);
-        load_piece<T, W, WHOLE>(pd[i], static_cast<const T*>(a.dy) + r * a.lddy, (i * TPR + lane) * W, a.cols);
-        if (!LONG && a.y && a.residual) load_piece<T, W, WHOLE>(pt[i], static_cast<const T*>(a.residual) + r * a.ldr, (i * TPR + lane) * W, a.cols);
+        Piece(i, a.cols).load(px[i], static_cast<const T*>(a.x) + r * a.ldx, a.cols);
+        Piece(i, a.cols).load(pd[i], static_cast<const T*>(a.dy) + r * a.lddy, a.cols);
+        if (!LONG && a.y && a.residual) Piece(i, a.cols).load(pt[i], static_cast<const T*>(a.residual) + r * a.ldr, a.cols);
       }
       rstd = a.rstd[r];
     }
@@ -172,7 +210,7 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_backward_kernel(RmsA
       if constexpr (!LONG) dw[i * W + k] = 0.f;
       else if (k % 4 == 0) sum_at(i * W + k) = float4{0.f, 0.f, 0.f, 0.f};
     }
-    if (a.weight) load_piece<float, W, WHOLE>(w[i], a.weight, (i * TPR + lane) * W, a.cols);
+    if (a.weight) Piece(i, a.cols).load(w[i], a.weight, a.cols);
   }
   for (int turn = 0; row < a.rows; row += stride, turn ^= 1) {
     if (LONG) load(row);
@@ -185,7 +223,7 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_backward_kernel(RmsA
 #pragma unroll
       for (int k = 0; k < W; ++k) {
         const int x = i * W + k;
-        const bool here = in_row<W, WHOLE>((i * TPR + lane) * W, k, a.cols);
+        const bool here = Piece(i, a.cols).has(k);
         const float d = here ? to_float(pd[i].v[k]) : 0.f, hx = here ? to_float(px[i].v[k]) * scale : 0.f, gx = here ? d * w[i].v[k] : 0.f;
         s[0] += gx * hx;
         if constexpr (!LONG) {
@@ -209,7 +247,7 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_backward_kernel(RmsA
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
         Pack<T, W> out, late;
-        if (LONG && a.residual) load_piece<T, W, WHOLE>(late, static_cast<const T*>(a.residual) + row * a.ldr, (i * TPR + lane) * W, a.cols);
+        if (LONG && a.residual) Piece(i, a.cols).load(late, static_cast<const T*>(a.residual) + row * a.ldr, a.cols);
 #pragma unroll
         for (int k = 0; k < W; ++k) {
           float v;
@@ -218,7 +256,7 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_backward_kernel(RmsA
           if (a.residual) v += to_float(LONG ? late.v[k] : t[LONG ? 0 : i].v[k]);
           out.v[k] = from_float<T>(v);
         }
-        store_piece<T, W, WHOLE>(out, dx, (i * TPR + lane) * W, a.cols, LONG || a.past);      // (LONG: no registers for both)
+        Piece(i, a.cols).store(out, dx, a.cols, LONG || a.past);      // (LONG: no registers for both)
       }
     }
   }
@@ -252,7 +290,7 @@ __global__ __launch_bounds__(THREADS_OF<TPR>) void rms_norm_backward_kernel(RmsA
           out.v[k] = dw[i * W + k];
         }
       }
-      store_piece<float, W, WHOLE>(out, to, (i * TPR + lane) * W, a.cols);
+      Piece(i, a.cols).store(out, to, a.cols, false);
     }
   }
 }

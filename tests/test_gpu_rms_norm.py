@@ -183,6 +183,29 @@ def test_parts_may_be_left_out_and_in_place(rx, rows, cols):
     _backward_check(dy, total, None, rstd, None, only, dw2)
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,cols", [(37, 3), (300, 9), (5000, 61), (900, 235), (400, 511), (90, 1003), (33, 4093), (5, 16383)])
+def test_rows_that_start_anywhere_in_place(rx, rows, cols, dtype):
+    """The last piece of such a row begins inside the one before it: what a neighbour stores there meanwhile is of no account."""
+    x, res, dy, dt, w = _case(cols, rows, cols, dtype)
+    gx, gr, gd, gt, gw = (t.cuda() for t in (x, res, dy, dt, w))
+    y, total, rstd = torch.empty_like(gx), torch.empty_like(gx), torch.empty(rows, device="cuda")
+    rx.rslx_rms_norm(gx, gr, gw, EPS, total, y, rstd)
+    _forward_check(x, res, w, (y, total, rstd))
+    for a, b in ((0, 1), (1, 0)):
+        both = [gx.clone(), gr.clone()]
+        rx.rslx_rms_norm(both[0], both[1], gw, EPS, both[b], both[a], None)
+        assert torch.equal(both[a], y) and torch.equal(both[b], total)
+    ws = rx.workspace(rx.rslx_rms_norm_backward_workspace_bytes(rows, cols))
+    dx, dw, dw2 = torch.empty_like(gx), torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    rx.rslx_rms_norm_backward(gd, total, gw, rstd, gt, dx, dw, ws)
+    _backward_check(dy, total, w, rstd, dt, dx, dw)
+    for k in range(3):
+        ins = [gd.clone(), total.clone(), gt.clone()]
+        rx.rslx_rms_norm_backward(ins[0], ins[1], gw, rstd, ins[2], ins[k], dw2, ws)
+        assert torch.equal(ins[k], dx) and torch.equal(dw, dw2)
+
+
 def test_no_rows(rx):
     e = torch.empty(0, 40, device="cuda")
     rx.rslx_rms_norm(e, e, None, EPS, None, e, None)
