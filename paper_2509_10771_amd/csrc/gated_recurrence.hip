@@ -12,7 +12,7 @@
 //
 // Bound by memory where values are read once: a roll-out of 24 steps of 4096 environments of 256 in fp32 61 us = 5.1 TB/s, the gradients of a quarter of
 // it 27 us = 4.9 TB/s.  In pieces inputs are read twice, the second time from the last-level cache where they fit: 8192 steps of 4 environments of 1024 in
-// bf16 71 us (maps 31 us, 4.4 TB/s; join 5; results 34), gradients of 4096 steps 57 us.  Gates cost 16-bit walks as much as memory does, so that what stands
+// bf16 72 us (maps 31 us, 4.4 TB/s; join 5; results 35), gradients of 4096 steps 56 us.  Gates cost 16-bit walks as much as memory does, so that what stands
 // beside them counts: addresses are common to a wavefront where offsets fit 32 bits, steps are not asked one by one where all exist and none ends an episode
 // (40 -> 17 vector instructions a value; 90 -> 76 us and 92 -> 63 for these two).
 #include "memory.h"
