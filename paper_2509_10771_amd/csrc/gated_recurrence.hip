@@ -655,12 +655,14 @@ void run_shape(const RecArgs& a, hipStream_t s) {
 #undef RUN
 }
 
-// Whether every row of every matrix is a number of whole, aligned loads, and the rows of a workgroup's steps lie within 2^31 bytes, upwards.
-bool rec_whole(const RecArgs& a, int size) {
-  const int64_t MOST = steps_of(BACKWARD_4);      // steps that a workgroup holds at once, at most
+// Whether every row of every matrix is a number of whole, aligned loads, and the rows of the `held` steps that a workgroup has at once lie within 2^31 bytes,
+// upwards.  The distance of steps has no part in it where there is one: so for each shape of its own, and of the steps that there are (24 steps of 8192
+// environments of 256 channels in fp32: forward 123 us, as rows that start anywhere 150; gradients 205 and 242; of 16384 in bf16 162 and 180, 258 and 291).
+bool rec_whole(const RecArgs& a, int size, int held) {
+  if (held > a.T) held = a.T;
   auto fits = [&](const RecMatrix& m) {
-    return !m.p || (reinterpret_cast<uintptr_t>(m.p) % (W * size) == 0 && m.step % W == 0 && m.seq % W == 0 && m.step >= 0 &&
-                    m.step < ((int64_t)1 << 31) / MOST / size - a.D);
+    return !m.p || (reinterpret_cast<uintptr_t>(m.p) % (W * size) == 0 && m.seq % W == 0 &&
+                    (held <= 1 || (m.step % W == 0 && m.step >= 0 && m.step < ((int64_t)1 << 31) / held / size - a.D)));
   };
   return a.D % W == 0 && fits(a.x) && fits(a.g) && fits(a.h) && fits(a.dh) && fits(a.dx) && fits(a.dg);
 }
@@ -682,7 +684,7 @@ bool shared_lines(const RecArgs& a, int size) {
 
 template <typename T>
 void run_type(const RecArgs& a, bool maps, hipStream_t s) {
-  const bool whole = rec_whole(a, (int)sizeof(T));
+  const bool whole = rec_whole(a, (int)sizeof(T), steps_of(a.shape));
   const int stream = stream_of(a, (int)sizeof(T));
   if (maps) whole ? run_shape<T, true, 0, true>(a, s) : run_shape<T, false, 0, true>(a, s);
   else if (!whole) run_shape<T, false, 0, false>(a, s);
@@ -716,7 +718,7 @@ void plan_recurrence(host::Carver& c, RecArgs& a, int dtype, bool backward) {
     else if (a.T <= steps_of(BACKWARD_4_SHORT)) a.shape = BACKWARD_4_SHORT;
     else if (a.T <= steps_of(BACKWARD_4)) a.shape = BACKWARD_4;
     else if (a.T <= 2048 && pieces(BACKWARD_2_SHORT) < (int64_t)1 << 24) a.shape = BACKWARD_2_SHORT;      // (as many as a launch has)
-    else if (a.T > 2048 && a.x.p && rec_whole(a, host::type_size(dtype)) && pieces(BACKWARD_4) >= 1536) a.shape = BACKWARD_4;
+    else if (a.T > 2048 && a.x.p && rec_whole(a, host::type_size(dtype), steps_of(BACKWARD_4)) && pieces(BACKWARD_4) >= 1536) a.shape = BACKWARD_4;
     else a.shape = BACKWARD_4_SHORT;
     a.piece_steps = steps_of(a.shape);
   } else {
@@ -759,7 +761,7 @@ hipError_t launch_recurrence_step(const RecArgs& a, int dtype, hipStream_t strea
   const double n = (double)a.N * a.D, size = dtype == RSLX_F32 ? 4 : 2;
   TraceScope trace(stream, "recurrence_step", 10 * n, (3 * size + 8) * n);
   const dim3 grid((unsigned)(((int64_t)a.N * ((a.D + W - 1) / W) + REC_THREADS - 1) / REC_THREADS)), block(REC_THREADS);
-  const bool whole = rec_whole(a, (int)size);
+  const bool whole = rec_whole(a, (int)size, 1);
 #define RUN(T)                                                                                          \
   do {                                                                                                  \
     if (whole) hipLaunchKernelGGL((recurrence_step_kernel<T, true>), grid, block, 0, stream, a);        \

@@ -1,0 +1,79 @@
+"""Which kernels the entry points around a gated memory launch, by sizes and layouts, found on the CPU: a small program takes the place of the runtime's launch
+and prints what it is asked for (host_launches/memory_launches.cpp).  What a rule chooses has no part in a call's results, so that no other test sees it."""
+import os
+import re
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+PACKAGE = os.path.join(ROOT, "paper_2509_10771_amd")
+CLANGXX = os.environ.get("CLANGXX", "/opt/rocm/lib/llvm/bin/clang++")
+F32, BF16, F16 = 0, 1, 2
+
+pytestmark = pytest.mark.skipif(not os.path.exists(CLANGXX), reason="clang++ not installed")
+
+
+@pytest.fixture(scope="module")
+def launches(tmp_path_factory):
+    """launches(call) -> [(kernel, its template's arguments, workgroups)]."""
+    exe = str(tmp_path_factory.mktemp("launches") / "memory_launches")
+    subprocess.run([CLANGXX, "-std=c++17", "-O1", os.path.join(ROOT, "tests", "host_launches", "memory_launches.cpp"), "-o", exe,
+                    os.path.join(PACKAGE, "librslx.so"), "-Wl,-rpath," + PACKAGE, "-Wl,--export-dynamic", "-Wl,--allow-shlib-undefined"], check=True)
+
+    def ask(call):
+        out = subprocess.run([exe], input=call + "\n", capture_output=True, text=True, check=True, timeout=60).stdout
+        found = re.findall(r"(\w+)(?:<([^;]*)>)? (\d+)x\d+; ", out)
+        assert found, (call, out)
+        return [(kernel, tuple(arguments.split(", ")), int(groups)) for kernel, arguments, groups in found]
+    return ask
+
+
+def _side_by_side(kind, dtype, T, N, D):
+    """Candidates and gates side by side [T, N, 2 D], as one product leaves them; everything else [T, N, D]."""
+    return "%s %d %d %d %d %d %d %d %d" % (kind, dtype, T, N, D, 2 * N * D, 2 * D, N * D, D)
+
+
+def _by_sequence(kind, dtype, T, N, D):
+    """The same with a sequence's steps one after another [N, T, ..]."""
+    return "%s %d %d %d %d %d %d %d %d" % (kind, dtype, T, N, D, 2 * D, 2 * T * D, D, T * D)
+
+
+def _whole(found):
+    """Whether all walks and steps of a call take rows as whole, aligned loads."""
+    walks = [arguments for kernel, arguments, _ in found if kernel.startswith("recurrence") and "join" not in kernel]
+    assert walks
+    return all("true" == arguments[1 if len(arguments) == 2 else 3] for arguments in walks)
+
+
+@pytest.mark.parametrize("dtype,T,N,D", [(F32, 24, 4096, 256), (F32, 24, 8192, 256), (F32, 24, 4096, 512), (BF16, 24, 16384, 256), (F16, 20, 16384, 256),
+                                         (F32, 24, 16384, 512), (F32, 2, 65536, 1024), (BF16, 100, 8192, 512), (F32, 300, 4096, 256)])
+@pytest.mark.parametrize("kind", ["forward", "backward"])
+def test_many_aligned_environments_are_whole_loads(launches, kind, dtype, T, N, D):
+    """Steps of many environments lie far apart; what has to fit 32 bits is the steps that one workgroup holds, of those that there are."""
+    for layout in (_side_by_side, _by_sequence):
+        assert _whole(launches(layout(kind, dtype, T, N, D)))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N", [64, 8192, 16384, 1 << 20])
+def test_one_step_has_no_distance(launches, dtype, N):
+    """The distance of steps is not used where there is one, whatever it is."""
+    D = 256
+    for step in (2 * N * D, 0, 7, -3, 1 << 40, -(1 << 62)):
+        for kind in ("step", "forward", "backward"):
+            assert _whole(launches("%s %d 1 %d %d %d %d %d %d" % (kind, dtype, N, D, step, 2 * D, step, D)))
+
+
+@pytest.mark.parametrize("kind,T,N,D,step", [("forward", 24, 8, 256, 1 << 40), ("backward", 24, 8, 256, 1 << 25), ("forward", 24, 8, 256, -4096), ("forward", 24, 8, 256, 4099),
+                                             ("backward", 24, 8, 255, 4096), ("step", 1, 8, 255, 0)])
+def test_rows_that_start_anywhere_or_far_apart_are_not(launches, kind, T, N, D, step):
+    assert not _whole(launches("%s %d %d %d %d %d %d %d %d" % (kind, F32, T, N, D, step, 2 * D, N * D, D)))
+
+
+@pytest.mark.parametrize("dtype,T,N,D", [(BF16, 32, 12288, 256), (F16, 32, 12288, 256), (BF16, 24, 16384, 256), (F32, 24, 8192, 256), (F32, 20, 4096, 512)])
+def test_large_roll_outs_go_past_the_caches(launches, dtype, T, N, D):
+    """The calls of test_gpu_memory_paths.py: one walk, which reads and writes past the caches."""
+    for kind, kernel, steps in (("forward", "recurrence_kernel", "4"), ("backward", "recurrence_backward_kernel", "8")):
+        (name, arguments, _), = launches(_side_by_side(kind, dtype, T, N, D))
+        assert name == kernel and arguments[1:] == (steps, "1", "true", "2", "false")
