@@ -655,19 +655,36 @@ size_t muon_item_bytes(int32_t rows, int32_t cols) {
   return values_bytes(rows, cols) + MUON_NORM_BLOCKS * sizeof(double) + sizeof(uint16_t) * 2 * (3 * P * Q + 2 * P * P);
 }
 
-// Symmetric products go through the large tiles where these, in at most as many pieces as there are compute units for, fill the GPU, and a piece is 16 stages of 32
-// contraction indices or more.
+// Symmetric products go through the large tiles, in as many pieces as there are compute units for and of 16 stages of 32 contraction indices or more, where
+// that takes less time than 64 x 64 tiles.  In stages of a large tile, both products together: the first the longest piece for each round over the compute units,
+// and 16 for the sums' way through memory; the second 0.23 of a stage for each of a 64 x 64 tile on every compute unit.  Steps with and without large tiles, us:
+// 1930 x 1930 712 and 645, 2048 x 2048 755 and 778, 2048 x 4096 1057 and 1155, 2304 x 2304 1055 and 1035, 2600 x 2600 1397 and 1470, 2700 x 2700 1797 and
+// 1617, 3456 x 3456 2820 and 2900, 4096 x 4096 4910 and 4445, two of 1536 x 1536 698 and 670, ten of 1000 x 1024 1050 and 972, thirty-two of
+// 600 x 610 1062 and 813.
 size_t plan_muon_parts(MuonTable& t, int count) {
-  int64_t tiles = 0, longest = INT32_MAX;
+  int64_t tiles = 0, longest = 0;
+  int least = INT32_MAX;
+  double medium = 0;
   for (int i = 0; i < count; ++i) {
-    const int P = pad32(t.item[i].rows < t.item[i].cols ? t.item[i].rows : t.item[i].cols) / 32;
+    const MuonItem& m = t.item[i];
+    const int P = pad32(m.rows < m.cols ? m.rows : m.cols) / 32, Q = pad32(m.rows < m.cols ? m.cols : m.rows) / 32, n = (P + 1) / 2;
     tiles += wide_triangle_tiles(P);
-    longest = P / 16 < longest ? P / 16 : longest;
+    least = P < least ? P : least;
+    medium += (double)n * (n + 1) / 2 * (P + Q);
   }
-  int64_t pieces = tiles > 0 && tiles < 256 ? 256 / tiles : 1;
-  if (pieces > longest) pieces = longest;
-  t.pieces = tiles * pieces >= 200 ? (int32_t)pieces : 0;
-  return t.pieces > 0 ? (size_t)tiles * pieces * PART : 0;
+  const int64_t fill = tiles > 0 && tiles < 256 ? 256 / tiles : 1, pieces = fill < least / 16 ? fill : least / 16;
+  t.pieces = 0;
+  if (pieces < 1 || count < 1) return 0;
+  for (int i = 0; i < count; ++i) {
+    const MuonItem& m = t.item[i];
+    const int64_t P = pad32(m.rows < m.cols ? m.rows : m.cols) / 32, Q = pad32(m.rows < m.cols ? m.cols : m.rows) / 32;
+    const int64_t stages = (P + pieces - 1) / pieces + (Q + pieces - 1) / pieces;
+    longest = stages > longest ? stages : longest;
+  }
+  const int64_t rounds = (tiles * pieces + 255) / 256;
+  if (rounds * longest + 16 > 0.23 * medium / 256) return 0;
+  t.pieces = (int32_t)pieces;
+  return (size_t)tiles * pieces * PART;
 }
 
 hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int steps, hipStream_t stream) {

@@ -77,3 +77,18 @@ def test_large_roll_outs_go_past_the_caches(launches, dtype, T, N, D):
     for kind, kernel, steps in (("forward", "recurrence_kernel", "4"), ("backward", "recurrence_backward_kernel", "8")):
         (name, arguments, _), = launches(_side_by_side(kind, dtype, T, N, D))
         assert name == kernel and arguments[1:] == (steps, "1", "true", "2", "false")
+
+
+def _symmetric(found):
+    """The kernels of X X^T and its square, each once, with their workgroups."""
+    return sorted({(kernel, arguments[0], groups) for kernel, arguments, groups in found if arguments[0] in ("(MuonProduct)0", "(MuonProduct)1")})
+
+
+@pytest.mark.parametrize("shapes,large", [
+    ("1536x1536", False), ("1800x1800", False), ("1930x1930", False), ("2048x4096", True), ("4096x2048", True), ("2048x8192", True), ("2176x2176", True), ("2304x2304", False),
+    ("2600x2600", True), ("2700x2700", False), ("3000x3000", False), ("3456x3456", True), ("3500x3500", True), ("4096x4096", False),
+    (",".join(["1024x1024"] * 4), False), (",".join(["1000x1024"] * 10), False), (",".join(["600x610"] * 32), False), ("512x256,256x128,128x12", False)])
+def test_symmetric_products_take_large_tiles_where_these_gain(launches, shapes, large):
+    """Both sides of these were timed; two rounds over the compute units for a few tiles more than there are of those, or short contractions in pieces, lose."""
+    kernels = {kernel for kernel, _, _ in _symmetric(launches("muon " + shapes))}
+    assert kernels == ({"muon_large_kernel", "muon_fold_kernel"} if large else {"muon_product_kernel"})
