@@ -634,7 +634,8 @@ int32_t rslx_rms_norm_backward(int32_t dtype, const void* dy, int64_t lddy, cons
  *   w_out = (1 - lr weight_decay) w_in - lr scale X
  * (Jordan et al. 2024: quintic Newton-Schulz steps, which bring every singular value near one).  Each product is fp32's in effect:
  * operands are held as pairs of fp16 values (22 significant bits), sums in fp32.  u = 0 leaves X = 0; a matrix whose u
- * holds a value that is not finite gets NaN, the others of the call nothing of it.
+ * holds a value that is not finite gets NaN, the others of the call nothing of it.  Tiles are chosen for
+ * the call: a matrix's rounding may depend on the sizes of those beside it, the same call gives the same bits.
  * w_in NULL: 0; m_in NULL: 0; m_out NULL: not kept (w_in = m_in = m_out = NULL, lr = -1: X itself).  w_out may be w_in and m_out
  * may be m_in; nothing else that is written may overlap what is read or written.  Pointers are aligned to 4 bytes; the descriptions are host memory,
  * read before the call returns (a captured call keeps them, lr among them). */

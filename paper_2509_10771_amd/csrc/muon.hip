@@ -486,7 +486,7 @@ __global__ __launch_bounds__(256) void muon_large_kernel(const MuonTable* t, int
     half8 right[2][CW][2][2][64];                        // turn, column, step, hi and lo
     Tile tile[4];
   } lds;
-  const Matrix m = matrix_of(*t, SYMMETRIC ? MUON_SYMMETRIC_GRID : MUON_APPLY_GRID);
+  const Matrix m = matrix_of(*t, SYMMETRIC ? MUON_PIECES_GRID : MUON_APPLY_GRID);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), columns = SYMMETRIC ? m.P : m.Q;
   const int kb = (KIND == MUON_GRAM ? m.Q : m.P) * 2;
   int ti, tj, first = 0, stages = kb / 2;
@@ -612,7 +612,7 @@ __global__ __launch_bounds__(256) void muon_fold_kernel(const MuonTable* t, int 
   wide_triangle(at, (m.P + 3) / 4, ti, tj);
   const int rb = ti * 8 + block / 4, cb = tj * 4 + block % 4;
   if (rb > cb || cb >= m.P) return;
-  const float4v* part = reinterpret_cast<const float4v*>(t->parts + (int64_t)(t->first[MUON_SYMMETRIC_GRID][m.index] + at) * PART) + block * 256 + lane;
+  const float4v* part = reinterpret_cast<const float4v*>(t->parts + (int64_t)(t->first[MUON_PIECES_GRID][m.index] + at) * PART) + block * 256 + lane;
   float4v sum[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) sum[q] = get(part + q * 64);
@@ -637,16 +637,20 @@ __global__ __launch_bounds__(256) void muon_fold_kernel(const MuonTable* t, int 
 
 enum MuonShape { SMALL, MEDIUM, LARGE };                 // tiles of 32 x 32, 64 x 64, 256 x 128
 
-// Workgroups of a launch, matrix by matrix.
+// Workgroups of a launch, matrix by matrix.  One that has none begins where the next one does, and matrix_of finds the next.
 template <typename Count>
 unsigned place_items(MuonTable& t, int count, MuonGrid grid, Count of) {
   int64_t n = 0;
   for (int i = 0; i < RSLX_MUON_MAX_MATRICES; ++i) {
     t.first[grid][i] = i < count ? (int32_t)n : INT32_MAX;
-    if (i < count) n += of(t.item[i].rows, t.item[i].cols);
+    if (i < count) n += of(t.item[i]);
   }
   return (unsigned)n;
 }
+
+// Blocks of the shorter and of the longer side.
+int short_blocks(const MuonItem& m) { return pad32(m.rows < m.cols ? m.rows : m.cols) / 32; }
+int long_blocks(const MuonItem& m) { return pad32(m.rows < m.cols ? m.cols : m.rows) / 32; }
 
 }  // namespace
 
@@ -661,104 +665,118 @@ size_t muon_item_bytes(int32_t rows, int32_t cols) {
 // 1930 x 1930 712 and 645, 2048 x 2048 755 and 778, 2048 x 4096 1057 and 1155, 2304 x 2304 1055 and 1035, 2600 x 2600 1397 and 1470, 2700 x 2700 1797 and
 // 1617, 3456 x 3456 2820 and 2900, 4096 x 4096 4910 and 4445, two of 1536 x 1536 698 and 670, ten of 1000 x 1024 1050 and 972, thirty-two of
 // 600 x 610 1062 and 813.
+// It is asked of the matrices from some short side on, of those that save most; the others of the call have launches of their own, which are worth 6 stages (2048 x
+// 4096 with 30 x 100: 1365, all in 64 x 64 tiles 1440).
 size_t plan_muon_parts(MuonTable& t, int count) {
-  int64_t tiles = 0, longest = 0;
-  int least = INT32_MAX;
-  double medium = 0;
-  for (int i = 0; i < count; ++i) {
-    const MuonItem& m = t.item[i];
-    const int P = pad32(m.rows < m.cols ? m.rows : m.cols) / 32, Q = pad32(m.rows < m.cols ? m.cols : m.rows) / 32, n = (P + 1) / 2;
-    tiles += wide_triangle_tiles(P);
-    least = P < least ? P : least;
-    medium += (double)n * (n + 1) / 2 * (P + Q);
-  }
-  const int64_t fill = tiles > 0 && tiles < 256 ? 256 / tiles : 1, pieces = fill < least / 16 ? fill : least / 16;
+  int P[RSLX_MUON_MAX_MATRICES], Q[RSLX_MUON_MAX_MATRICES], least = 0;
+  for (int i = 0; i < count; ++i) P[i] = short_blocks(t.item[i]), Q[i] = long_blocks(t.item[i]);
+  int64_t taken = 0;
+  double most = 0;
   t.pieces = 0;
-  if (pieces < 1 || count < 1) return 0;
   for (int i = 0; i < count; ++i) {
-    const MuonItem& m = t.item[i];
-    const int64_t P = pad32(m.rows < m.cols ? m.rows : m.cols) / 32, Q = pad32(m.rows < m.cols ? m.cols : m.rows) / 32;
-    const int64_t stages = (P + pieces - 1) / pieces + (Q + pieces - 1) / pieces;
-    longest = stages > longest ? stages : longest;
+    if (P[i] < 16) continue;
+    int64_t tiles = 0, longest = 0;
+    double medium = 0;
+    bool others = false;
+    for (int j = 0; j < count; ++j) {
+      if (P[j] < P[i]) {
+        others = true;
+        continue;
+      }
+      const int n = (P[j] + 1) / 2;
+      tiles += wide_triangle_tiles(P[j]);
+      medium += (double)n * (n + 1) / 2 * (P[j] + Q[j]);
+    }
+    const int64_t fill = tiles < 256 ? 256 / tiles : 1, pieces = fill < P[i] / 16 ? fill : P[i] / 16;
+    for (int j = 0; j < count; ++j) {
+      const int64_t stages = (P[j] + pieces - 1) / pieces + (Q[j] + pieces - 1) / pieces;
+      if (P[j] >= P[i] && stages > longest) longest = stages;
+    }
+    const double saves = 0.23 * medium / 256 - (double)((tiles * pieces + 255) / 256 * longest + 16 + (others ? 6 : 0));
+    if (saves < 0 || (least > 0 && saves <= most)) continue;
+    least = P[i];
+    most = saves;
+    taken = tiles * pieces;
+    t.pieces = (int32_t)pieces;
   }
-  const int64_t rounds = (tiles * pieces + 255) / 256;
-  if (rounds * longest + 16 > 0.23 * medium / 256) return 0;
-  t.pieces = (int32_t)pieces;
-  return (size_t)tiles * pieces * PART;
+  for (int i = 0; i < count; ++i) t.item[i].in_pieces = least > 0 && P[i] >= least;
+  return (size_t)taken * PART;
 }
 
 hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int steps, hipStream_t stream) {
-  double values = 0, gram = 0, square = 0, apply = 0, planes = 0, symmetric = 0;
+  // operations and bytes of the symmetric products of matrices whose are not and are made in pieces, and of the others of all
+  double values = 0, apply = 0, planes[2] = {}, gram[2] = {}, square[2] = {}, symmetric[2] = {};
   for (int i = 0; i < count; ++i) {
     const double rows = t.item[i].rows, cols = t.item[i].cols, p = rows < cols ? rows : cols, q = rows < cols ? cols : rows;
+    const int k = t.item[i].in_pieces;
     values += p * q;
-    gram += p * p * q;
-    square += p * p * p;
     apply += 2 * p * p * q;
-    planes += 4 * p * q;
-    symmetric += 4 * p * p;
+    gram[k] += p * p * q;
+    square[k] += p * p * p;
+    planes[k] += 4 * p * q;
+    symmetric[k] += 4 * p * p;
   }
+  const double all_planes = planes[0] + planes[1], all_symmetric = symmetric[0] + symmetric[1];
   // tiles of b x b blocks
   const auto symmetric_tiles = [](int b) {
-    return [=](int rows, int cols) {
-      const int64_t n = (pad32(rows < cols ? rows : cols) / 32 + b - 1) / b;
-      return n * (n + 1) / 2;
+    return [=](const MuonItem& m) {
+      const int64_t n = (short_blocks(m) + b - 1) / b;
+      return m.in_pieces ? 0 : n * (n + 1) / 2;
     };
   };
   const auto apply_tiles = [](int high, int wide) {
-    return [=](int rows, int cols) {
-      const int p = rows < cols ? rows : cols, q = rows < cols ? cols : rows;
-      return (int64_t)((pad32(p) / 32 + high - 1) / high) * ((pad32(q) / 32 + wide - 1) / wide);
-    };
+    return [=](const MuonItem& m) { return (int64_t)((short_blocks(m) + high - 1) / high) * ((long_blocks(m) + wide - 1) / wide); };
   };
   // the largest tiles that are as many as the GPU has compute units, the smallest where none are
-  MuonShape symmetric_shape = SMALL, apply_shape = SMALL;
-  unsigned on_symmetric, on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(8, 4)), on_fold = 0;
-  if (t.pieces > 0) {
-    symmetric_shape = LARGE;
-    const auto tiles = [](int rows, int cols) { return (int64_t)wide_triangle_tiles(pad32(rows < cols ? rows : cols) / 32); };
-    on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, [&](int rows, int cols) { return tiles(rows, cols) * t.pieces; });
-    on_fold = place_items(t, count, MUON_FOLD_GRID, [&](int rows, int cols) { return tiles(rows, cols) * 8; });
-  } else if ((on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(2))) >= 256) {
-    symmetric_shape = MEDIUM;
-  } else {
+  MuonShape symmetric_shape = MEDIUM, apply_shape = LARGE;
+  const auto large_tiles = [](const MuonItem& m) { return m.in_pieces ? (int64_t)wide_triangle_tiles(short_blocks(m)) : 0; };
+  const unsigned on_pieces = place_items(t, count, MUON_PIECES_GRID, [&](const MuonItem& m) { return large_tiles(m) * t.pieces; });
+  const unsigned on_fold = place_items(t, count, MUON_FOLD_GRID, [&](const MuonItem& m) { return large_tiles(m) * 8; });
+  unsigned on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(2)), on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(8, 4));
+  if (on_symmetric < 256) {
+    symmetric_shape = SMALL;
     on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(1));
   }
-  if (on_apply >= 256) apply_shape = LARGE;
-  else if ((on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(2, 2))) >= 256) apply_shape = MEDIUM;
-  else on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(1, 1));
-  const unsigned on_pack = place_items(t, count, MUON_PACK_GRID, [](int rows, int cols) { return ((int64_t)(pad32(rows) / 32) * (pad32(cols) / 32) + 3) / 4; });
-  const unsigned on_momentum = place_items(t, count, MUON_MOMENTUM_GRID, [](int rows, int cols) { return (int64_t)norm_blocks(rows, cols); });
+  if (on_apply < 256) {
+    apply_shape = MEDIUM;
+    if ((on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(2, 2))) < 256) {
+      apply_shape = SMALL;
+      on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(1, 1));
+    }
+  }
+  const unsigned on_pack = place_items(t, count, MUON_PACK_GRID, [](const MuonItem& m) { return ((int64_t)short_blocks(m) * long_blocks(m) + 3) / 4; });
+  const unsigned on_momentum = place_items(t, count, MUON_MOMENTUM_GRID, [](const MuonItem& m) { return (int64_t)norm_blocks(m.rows, m.cols); });
   {
     TraceScope trace(stream, "muon_momentum", 6 * values, 16 * values);
     hipLaunchKernelGGL(muon_momentum_kernel, dim3(on_momentum), dim3(ELEMENT_THREADS), 0, stream, t, in_workspace);
   }
   {
-    TraceScope trace(stream, "muon_pack", values, 4 * values + 2 * planes);
+    TraceScope trace(stream, "muon_pack", values, 4 * values + 2 * all_planes);
     hipLaunchKernelGGL(muon_pack_kernel, dim3(on_pack), dim3(ELEMENT_THREADS), 0, stream, in_workspace);
   }
-  auto product = [&](auto kind, const char* name, double flops, double bytes, int turn) {
+  auto tiles = [&](auto kind, MuonShape shape, unsigned groups, const char* name, double flops, double bytes, int turn) {
     constexpr MuonProduct KIND = decltype(kind)::value;
-    constexpr bool SYMMETRIC = KIND == MUON_GRAM || KIND == MUON_SQUARE;
-    const dim3 grid(SYMMETRIC ? on_symmetric : on_apply);
-    const MuonShape shape = SYMMETRIC ? symmetric_shape : apply_shape;
-    {
-      TraceScope trace(stream, name, flops, bytes);
-      if (shape == SMALL) hipLaunchKernelGGL((muon_product_kernel<KIND, 1, 4>), grid, dim3(256), 0, stream, in_workspace, turn);
-      else if (shape == MEDIUM) hipLaunchKernelGGL((muon_product_kernel<KIND, 2, 3>), grid, dim3(256), 0, stream, in_workspace, turn);
-      else hipLaunchKernelGGL((muon_large_kernel<KIND>), grid, dim3(256), 0, stream, in_workspace, turn);
-    }
-    if constexpr (SYMMETRIC)
-      if (shape == LARGE) {
-        TraceScope trace(stream, "muon_fold", 0, 0);
-        hipLaunchKernelGGL((muon_fold_kernel<KIND>), dim3(on_fold), dim3(256), 0, stream, in_workspace, turn);
-      }
+    const dim3 grid(groups);
+    TraceScope trace(stream, name, flops, bytes);
+    if (shape == SMALL) hipLaunchKernelGGL((muon_product_kernel<KIND, 1, 4>), grid, dim3(256), 0, stream, in_workspace, turn);
+    else if (shape == MEDIUM) hipLaunchKernelGGL((muon_product_kernel<KIND, 2, 3>), grid, dim3(256), 0, stream, in_workspace, turn);
+    else hipLaunchKernelGGL((muon_large_kernel<KIND>), grid, dim3(256), 0, stream, in_workspace, turn);
   };
+  auto symmetric_product = [&](auto kind, const char* name, const double (&flops)[2], const double (&bytes)[2], int turn) {
+    constexpr MuonProduct KIND = decltype(kind)::value;
+    if (on_pieces > 0) {
+      tiles(kind, LARGE, on_pieces, name, flops[1], bytes[1], turn);
+      TraceScope trace(stream, "muon_fold", 0, 0);
+      hipLaunchKernelGGL((muon_fold_kernel<KIND>), dim3(on_fold), dim3(256), 0, stream, in_workspace, turn);
+    }
+    if (on_symmetric > 0) tiles(kind, symmetric_shape, on_symmetric, name, flops[0], bytes[0], turn);
+  };
+  const double gram_bytes[] = {planes[0] + symmetric[0], planes[1] + symmetric[1]}, square_bytes[] = {2 * symmetric[0], 2 * symmetric[1]};
   for (int s = 0; s < steps; ++s) {
-    product(std::integral_constant<MuonProduct, MUON_GRAM>(), "muon_gram", gram, planes + symmetric, s & 1);
-    product(std::integral_constant<MuonProduct, MUON_SQUARE>(), "muon_square", square, 2 * symmetric, s & 1);
-    if (s + 1 < steps) product(std::integral_constant<MuonProduct, MUON_APPLY>(), "muon_apply", apply, symmetric + 3 * planes, s & 1);
-    else product(std::integral_constant<MuonProduct, MUON_LAST>(), "muon_apply", apply, symmetric + 3 * planes, s & 1);
+    symmetric_product(std::integral_constant<MuonProduct, MUON_GRAM>(), "muon_gram", gram, gram_bytes, s & 1);
+    symmetric_product(std::integral_constant<MuonProduct, MUON_SQUARE>(), "muon_square", square, square_bytes, s & 1);
+    if (s + 1 < steps) tiles(std::integral_constant<MuonProduct, MUON_APPLY>(), apply_shape, on_apply, "muon_apply", apply, all_symmetric + 3 * all_planes, s & 1);
+    else tiles(std::integral_constant<MuonProduct, MUON_LAST>(), apply_shape, on_apply, "muon_apply", apply, all_symmetric + 3 * all_planes, s & 1);
   }
   return hipGetLastError();
 }

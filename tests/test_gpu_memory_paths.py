@@ -1,8 +1,10 @@
 """Paths of the operators around a gated memory that sizes choose (test_memory_launches.py holds which sizes choose which): 16-bit and fp32 roll-outs past the
-caches."""
+caches, the Muon step's symmetric products in pieces for several matrices."""
 import pytest
 import torch
 
+from oracle import muon as om
+from sequence_util import U
 from test_gpu_memory_large import _recurrence
 
 pytestmark = pytest.mark.gpu
@@ -50,3 +52,63 @@ def test_one_step_of_many_environments_is_theirs(rx, dtype):
         part = slice(n, n + 33)
         for a, b in zip(whole, step(xg[:, part].contiguous(), s[part].contiguous(), reset[part].contiguous())):
             assert torch.equal(a[part], b)
+
+
+def _apart(x, y, ex, ey):
+    """|x y| and the error of a product of held operands that are off by ex and ey, entry by entry: 3 K terms are summed in fp32, in whatever order, each addition off
+    by a unit (2 u) at most; what the pairs of fp16 leave out is 4 u of a term, and an operand's rest is lost below 2^-37."""
+    k = x.shape[1]
+    size = x @ y
+    off = ex @ (y + ey) + x @ ey + 1.01 * (6 * k + 16) * U * size
+    return size, off + 2.0 ** -37 * (x.sum(1, keepdim=True) + y.sum(0, keepdim=True))
+
+
+def _held(x, off):
+    """The error of values that are held as two fp16 numbers after it."""
+    return off + 2.0 ** -22 * (x + off) + 2.0 ** -37
+
+
+def _two_steps(u):
+    """X after two steps in fp64, shorter side first, and what each entry may be off by: first order and all higher ones, in absolute values."""
+    t = lambda m: m.t().contiguous()  # noqa: E731
+    x = u.double() / u.double().norm()
+    x = t(x) if x.shape[0] > x.shape[1] else x
+    off = _held(x.abs(), 4 * U * x.abs())
+    eye = torch.eye(x.shape[0], dtype=torch.float64, device=x.device)
+    for _ in range(2):
+        a = x @ t(x)
+        ea = _apart(x.abs(), t(x).abs(), off, t(off))[1]
+        ea = _held(a.abs(), ea)
+        square = a @ a
+        es = _apart(a.abs(), a.abs(), ea, ea)[1]
+        b = om.A * eye + om.B * a + om.C * square
+        eb = -om.B * ea + om.C * es + 8 * U * (om.A * eye - om.B * (a.abs() + ea) + om.C * (square.abs() + es))
+        off = _apart(b.abs(), x.abs(), _held(b.abs(), eb), off)[1]
+        x = b @ x
+        off = _held(x.abs(), off)
+    return x, off + 4 * U * x.abs()
+
+
+@pytest.mark.parametrize("shapes", [
+    [(1536, 1536), (1530, 1700)],                              # two matrices in three pieces each
+    [(1900, 3000), (1600, 2000)],                              # in two
+    [(2600, 2600), (2600, 2700)],                              # in one
+    [(40, 70), (2000, 4200), (12, 2000), (4200, 40)],          # one in three pieces among others in tiles of 32 x 32
+    [(300, 9000), (2700, 2600), (2600, 2600)] + [(480, 500)] * 8,        # two in one piece each, the others in tiles of 64 x 64
+    [(100, 130), (1, 1), (333, 777)], [(1000, 1024)] * 3,      # no pieces: tiles of 32 x 32, of 64 x 64
+], ids=lambda s: "%dx%dx%d" % (len(s), *s[0]))
+def test_symmetric_products_of_several_matrices(rx, shapes):
+    """Two steps, every entry within a bound of its own: what belongs to another block, piece or matrix is seen wherever it is."""
+    g = torch.Generator("cuda").manual_seed(len(shapes))
+    us = [torch.randn(s, generator=g, device="cuda") for s in shapes]
+    outs = [torch.full_like(u, float("nan")) for u in us]
+    mu = rx.Muon([(None, o, u, None, None, 1.0) for u, o in zip(us, outs)], -1.0, nesterov=False, steps=2)
+    rx.rslx_muon_step(mu, rx.workspace(rx.rslx_muon_step_workspace_bytes(mu)))
+    for i, (u, o) in enumerate(zip(us, outs)):
+        ref, bound = _two_steps(u)
+        got = o.double().t() if o.shape[0] > o.shape[1] else o.double()
+        rms = ref.square().mean().sqrt().item()
+        assert bound.max().item() < 0.3 * rms, (i, u.shape, bound.max().item(), rms)
+        off = (got - ref).abs()
+        worst = (off / bound).max().item()
+        assert torch.isfinite(off).all() and worst <= 1, (i, u.shape, worst)

@@ -92,3 +92,28 @@ def test_symmetric_products_take_large_tiles_where_these_gain(launches, shapes, 
     """Both sides of these were timed; two rounds over the compute units for a few tiles more than there are of those, or short contractions in pieces, lose."""
     kernels = {kernel for kernel, _, _ in _symmetric(launches("muon " + shapes))}
     assert kernels == ({"muon_large_kernel", "muon_fold_kernel"} if large else {"muon_product_kernel"})
+
+
+@pytest.mark.parametrize("large", ["2048x4096", "4096x2048", "3500x3500", "2600x2600,2600x2700"])
+@pytest.mark.parametrize("small", ["30x100", "2048x12", "512x2048", "12x12,1x1", "480x65536", "1000x1000,300x200"])
+def test_a_small_matrix_takes_nothing_from_a_large_one(launches, large, small):
+    """Symmetric products of large matrices in large tiles and pieces of the contraction, whatever else is in the call, and wherever: the same workgroups, or more
+    of the same round where smaller matrices go with them."""
+    alone, beside = _symmetric(launches("muon " + large)), small.split(",")
+    assert [kernel for kernel, _, _ in alone] == ["muon_fold_kernel"] * 2 + ["muon_large_kernel"] * 2
+    for together in (large.split(",") + beside, beside + large.split(","), large.split(",")[:1] + beside + large.split(",")[1:]):
+        found = _symmetric(launches("muon " + ",".join(together)))
+        there = [x for x in found if x[0] != "muon_product_kernel"]
+        assert there == alone or ([x[:2] for x in there] == [x[:2] for x in alone] and all(a[2] < b[2] <= max(256, a[2]) * (1 if "large" in a[0] else 8)
+                                                                                          for a, b in zip(alone, there)))
+
+
+@pytest.mark.parametrize("shapes,pieces,others", [
+    ("1536x1536,1530x1700", 252, None), ("1900x3000,1600x2000", 226, None), ("2600x2600,2600x2700", 242, None), ("40x70,2000x4200,12x2000,4200x40", 216, "1"),
+    ("300x9000,2700x2600,2600x2600" + ",480x500" * 8, 242, "2"), ("100x130,1x1,333x777", 0, "1"), ("1000x1024,1000x1024,1000x1024", 0, "2")])
+def test_symmetric_products_take_their_forms(launches, shapes, pieces, others):
+    """The calls of test_gpu_memory_paths.py: workgroups of the pieces, tiles of the others in blocks."""
+    found = launches("muon " + shapes)
+    for product in ("(MuonProduct)0", "(MuonProduct)1"):
+        assert {groups for kernel, arguments, groups in found if kernel == "muon_large_kernel" and arguments[0] == product} == ({pieces} if pieces else set())
+        assert {arguments[1] for kernel, arguments, _ in found if kernel == "muon_product_kernel" and arguments[0] == product} == ({others} if others else set())
