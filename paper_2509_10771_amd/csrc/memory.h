@@ -66,11 +66,11 @@ struct alignas(16) MuonItem {
   char* base;                   // the matrix's part of the workspace (muon_item_bytes)
   int32_t rows, cols;
   float scale;
-  int32_t in_pieces;            // whether its symmetric products are made in pieces of the contraction (plan_muon_parts)
+  int16_t in_pieces, large;     // whether its symmetric products are made in pieces of the contraction (plan_muon_parts), whether that with X in large tiles
 };
 // What every launch reads: the first one, which has it as an argument, leaves it at the start of the workspace for the others (an argument of that size
 // is read from memory of the host, several times in a row).
-enum MuonGrid { MUON_MOMENTUM_GRID, MUON_PACK_GRID, MUON_SYMMETRIC_GRID, MUON_PIECES_GRID, MUON_FOLD_GRID, MUON_APPLY_GRID, MUON_GRIDS };
+enum MuonGrid { MUON_MOMENTUM_GRID, MUON_PACK_GRID, MUON_SYMMETRIC_GRID, MUON_PIECES_GRID, MUON_FOLD_GRID, MUON_APPLY_GRID, MUON_LARGE_GRID, MUON_GRIDS };
 struct MuonTable {
   MuonItem item[RSLX_MUON_MAX_MATRICES];
   int32_t first[MUON_GRIDS][RSLX_MUON_MAX_MATRICES];     // workgroup of a launch that a matrix begins with; INT32_MAX behind the last one

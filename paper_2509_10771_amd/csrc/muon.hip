@@ -486,7 +486,7 @@ __global__ __launch_bounds__(256) void muon_large_kernel(const MuonTable* t, int
     half8 right[2][CW][2][2][64];                        // turn, column, step, hi and lo
     Tile tile[4];
   } lds;
-  const Matrix m = matrix_of(*t, SYMMETRIC ? MUON_PIECES_GRID : MUON_APPLY_GRID);
+  const Matrix m = matrix_of(*t, SYMMETRIC ? MUON_PIECES_GRID : MUON_LARGE_GRID);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), columns = SYMMETRIC ? m.P : m.Q;
   const int kb = (KIND == MUON_GRAM ? m.Q : m.P) * 2;
   int ti, tj, first = 0, stages = kb / 2;
@@ -703,20 +703,59 @@ size_t plan_muon_parts(MuonTable& t, int count) {
   return (size_t)taken * PART;
 }
 
+// Tiles of high x wide blocks of a product with X.
+static int64_t apply_tiles(const MuonItem& m, int high, int wide) {
+  return (int64_t)((short_blocks(m) + high - 1) / high) * ((long_blocks(m) + wide - 1) / wide);
+}
+
+// Products with X take 256 x 128 tiles where these are as many as the GPU has compute units: those of the matrices from some short side on, of as many as take the
+// least time.  In stages of such a tile: the longest for each round over the compute units, 0.175 for each of a 64 x 64 tile of the others on every compute unit,
+// 3 for a launch of the others (2048 x 4096, whose 256 tiles are one round, with 30 x 100 in a launch of its own 97 and 5 us, with 257 tiles 148).
+static void plan_muon_large(MuonTable& t, int count) {
+  int64_t all = 0;
+  for (int i = 0; i < count; ++i) all += apply_tiles(t.item[i], 8, 4);
+  int least = INT32_MAX;
+  double most = 0;
+  for (int i = 0; i < count && all >= 256; ++i) {
+    const int from = short_blocks(t.item[i]);
+    int64_t tiles = 0;
+    int longest = 0;
+    double medium = 0;
+    bool others = false;
+    for (int j = 0; j < count; ++j) {
+      const int P = short_blocks(t.item[j]);
+      if (P < from) {
+        others = true;
+        medium += (double)apply_tiles(t.item[j], 2, 2) * P;
+      } else {
+        tiles += apply_tiles(t.item[j], 8, 4);
+        longest = P > longest ? P : longest;
+      }
+    }
+    const double takes = (double)((tiles + 255) / 256 * longest) + 0.175 * medium / 256 + (others ? 3 : 0);
+    if (tiles < 256 || (least < INT32_MAX && takes >= most)) continue;
+    least = from;
+    most = takes;
+  }
+  for (int i = 0; i < count; ++i) t.item[i].large = short_blocks(t.item[i]) >= least;
+}
+
 hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int steps, hipStream_t stream) {
-  // operations and bytes of the symmetric products of matrices whose are not and are made in pieces, and of the others of all
-  double values = 0, apply = 0, planes[2] = {}, gram[2] = {}, square[2] = {}, symmetric[2] = {};
+  plan_muon_large(t, count);
+  // operations and bytes of products, of matrices that take large tiles in the second place
+  double values = 0, planes = 0, gram[2] = {}, square[2] = {}, apply[2] = {}, gram_bytes[2] = {}, square_bytes[2] = {}, apply_bytes[2] = {};
   for (int i = 0; i < count; ++i) {
     const double rows = t.item[i].rows, cols = t.item[i].cols, p = rows < cols ? rows : cols, q = rows < cols ? cols : rows;
-    const int k = t.item[i].in_pieces;
+    const int k = t.item[i].in_pieces, l = t.item[i].large;
     values += p * q;
-    apply += 2 * p * p * q;
+    planes += 4 * p * q;
     gram[k] += p * p * q;
+    gram_bytes[k] += 4 * p * q + 4 * p * p;
     square[k] += p * p * p;
-    planes[k] += 4 * p * q;
-    symmetric[k] += 4 * p * p;
+    square_bytes[k] += 8 * p * p;
+    apply[l] += 2 * p * p * q;
+    apply_bytes[l] += 4 * p * p + 12 * p * q;
   }
-  const double all_planes = planes[0] + planes[1], all_symmetric = symmetric[0] + symmetric[1];
   // tiles of b x b blocks
   const auto symmetric_tiles = [](int b) {
     return [=](const MuonItem& m) {
@@ -724,26 +763,24 @@ hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int ste
       return m.in_pieces ? 0 : n * (n + 1) / 2;
     };
   };
-  const auto apply_tiles = [](int high, int wide) {
-    return [=](const MuonItem& m) { return (int64_t)((short_blocks(m) + high - 1) / high) * ((long_blocks(m) + wide - 1) / wide); };
+  const auto tiles_with_x = [](int high, int wide, bool large) {
+    return [=](const MuonItem& m) { return large == (m.large != 0) ? apply_tiles(m, high, wide) : 0; };
   };
-  // the largest tiles that are as many as the GPU has compute units, the smallest where none are
-  MuonShape symmetric_shape = MEDIUM, apply_shape = LARGE;
+  // of those that are not in pieces or large: the larger tiles that are as many as the GPU has compute units, the smallest where these are fewer
+  MuonShape symmetric_shape = MEDIUM, apply_shape = MEDIUM;
   const auto large_tiles = [](const MuonItem& m) { return m.in_pieces ? (int64_t)wide_triangle_tiles(short_blocks(m)) : 0; };
   const unsigned on_pieces = place_items(t, count, MUON_PIECES_GRID, [&](const MuonItem& m) { return large_tiles(m) * t.pieces; });
   const unsigned on_fold = place_items(t, count, MUON_FOLD_GRID, [&](const MuonItem& m) { return large_tiles(m) * 8; });
-  unsigned on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(2)), on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(8, 4));
+  unsigned on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(2)), on_apply = place_items(t, count, MUON_APPLY_GRID, tiles_with_x(2, 2, false));
   if (on_symmetric < 256) {
     symmetric_shape = SMALL;
     on_symmetric = place_items(t, count, MUON_SYMMETRIC_GRID, symmetric_tiles(1));
   }
   if (on_apply < 256) {
-    apply_shape = MEDIUM;
-    if ((on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(2, 2))) < 256) {
-      apply_shape = SMALL;
-      on_apply = place_items(t, count, MUON_APPLY_GRID, apply_tiles(1, 1));
-    }
+    apply_shape = SMALL;
+    on_apply = place_items(t, count, MUON_APPLY_GRID, tiles_with_x(1, 1, false));
   }
+  const unsigned on_large = place_items(t, count, MUON_LARGE_GRID, tiles_with_x(8, 4, true));
   const unsigned on_pack = place_items(t, count, MUON_PACK_GRID, [](const MuonItem& m) { return ((int64_t)short_blocks(m) * long_blocks(m) + 3) / 4; });
   const unsigned on_momentum = place_items(t, count, MUON_MOMENTUM_GRID, [](const MuonItem& m) { return (int64_t)norm_blocks(m.rows, m.cols); });
   {
@@ -751,7 +788,7 @@ hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int ste
     hipLaunchKernelGGL(muon_momentum_kernel, dim3(on_momentum), dim3(ELEMENT_THREADS), 0, stream, t, in_workspace);
   }
   {
-    TraceScope trace(stream, "muon_pack", values, 4 * values + 2 * all_planes);
+    TraceScope trace(stream, "muon_pack", values, 4 * values + 2 * planes);
     hipLaunchKernelGGL(muon_pack_kernel, dim3(on_pack), dim3(ELEMENT_THREADS), 0, stream, in_workspace);
   }
   auto tiles = [&](auto kind, MuonShape shape, unsigned groups, const char* name, double flops, double bytes, int turn) {
@@ -771,12 +808,15 @@ hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int ste
     }
     if (on_symmetric > 0) tiles(kind, symmetric_shape, on_symmetric, name, flops[0], bytes[0], turn);
   };
-  const double gram_bytes[] = {planes[0] + symmetric[0], planes[1] + symmetric[1]}, square_bytes[] = {2 * symmetric[0], 2 * symmetric[1]};
+  auto product_with_x = [&](auto kind, int turn) {
+    if (on_large > 0) tiles(kind, LARGE, on_large, "muon_apply", apply[1], apply_bytes[1], turn);
+    if (on_apply > 0) tiles(kind, apply_shape, on_apply, "muon_apply", apply[0], apply_bytes[0], turn);
+  };
   for (int s = 0; s < steps; ++s) {
     symmetric_product(std::integral_constant<MuonProduct, MUON_GRAM>(), "muon_gram", gram, gram_bytes, s & 1);
     symmetric_product(std::integral_constant<MuonProduct, MUON_SQUARE>(), "muon_square", square, square_bytes, s & 1);
-    if (s + 1 < steps) tiles(std::integral_constant<MuonProduct, MUON_APPLY>(), apply_shape, on_apply, "muon_apply", apply, all_symmetric + 3 * all_planes, s & 1);
-    else tiles(std::integral_constant<MuonProduct, MUON_LAST>(), apply_shape, on_apply, "muon_apply", apply, all_symmetric + 3 * all_planes, s & 1);
+    if (s + 1 < steps) product_with_x(std::integral_constant<MuonProduct, MUON_APPLY>(), s & 1);
+    else product_with_x(std::integral_constant<MuonProduct, MUON_LAST>(), s & 1);
   }
   return hipGetLastError();
 }

@@ -1,5 +1,5 @@
 """Paths of the operators around a gated memory that sizes choose (test_memory_launches.py holds which sizes choose which): 16-bit and fp32 roll-outs past the
-caches, the Muon step's symmetric products in pieces for several matrices."""
+caches, the Muon step's products for several matrices, in tiles and pieces of each kind."""
 import pytest
 import torch
 
@@ -96,8 +96,10 @@ def _two_steps(u):
     [(40, 70), (2000, 4200), (12, 2000), (4200, 40)],          # one in three pieces among others in tiles of 32 x 32
     [(300, 9000), (2700, 2600), (2600, 2600)] + [(480, 500)] * 8,        # two in one piece each, the others in tiles of 64 x 64
     [(100, 130), (1, 1), (333, 777)], [(1000, 1024)] * 3,      # no pieces: tiles of 32 x 32, of 64 x 64
+    [(30, 100), (2040, 4090), (300, 200)],                     # a product with X in large tiles beside others in tiles of 32 x 32
+    [(2048, 2000), (1900, 600), (2000, 2048)],                 # two beside one in tiles of 64 x 64
 ], ids=lambda s: "%dx%dx%d" % (len(s), *s[0]))
-def test_symmetric_products_of_several_matrices(rx, shapes):
+def test_products_of_several_matrices(rx, shapes):
     """Two steps, every entry within a bound of its own: what belongs to another block, piece or matrix is seen wherever it is."""
     g = torch.Generator("cuda").manual_seed(len(shapes))
     us = [torch.randn(s, generator=g, device="cuda") for s in shapes]

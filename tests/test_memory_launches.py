@@ -117,3 +117,30 @@ def test_symmetric_products_take_their_forms(launches, shapes, pieces, others):
     for product in ("(MuonProduct)0", "(MuonProduct)1"):
         assert {groups for kernel, arguments, groups in found if kernel == "muon_large_kernel" and arguments[0] == product} == ({pieces} if pieces else set())
         assert {arguments[1] for kernel, arguments, _ in found if kernel == "muon_product_kernel" and arguments[0] == product} == ({others} if others else set())
+
+
+def _apply(found):
+    """The kernels of the product with X, each once, with their tiles and workgroups."""
+    return sorted({(kernel, arguments[1:2], groups) for kernel, arguments, groups in found if arguments[0] == "(MuonProduct)2"})
+
+
+@pytest.mark.parametrize("large", ["2048x4096", "4096x2048", "2048x8192", "4096x4096"])
+@pytest.mark.parametrize("small", ["30x100", "2048x12", "512x2048", "12x12,1x1", "300x200,200x300,12x300"])
+def test_a_small_matrix_adds_no_round_to_a_large_ones_product(launches, large, small):
+    """Tiles of 256 x 128 that are as many as the compute units, or twice as many: one more would take as long as all of them."""
+    alone, beside = _apply(launches("muon " + large)), small.split(",")
+    (kernel, _, groups), = alone
+    assert kernel == "muon_large_kernel" and groups % 256 == 0
+    for together in ([large] + beside, beside + [large], beside[:1] + [large] + beside[1:]):
+        found = _apply(launches("muon " + ",".join(together)))
+        assert [x for x in found if x[0] == kernel] == alone and any(x[0] == "muon_product_kernel" for x in found)
+
+
+@pytest.mark.parametrize("shapes,groups,others", [
+    (",".join(["500x520"] * 31 + ["40x33"]), 311, None), ("3000x3000", 288, None), (",".join(["1000x1024"] * 10), 320, None), ("2048x4096,1900x1900", 256, "2"),
+    ("2048x4096,333x100", 256, "1"), ("777x333,235x512,333x1001,30x100", None, "1"), ("2047x4065", 256, None), ("2048x2048", None, "2"), ("30x100,2040x4090,300x200", 256, "1"),
+    ("2048x2000,1900x600,2000x2048", 256, "2")])
+def test_products_with_x_take_their_forms(launches, shapes, groups, others):
+    found = _apply(launches("muon " + shapes))
+    assert [x[2] for x in found if x[0] == "muon_large_kernel"] == ([groups] if groups else [])
+    assert [x[1] for x in found if x[0] == "muon_product_kernel"] == ([(others,)] if others else [])
