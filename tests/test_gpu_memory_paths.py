@@ -1,10 +1,12 @@
 """Paths of the operators around a gated memory that sizes choose (test_memory_launches.py holds which sizes choose which): 16-bit and fp32 roll-outs past the
-caches, the Muon step's products for several matrices, in tiles and pieces of each kind."""
+caches, the Muon step's products for several matrices, in tiles and pieces of each kind,
+long sequences in pieces of 128 steps and in more than 128 pieces."""
 import pytest
 import torch
 
 from oracle import muon as om
 from sequence_util import U
+from test_gpu_gated_recurrence import Case
 from test_gpu_memory_large import _recurrence
 
 pytestmark = pytest.mark.gpu
@@ -114,3 +116,15 @@ def test_products_of_several_matrices(rx, shapes):
         off = (got - ref).abs()
         worst = (off / bound).max().item()
         assert torch.isfinite(off).all() and worst <= 1, (i, u.shape, worst)
+
+
+@pytest.mark.parametrize("T,N,D,dtype,layout,ragged", [
+    (4096, 4, 1024, "bf16", "side", False), (2500, 6, 896, "fp32", "dense", True), (3001, 5, 1280, "fp16", "side", True),      # gradients in pieces of 128 steps
+    (9000, 2, 64, "fp32", "side", False), (12345, 1, 40, "bf16", "odd", True), (20000, 3, 20, "fp16", "batch_first", True)],   # more than 128 pieces to join
+    ids=lambda x: str(x))
+def test_long_sequences(rx, T, N, D, dtype, layout, ragged):
+    c = Case(T, T, N, D, dtype, done_p=0.0005, ragged=ragged, layout=layout)
+    if ragged and N > 2:
+        c.lengths[2] = T - 1
+    c.check_forward(*c.forward(rx))
+    c.check_backward(*c.backward(rx))

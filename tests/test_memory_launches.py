@@ -144,3 +144,18 @@ def test_products_with_x_take_their_forms(launches, shapes, groups, others):
     found = _apply(launches("muon " + shapes))
     assert [x[2] for x in found if x[0] == "muon_large_kernel"] == ([groups] if groups else [])
     assert [x[1] for x in found if x[0] == "muon_product_kernel"] == ([(others,)] if others else [])
+
+
+@pytest.mark.parametrize("dtype,T,N,D,layout,forward,backward", [
+    (BF16, 4096, 4, 1024, _side_by_side, 1024, ("8", "4", 32)), (F32, 2500, 6, 896, _side_by_side, None, ("8", "4", 20)), (F16, 3001, 5, 1280, _side_by_side, None, ("8", "4", 24)),
+    (F32, 9000, 2, 64, _side_by_side, 282, ("4", "4", 141)), (BF16, 12345, 1, 40, _side_by_side, 193, ("4", "4", 193)), (F16, 20000, 3, 20, _by_sequence, 939, ("4", "4", 313))])
+def test_long_sequences_take_their_pieces(launches, dtype, T, N, D, layout, forward, backward):
+    """The calls of test_gpu_memory_paths.py: forward workgroups; backward steps of a lane, wavefronts, pieces of a sequence."""
+    tiles = N * ((D + 63) // 64)
+    found = launches(layout("forward", dtype, T, N, D))
+    assert [kernel for kernel, _, _ in found] == ["recurrence_kernel", "recurrence_join_kernel", "recurrence_kernel"]
+    assert forward is None or found[0][2] == found[2][2] == forward
+    found = launches(layout("backward", dtype, T, N, D))
+    assert [kernel for kernel, _, _ in found] == ["recurrence_backward_kernel", "recurrence_join_kernel", "recurrence_backward_kernel"]
+    steps, waves, pieces = backward
+    assert all(arguments[1:3] == (steps, waves) and groups == tiles * pieces for kernel, arguments, groups in found if kernel == "recurrence_backward_kernel")
