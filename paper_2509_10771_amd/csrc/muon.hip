@@ -708,32 +708,32 @@ static int64_t apply_tiles(const MuonItem& m, int high, int wide) {
   return (int64_t)((short_blocks(m) + high - 1) / high) * ((long_blocks(m) + wide - 1) / wide);
 }
 
-// Products with X take 256 x 128 tiles where these are as many as the GPU has compute units: those of the matrices from some short side on, of as many as take the
-// least time.  In stages of such a tile: the longest for each round over the compute units, 0.175 for each of a 64 x 64 tile of the others on every compute unit,
-// 3 for a launch of the others (2048 x 4096, whose 256 tiles are one round, with 30 x 100 in a launch of its own 97 and 5 us, with 257 tiles 148).
+// Products with X take 256 x 128 tiles where these take less time than 64 x 64 ones, of the matrices from some short side on, whose take the least.  In stages of
+// such a tile: the longest contraction for each round over the compute units; 0.175 of a stage for each of a 64 x 64 tile on every compute unit; 3 for a launch of
+// others.  Steps with and without large tiles, us: 2048 x 2048 842 and 770, 2048 x 3000 942 and 985, 2048 x 3900 1051 and 1186, 2048 x 4096 1070 and 1207,
+// 2300 x 3000 1130 and 1225, 2900 x 2900 2187 and 2004, 3000 x 3000 2272 and 2162, 4096 x 3000 2539 and 2720.  2048 x 4096, whose 256 tiles are one round, with
+// 30 x 100 in a launch of its own 97 and 5 us a product, with 257 tiles 148.
 static void plan_muon_large(MuonTable& t, int count) {
-  int64_t all = 0;
-  for (int i = 0; i < count; ++i) all += apply_tiles(t.item[i], 8, 4);
+  double most = 0;                                       // all of them in 64 x 64 tiles
+  for (int i = 0; i < count; ++i) most += 0.175 / 256 * (double)apply_tiles(t.item[i], 2, 2) * short_blocks(t.item[i]);
   int least = INT32_MAX;
-  double most = 0;
-  for (int i = 0; i < count && all >= 256; ++i) {
+  for (int i = 0; i < count; ++i) {
     const int from = short_blocks(t.item[i]);
+    if (from == least || from >= most) continue;         // (a round takes as many stages)
     int64_t tiles = 0;
     int longest = 0;
-    double medium = 0;
-    bool others = false;
+    double takes = 0;
     for (int j = 0; j < count; ++j) {
       const int P = short_blocks(t.item[j]);
       if (P < from) {
-        others = true;
-        medium += (double)apply_tiles(t.item[j], 2, 2) * P;
+        takes += (takes == 0 ? 3 : 0) + 0.175 / 256 * (double)apply_tiles(t.item[j], 2, 2) * P;
       } else {
         tiles += apply_tiles(t.item[j], 8, 4);
         longest = P > longest ? P : longest;
       }
     }
-    const double takes = (double)((tiles + 255) / 256 * longest) + 0.175 * medium / 256 + (others ? 3 : 0);
-    if (tiles < 256 || (least < INT32_MAX && takes >= most)) continue;
+    takes += (double)((tiles + 255) / 256 * longest);
+    if (takes >= most) continue;
     least = from;
     most = takes;
   }
