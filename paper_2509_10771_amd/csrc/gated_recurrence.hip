@@ -667,8 +667,10 @@ bool rec_whole(const RecArgs& a, int size, int held) {
   return a.D % W == 0 && fits(a.x) && fits(a.g) && fits(a.h) && fits(a.dh) && fits(a.dx) && fits(a.dg);
 }
 
-// Outputs of 16 MB and more, which the dies' L2 could not keep beside the inputs, are written past the caches (gradients of a minibatch's roll-out: 28 us, through
-// them 41); inputs are read past them where the call moves more than the last-level cache's 256 MB and reads them once (a roll-out: 65 us, through them 73).
+// Outputs of 16 MB and more, which the dies' L2 could not keep beside the inputs, are written past the caches; inputs are read past them where the call moves more than
+// the last-level cache's 256 MB and reads them once.  24 steps of fp32 roll-outs of 256 channels, us through the caches, outputs past them, inputs as well: forward
+// 341 environments (8 MB of outputs) 12.5, 11.9, 12.2; 683 (17 MB) 14.0, 14.0, 15.3; 2048 37.6, 29.4, 33.8; 3000 (221 MB moved) 53.3, 46.6, 48.1; 3600 (265 MB) 65, 63.6,
+// 61.9; 4096 74.8, 71.9, 62.1; gradients of 1024 31.2, 28.3, 31.6; of 4096 130, 127, 107.  In bf16 forward 4096 50.5, 38.4, 44.8; 8192 95.8, 94.2, 84.0.
 int stream_of(const RecArgs& a, int size) {
   const double matrix = (double)a.T * a.N * a.D * size;
   const int outputs = a.h.p ? 1 : 2, inputs = a.h.p ? 2 : 3;
@@ -705,9 +707,10 @@ void run(const RecArgs& a, int dtype, bool maps, hipStream_t s) {
 // otherwise four, 64 steps at a time, in about 1024 pieces where these are few (100 steps of 300 sequences of 256 channels in bf16: 14.1 us, with one
 // 16.7; 777 steps of 37 of 200 in fp32: 32, in 512 pieces 37, in 2048 31; 8192 steps of 4 of 1024 in bf16: 72, in 512 pieces 81).
 // Backward, the smallest workgroup that holds the sequence: 32, 64 or 128 steps.  Longer ones are cut into pieces: of 32 up to 2048 steps (777 steps of 37 of 203 in
-// fp16, ragged: 37.5 us, pieces of 64 41.5; 200 steps of 500 of 203 in bf16 129 and 149; 1024 steps of 300 of 256 in bf16 277, pieces of 128 284), where the
-// join has few; beyond, of 128 where these are many and rows aligned (4096 steps of 4 of 1024 in bf16: 58 us, pieces of 64 61), of 64 otherwise (8192
-// steps of 4 of 256 in fp32: 53 us, pieces of 128 55, of 32 58).
+// fp16, ragged: 37.5 us, pieces of 64 41.5, in fp32 57 and 59.5; 200 steps of 500 of 203 in bf16 112 and 123, in fp32 203 and 223; 2000 steps of 16 of 512 in bf16 53.6
+// and 54.3, in fp32 95.9 and 97.5; 1024 steps of 300 of 256 in bf16 270 and 270, in fp32 504 and 497), where the join has few; beyond, of 128 where these
+// are many and rows aligned (4096 steps of 4 of 1024 in bf16: 58 us, pieces of 64 61), of 64 otherwise (8192 steps of 4 of 256 in fp32: 53 us, pieces of 128
+// 55, of 32 58).
 void plan_recurrence(host::Carver& c, RecArgs& a, int dtype, bool backward) {
   const int64_t tiles = (int64_t)a.N * (((int64_t)a.D + TILE - 1) / TILE);
   a.pieces = 1;

@@ -16,7 +16,7 @@
 //
 // Small networks are bound by 17 dependent launches of 4 to 5 us each (actor and critic: 78 us; 2 us of each is the start and the table's load), so a
 // launch takes all matrices, and its wavefronts share the contraction.  A large matrix is bound by the matrix cores at the rate that large products reach on the
-// card: 2048 x 4096 1.05 to 1.12 ms, its products with X 97 to 107 us = 960 to 1060 TFLOP/s of fp16 (a library's 8192^3: 1110).
+// card: 2048 x 4096 1.05 to 1.08 ms, its products with X 101 us = 1020 TFLOP/s of fp16 (a library's 8192^3: 1110), the last, with the weights' step, 118.
 #include <type_traits>
 
 #include "memory.h"
@@ -662,11 +662,11 @@ size_t muon_item_bytes(int32_t rows, int32_t cols) {
 // Symmetric products go through the large tiles, in as many pieces as there are compute units for and of 16 stages of 32 contraction indices or more, where
 // that takes less time than 64 x 64 tiles.  In stages of a large tile, both products together: the first the longest piece for each round over the compute units,
 // and 16 for the sums' way through memory; the second 0.23 of a stage for each of a 64 x 64 tile on every compute unit.  Steps with and without large tiles, us:
-// 1930 x 1930 712 and 645, 2048 x 2048 755 and 778, 2048 x 4096 1057 and 1155, 2304 x 2304 1055 and 1035, 2600 x 2600 1397 and 1470, 2700 x 2700 1797 and
-// 1617, 3456 x 3456 2820 and 2900, 4096 x 4096 4910 and 4445, two of 1536 x 1536 698 and 670, ten of 1000 x 1024 1050 and 972, thirty-two of
-// 600 x 610 1062 and 813.
+// 1930 x 1930 715 and 645, 2048 x 2048 760 and 774, 2048 x 4096 1060 and 1168, 2304 x 2304 1054 and 1025, 2600 x 2600 1283 and 1358, 2700 x 2700 1665 and
+// 1444, 3456 x 3456 2975 and 3107, 4096 x 4096 4913 and 4464, two of 1536 x 1536 700 and 662, ten of 1000 x 1024 1011 and 931, thirty-two of 600 x 610
+// 1073 and 817.
 // It is asked of the matrices from some short side on, of those that save most; the others of the call have launches of their own, which are worth 6 stages (2048 x
-// 4096 with 30 x 100: 1365, all in 64 x 64 tiles 1440).
+// 4096 with 30 x 100 1113, both in 64 x 64 tiles 1188).
 size_t plan_muon_parts(MuonTable& t, int count) {
   int P[RSLX_MUON_MAX_MATRICES], Q[RSLX_MUON_MAX_MATRICES], least = 0;
   for (int i = 0; i < count; ++i) P[i] = short_blocks(t.item[i]), Q[i] = long_blocks(t.item[i]);
@@ -709,13 +709,14 @@ static int64_t apply_tiles(const MuonItem& m, int high, int wide) {
 }
 
 // Products with X take 256 x 128 tiles where these take less time than 64 x 64 ones, of the matrices from some short side on, whose take the least.  In stages of
-// such a tile: the longest contraction for each round over the compute units; 0.175 of a stage for each of a 64 x 64 tile on every compute unit; 3 for a launch of
-// others.  Steps with and without large tiles, us: 2048 x 2048 842 and 770, 2048 x 3000 942 and 985, 2048 x 3900 1051 and 1186, 2048 x 4096 1070 and 1207,
-// 2300 x 3000 1130 and 1225, 2900 x 2900 2187 and 2004, 3000 x 3000 2272 and 2162, 4096 x 3000 2539 and 2720.  2048 x 4096, whose 256 tiles are one round, with
-// 30 x 100 in a launch of its own 97 and 5 us a product, with 257 tiles 148.
+// such a tile: the longest contraction for each round over the compute units; 0.197 of a stage for each of a 64 x 64 tile on every compute unit; 3 for a launch of
+// others.  Steps with and without large tiles, us: 2048 x 2048 (128 of them) 830 and 760, 1500 x 3500 (168) 721 and 740, 2048 x 3000 (192) 924 and 970, 2048 x 4096
+// (256) 1055 and 1193, 2900 x 2900 (276) 2158 and 1988, 3000 x 3000 (288) 2246 and 2122, 3200 x 3200 (325) 2539 and 2441, 3300 x 3300 (338) 2680 and 2700, 2600 x
+// 4096 (352) 1876 and 1922, 3456 x 3456 (378) 2840 and 2983, 4096 x 3000 (384) 2492 and 2674.  2048 x 4096 with 30 x 100 in a launch of its own 1112, with 257 tiles
+// 1373.
 static void plan_muon_large(MuonTable& t, int count) {
   double most = 0;                                       // all of them in 64 x 64 tiles
-  for (int i = 0; i < count; ++i) most += 0.175 / 256 * (double)apply_tiles(t.item[i], 2, 2) * short_blocks(t.item[i]);
+  for (int i = 0; i < count; ++i) most += 0.197 / 256 * (double)apply_tiles(t.item[i], 2, 2) * short_blocks(t.item[i]);
   int least = INT32_MAX;
   for (int i = 0; i < count; ++i) {
     const int from = short_blocks(t.item[i]);
@@ -726,7 +727,7 @@ static void plan_muon_large(MuonTable& t, int count) {
     for (int j = 0; j < count; ++j) {
       const int P = short_blocks(t.item[j]);
       if (P < from) {
-        takes += (takes == 0 ? 3 : 0) + 0.175 / 256 * (double)apply_tiles(t.item[j], 2, 2) * P;
+        takes += (takes == 0 ? 3 : 0) + 0.197 / 256 * (double)apply_tiles(t.item[j], 2, 2) * P;
       } else {
         tiles += apply_tiles(t.item[j], 8, 4);
         longest = P > longest ? P : longest;
@@ -766,7 +767,9 @@ hipError_t launch_muon(MuonTable& t, int count, MuonTable* in_workspace, int ste
   const auto tiles_with_x = [](int high, int wide, bool large) {
     return [=](const MuonItem& m) { return large == (m.large != 0) ? apply_tiles(m, high, wide) : 0; };
   };
-  // of those that are not in pieces or large: the larger tiles that are as many as the GPU has compute units, the smallest where these are fewer
+  // of those that are not in pieces or large: 64 x 64 tiles that are as many as the GPU has compute units, 32 x 32 where these are fewer.  Steps with the one and the
+  // other, us: 896 x 896 (105 of a symmetric product, 196 with X) 167 and 152, 1024 x 1024 (136 and 256) 179 and 186, 1100 x 1100 (171 and 324) 232 and 216, 1400 x
+  // 1400 (253 and 484) 293 and 341
   MuonShape symmetric_shape = MEDIUM, apply_shape = MEDIUM;
   const auto large_tiles = [](const MuonItem& m) { return m.in_pieces ? (int64_t)wide_triangle_tiles(short_blocks(m)) : 0; };
   const unsigned on_pieces = place_items(t, count, MUON_PIECES_GRID, [&](const MuonItem& m) { return large_tiles(m) * t.pieces; });

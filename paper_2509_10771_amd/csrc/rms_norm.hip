@@ -334,8 +334,8 @@ void run_type(const RmsArgs& a, RmsKind kind, int blocks, hipStream_t s) {
   whole ? dispatch_rms<T, true>(a, kind, blocks, s) : dispatch_rms<T, false>(a, kind, blocks, s);
 }
 
-// Outputs of 16 MB and more, which the dies' L2 could not keep beside the inputs, go past the caches: 98304 rows of 512 in bf16 74.6 us, through them 78.8;
-// gradients of 24576 rows of 235 in fp32 23.9 and 27.7.
+// Outputs of 16 MB and more, which the dies' L2 could not keep beside the inputs, go past the caches.  Rows of 512 in bf16: 98304 74.6 us, through them 78.4, into bytes
+// 68.0 and 70.0, gradients 80.8 and 82.7; 16384 12.1 and 13.0, 11.9 and 12.3, 18.1 and 18.7; 8192 (8 to 17 MB) no difference, nor for gradients of 24576 of 235 in fp32.
 constexpr double PAST_BYTES = 16 << 20;
 
 hipError_t run(RmsArgs a, int dtype, RmsKind kind, int blocks, hipStream_t s) {

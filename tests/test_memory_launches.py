@@ -137,7 +137,7 @@ def test_a_small_matrix_adds_no_round_to_a_large_ones_product(launches, large, s
 
 
 @pytest.mark.parametrize("shapes,groups,others", [
-    ("3000x3000", None, "2"), ("2900x2900", None, "2"), ("2600x3400", None, "2"), ("4096x3000", 384, None), ("3500x3500", 392, None), ("2048x3900", 248, None),
+    ("3000x3000", None, "2"), ("2900x2900", None, "2"), ("2600x3400", None, "2"), ("4096x3000", 384, None), ("3200x3200", None, "2"), ("2600x4096", 352, None), ("3456x3456", 378, None), ("1500x3500", 168, None), ("3500x3500", 392, None), ("2048x3900", 248, None),
     ("2300x3000", 216, None), ("2048x2048", None, "2"), ("2047x4065", 256, None), (",".join(["500x520"] * 31 + ["40x33"]), None, "2"), ("2048x4096,1900x1900", 256, "2"),
     ("2048x4096,333x100", 256, "1"), ("777x333,235x512,333x1001,30x100", None, "1"), ("30x100,2040x4090,300x200", 256, "1"), ("2048x2000,1900x600,2000x2048", 256, "2")])
 def test_products_with_x_take_their_forms(launches, shapes, groups, others):
